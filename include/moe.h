@@ -142,7 +142,9 @@ typedef enum {
     MOE_BUF_WS_FORWARD = 1,  /* ws of moe_forward / moe_layer_forward         */
     MOE_BUF_WS_BACKWARD = 2, /* ws of moe_backward / moe_layer_backward       */
     MOE_BUF_CONTEXT = 3,     /* ctx of the fused calls                        */
-    MOE_BUF_WS_ADAM = 4      /* ws of moe_expert_adam_factored                */
+    MOE_BUF_WS_ADAM = 4,     /* ws of moe_expert_adam_factored                */
+    MOE_BUF_WS_NORM = 5,     /* ws of moe_norm_in_bwd / moe_norm_out_bwd      */
+    MOE_BUF_WS_FEW = 6       /* ws of moe_forward_few                         */
 } moe_buffer_role;
 int32_t moe_check_buffer_sizes(const moe_config *cfg, int32_t which, size_t bytes);
 
@@ -414,6 +416,100 @@ int32_t moe_layer_backward(const moe_config *cfg, const void *dOut, const void *
                            const void *b2, const uint8_t *keep_bits, float drop_prob, const void *ctx, void *dX,
                            float *dWg, float *dWnoise, void *dW1, void *db1, void *dW2, void *db2, void *ws,
                            void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Norms around the block. A pre-norm block with an output norm, a gate and a residual scale is
+ *     xn  = x * rsqrt(mean(x^2) + eps) * w                                  (moe_norm_in; then the layer: y from xn)
+ *     out = residual_scale * x + gate * (y * rsqrt(mean(y^2) + eps) * w)    (moe_norm_out)
+ * and moe_norm_out gives the norm before the NEXT block with it, while the row is at hand:
+ *     next = out * rsqrt(mean(out^2) + eps) * w_next                        (of `out` before it is rounded)
+ * Means are over the d columns of a row. w, w_next [d] float; gate [ceil(T / rows_per_gate), d] act: row t takes gate row
+ * t / rows_per_gate (1: a gate per token; the length of a sequence: one per sequence; T: one for all), or NULL for ones
+ * (rows_per_gate is then ignored). w_next NULL: no norm behind it; next and rstd_next are then ignored.
+ * rstd, rstd_next [T] float: the factors rsqrt(mean + eps) for the backward pass.
+ * Of cfg only T, d and act matter. d is at most MOE_NORM_MAX_D (MOE_ERR_UNSUPPORTED beyond). eps > 0, residual_scale finite.
+ * y may come from any call that writes [T,d]: moe_forward, moe_forward_few, moe_combine, moe_combine_balanced.
+ * xn may be x, out may be x or y, and next may be the one of them that out is not.
+ * ------------------------------------------------------------------------------------------ */
+#define MOE_NORM_MAX_D 16384
+
+/* in : x [T,d] act, w [d]   out: xn [T,d] act, rstd [T] (may be NULL) */
+int32_t moe_norm_in(const moe_config *cfg, const void *x, const float *w, float eps, void *xn, float *rstd, void *stream);
+
+/* dX = dres + the adjoint of moe_norm_in: dres [T,d] act is the gradient that reaches x beside the norm (the dX of
+ * moe_norm_out_bwd), or NULL.   in: dxn [T,d] act, x, w, rstd   out: dX [T,d] act, dw [d] float. dX may be dxn, dres or x.
+ * ws: moe_norm_workspace_bytes */
+int32_t moe_norm_in_bwd(const moe_config *cfg, const void *dxn, const void *x, const float *w, const float *rstd, const void *dres,
+                        void *dX, float *dw, void *ws, void *stream);
+
+/* out: out [T,d] act, next [T,d] act, rstd, rstd_next [T] */
+int32_t moe_norm_out(const moe_config *cfg, const void *x, const void *y, const float *w, const void *gate, int32_t rows_per_gate,
+                     float residual_scale, const float *w_next, float eps, void *out, void *next, float *rstd, float *rstd_next,
+                     void *stream);
+
+/* in : dOut, dNext [T,d] act, out, y, and the arguments of the forward call
+ * out: dX, dY [T,d] act (dX: of x through the residual connection alone), dw, dw_next [d] float, dgate like gate.
+ * Without w_next: dNext, out, rstd_next and dw_next are ignored. Without gate: dgate is ignored.
+ * dX and dY may each take the place of a different one of dOut, dNext, out and y. ws: moe_norm_workspace_bytes. */
+int32_t moe_norm_out_bwd(const moe_config *cfg, const void *dOut, const void *dNext, const void *out, const void *y, const float *w,
+                         const void *gate, int32_t rows_per_gate, float residual_scale, const float *w_next, const float *rstd,
+                         const float *rstd_next, void *dX, void *dY, float *dw, void *dgate, float *dw_next, void *ws, void *stream);
+int32_t moe_norm_workspace_bytes(const moe_config *cfg, size_t *host_bytes);
+
+/* ------------------------------------------------------------------------------------------
+ * The layer for a few tokens (serving: T <= MOE_FEW_MAX_TOKENS, flat layers, no gating noise, no losses, nothing kept for a
+ * backward pass), in two launches: what moe_forward with noise 0 computes,
+ *     logits = x.W_g by the fixed chain of moe_gate, topk_idx / gates as moe_gate chooses them,
+ *     hid = relu(x.W1 + b1) (one rounding to the act type), y = sum_s gates_s * (hid_s.W2 + b2) in float, one rounding.
+ * The routing is moe_gate's without its screen bit for bit. T larger or a hierarchical layer: MOE_ERR_UNSUPPORTED.
+ * in : x [T,d] act, Wg [d,n], W1, b1, W2, b2 as in moe_forward
+ * out: y [T,d] act; topk_idx [T,k], gates [T,k] (each may be NULL).   ws: moe_few_workspace_bytes, its own in every call that may
+ * run at the same time. MOE_ERR_TIMEOUT in its status word: see moe_check_status.
+ * ------------------------------------------------------------------------------------------ */
+#define MOE_FEW_MAX_TOKENS 64
+int32_t moe_few_workspace_bytes(const moe_config *cfg, size_t *host_bytes);
+int32_t moe_forward_few(const moe_config *cfg, const void *x, const float *Wg, const void *W1, const void *b1, const void *W2,
+                        const void *b2, void *y, int32_t *topk_idx, float *gates, void *ws, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * AdamW over a list of tensors in one pass (a launch for every 96 of them), moments in float or in 8 bits. For every element
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2      (g times grad_scale)
+ *     w = w - lr * (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay * w)
+ * in float, one rounding to w's type. With `master` (float, only beside bf16 weights) the step is taken on the master and w is
+ * its rounding; without it small steps on bf16 weights are lost in that rounding.
+ * moment_bits 8: m and sqrt(v) as e4m3 codes [count] and a float scale per MOE_ADAMW_BLOCK consecutive elements, value = code * scale,
+ * scale = the block's largest magnitude / 448 (all zero: 0). Rounding is up or down at random, the chances as the distances: bits 0-15 (m)
+ * and 16-31 (sqrt(v)) of mix((first + i) mod 2^32 ^ mix(seed + floor((first + i) / 2^32) * 0x9e3779b9)) of element i, mix being
+ * x ^= x >> 16, x *= 0x7feb352d, x ^= x >> 15, x *= 0x846ca68b, x ^= x >> 16: give every step its own seed and the tensors of a
+ * step ranges of `first` that do not overlap. v above 0 keeps a code above 0. An element that is no finite number is held as
+ * NaN and leaves its block's scale to the others. Zeroed codes and scales are the state before the first step.
+ * All pointers but host_tensors, host_params are device pointers, w, g, master, m, v on 32-byte boundaries. The list is read before the call
+ * returns; tensors of a list may not overlap. rates: NULL, or a moe_adamw_rates in device memory that takes the place of lr, step, grad_scale and
+ * seed when the kernels run, for recorded graphs.
+ * ------------------------------------------------------------------------------------------ */
+#define MOE_ADAMW_BLOCK 128
+typedef struct moe_adamw_tensor {
+    void *w;                   /* [count], in-out */
+    const void *g;             /* [count] */
+    float *master;             /* [count], in-out, or NULL */
+    void *m, *v;               /* [count] float or e4m3 codes, in-out */
+    float *m_scale, *v_scale;  /* [ceil(count / MOE_ADAMW_BLOCK)] with 8-bit moments, in-out */
+    int64_t count, first;      /* first: a multiple of MOE_ADAMW_BLOCK, the number of element 0 among the step's elements */
+    int32_t w_type, g_type;    /* moe_dtype */
+    int32_t moment_bits;       /* 32 or 8 */
+    float weight_decay;
+} moe_adamw_tensor;
+typedef struct moe_adamw_params {
+    double lr, beta1, beta2, eps, grad_scale;
+    int32_t step;              /* from 1 on */
+    uint32_t seed;
+} moe_adamw_params;
+typedef struct moe_adamw_rates {
+    float lr, bias1, bias2, grad_scale; /* bias1 = 1 - beta1^step, bias2 = 1 - beta2^step */
+    uint32_t seed;
+} moe_adamw_rates;
+int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe_adamw_params *host_params, const moe_adamw_rates *rates,
+                  void *stream);
 
 #ifdef __cplusplus
 }

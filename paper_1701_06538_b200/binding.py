@@ -26,7 +26,9 @@ EXPORTS = ["moe_debug_launch_count", "moe_validate", "moe_query_sizes", "moe_wor
            "moe_backward", "moe_combine_layer", "moe_combine_layer_bwd", "moe_layer_forward", "moe_layer_backward",
            "moe_expert_adam_factored", "moe_check_buffer_sizes", "moe_debug_wait_timeout", "moe_debug_bounds_violations",
            "moe_expert_ffn_bits", "moe_expert_ffn_bwd_bits", "moe_query_balanced_sizes", "moe_gate_balanced", "moe_dispatch_balanced", "moe_combine_balanced",
-           "moe_combine_balanced_bwd", "moe_gate_balanced_bwd", "moe_dispatch_balanced_bwd"]
+           "moe_combine_balanced_bwd", "moe_gate_balanced_bwd", "moe_dispatch_balanced_bwd",
+           "moe_norm_in", "moe_norm_in_bwd", "moe_norm_out", "moe_norm_out_bwd", "moe_norm_workspace_bytes", "moe_few_workspace_bytes",
+           "moe_forward_few", "moe_adamw"]
 
 
 class MoeError(RuntimeError):
@@ -55,6 +57,16 @@ class moe_ctx_layout(ctypes.Structure):
 
 class moe_balanced_sizes(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int64) for name in ("m", "R", "mask_words", "ws_bytes")]
+
+
+class moe_adamw_tensor(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("w", "g", "master", "m", "v", "m_scale", "v_scale")] + \
+               [(name, ctypes.c_int64) for name in ("count", "first")] + \
+               [(name, ctypes.c_int32) for name in ("w_type", "g_type", "moment_bits")] + [("weight_decay", ctypes.c_float)]
+
+
+class moe_adamw_params(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [("step", ctypes.c_int32), ("seed", ctypes.c_uint32)]
 
 
 _lib = None
@@ -308,6 +320,89 @@ def moe_layer_backward(cfg, dOut, x, Wg, Wnoise, noise, W1, b1, W2, b2, keep_bit
                        dW1, db1, dW2, db2, ws):
     _call("moe_layer_backward", cfg, dOut, x, Wg, Wnoise, noise, W1, b1, W2, b2, keep_bits, float(drop_prob), ctx, dX,
           dWg, dWnoise, dW1, db1, dW2, db2, ws)
+
+
+def _one_size(name, cfg):
+    out = ctypes.c_size_t(0)
+    status = getattr(lib(), name)(ctypes.byref(cfg), ctypes.byref(out))
+    if status:
+        raise MoeError(name, status)
+    return out.value
+
+
+def moe_norm_workspace_bytes(cfg) -> int:
+    return _one_size("moe_norm_workspace_bytes", cfg)
+
+
+def moe_norm_in(cfg, x, w, eps, xn, rstd):
+    _call("moe_norm_in", cfg, x, w, float(eps), xn, rstd)
+
+
+def moe_norm_in_bwd(cfg, dxn, x, w, rstd, dres, dX, dw, ws):
+    _call("moe_norm_in_bwd", cfg, dxn, x, w, rstd, dres, dX, dw, ws)
+
+
+def moe_norm_out(cfg, x, y, w, gate, rows_per_gate, residual_scale, w_next, eps, out, next, rstd, rstd_next):
+    _call("moe_norm_out", cfg, x, y, w, gate, int(rows_per_gate), float(residual_scale), w_next, float(eps), out, next, rstd, rstd_next)
+
+
+def moe_norm_out_bwd(cfg, dOut, dNext, out, y, w, gate, rows_per_gate, residual_scale, w_next, rstd, rstd_next, dX, dY, dw, dgate, dw_next,
+                     ws):
+    _call("moe_norm_out_bwd", cfg, dOut, dNext, out, y, w, gate, int(rows_per_gate), float(residual_scale), w_next, rstd, rstd_next, dX, dY,
+          dw, dgate, dw_next, ws)
+
+
+def moe_few_workspace_bytes(cfg) -> int:
+    return _one_size("moe_few_workspace_bytes", cfg)
+
+
+def moe_forward_few(cfg, x, Wg, W1, b1, W2, b2, y, topk_idx, gates, ws):
+    _call("moe_forward_few", cfg, x, Wg, W1, b1, W2, b2, y, topk_idx, gates, ws)
+
+
+class moe_adamw_list:
+    """The tensors of an optimiser step, made once for a model. `tensors`: dicts with w, g, m, v and, where they apply, master, m_scale,
+    v_scale (8-bit moments: m and v are torch.float8_e4m3fn or uint8), weight_decay (0), first (a running number from 0, tensor behind tensor).
+    Keeps references to the tensors: their addresses are what the call gets."""
+
+    def __init__(self, tensors):
+        self.tensors = [dict(t) for t in tensors]
+        self.array = (moe_adamw_tensor * max(len(self.tensors), 1))()
+        types, at, self.device = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}, 0, None
+        for t, r in zip(self.tensors, self.array):
+            count = t["w"].numel()
+            eight = t["m"].element_size() == 1
+            moment = (torch.float8_e4m3fn, torch.uint8) if eight else (torch.float32,)
+            blocks = -(-count // 128)
+            want = dict(w=(tuple(types), count), g=(tuple(types), count), master=((torch.float32,), count), m=(moment, count), v=(moment, count),
+                        m_scale=((torch.float32,), blocks), v_scale=((torch.float32,), blocks))
+            for q, (dtypes, n) in want.items():
+                x = t.get(q)
+                if x is None:
+                    if q in ("w", "g", "m", "v") or (eight and q != "master"):
+                        raise ValueError(f"moe_adamw_list: {q} is missing")
+                    continue
+                if x.dtype not in dtypes or x.numel() != n:
+                    raise ValueError(f"moe_adamw_list: {q} has {x.numel()} elements of {x.dtype}, wanted {n} of {dtypes}")
+                if self.device is None:
+                    self.device = x.get_device()
+                if x.get_device() != self.device:
+                    raise ValueError("moe_adamw_list: the tensors are on different devices")
+                setattr(r, q, _p(x))
+            r.count, r.first = count, t.get("first", at)
+            r.w_type, r.g_type, r.moment_bits, r.weight_decay = types[t["w"].dtype], types[t["g"].dtype], 8 if eight else 32, t.get("weight_decay", 0.0)
+            at = max(at, r.first + 128 * blocks)
+
+
+def moe_adamw(tensors, lr, beta1, beta2, eps, step, seed=0, grad_scale=1.0, rates=None):
+    """`tensors`: a moe_adamw_list. `rates`: five 4-byte words of device memory (lr, 1 - beta1^step, 1 - beta2^step, grad_scale as floats, seed) that
+    are read when the kernels run."""
+    if tensors.device is not None and tensors.device != torch.cuda.current_device():
+        raise ValueError("moe_adamw: the tensors are not on the current device")
+    p = moe_adamw_params(lr, beta1, beta2, eps, grad_scale, step, seed & 0xffffffff)
+    status = lib().moe_adamw(tensors.array, ctypes.c_int32(len(tensors.tensors)), ctypes.byref(p), ctypes.c_void_p(_p(rates)), ctypes.c_void_p(_stream()))
+    if status:
+        raise MoeError("moe_adamw", status)
 
 
 # ----------------------------------------------------------------------------------------------

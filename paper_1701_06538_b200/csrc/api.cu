@@ -893,6 +893,13 @@ int32_t moe_check_buffer_sizes(const moe_config *cfg, int32_t which, size_t byte
         case MOE_BUF_WS_BACKWARD: need = s.ws_bwd_bytes; break;
         case MOE_BUF_CONTEXT: need = s.ctx_bytes; break;
         case MOE_BUF_WS_ADAM: need = s.ws_adam_bytes; break;
+        case MOE_BUF_WS_NORM:
+        case MOE_BUF_WS_FEW: {
+            size_t own;
+            MOE_TRY(which == MOE_BUF_WS_NORM ? moe_norm_workspace_bytes(cfg, &own) : moe_few_workspace_bytes(cfg, &own));
+            need = (int64_t)own;
+            break;
+        }
         default: return MOE_ERR_INVALID_ARG;
     }
     return (int64_t)bytes >= need ? MOE_OK : MOE_ERR_WORKSPACE;
