@@ -458,9 +458,9 @@ int32_t moe_norm_workspace_bytes(const moe_config *cfg, size_t *host_bytes);
 
 /* ------------------------------------------------------------------------------------------
  * The layer for a few tokens (serving: T <= MOE_FEW_MAX_TOKENS, flat layers, no gating noise, no losses, nothing kept for a
- * backward pass), in two launches: what moe_forward with noise 0 computes,
+ * backward pass), in two launches (three with more than 256 experts): what moe_forward with noise 0 computes,
  *     logits = x.W_g by the fixed chain of moe_gate, topk_idx / gates as moe_gate chooses them,
- *     hid = relu(x.W1 + b1) (one rounding to the act type), y = sum_s gates_s * (hid_s.W2 + b2) in float, one rounding.
+ *     hid = relu(x.W1 + b1) (float; bf16 layers: two bf16 terms), y = sum_s gates_s * (hid_s.W2 + b2) in float, one rounding.
  * The routing is moe_gate's without its screen bit for bit. T larger or a hierarchical layer: MOE_ERR_UNSUPPORTED.
  * in : x [T,d] act, Wg [d,n], W1, b1, W2, b2 as in moe_forward
  * out: y [T,d] act; topk_idx [T,k], gates [T,k] (each may be NULL).   ws: moe_few_workspace_bytes, its own in every call that may

@@ -36,6 +36,7 @@ int32_t launch_norm_grads(const NormGradArgs &a, cudaStream_t st);
 int32_t launch_adamw(const moe_adamw_tensor *tensors, int32_t count, const moe_adamw_params &p, const moe_adamw_rates *rates, cudaStream_t st);
 
 // ----------------------------------------------------------------------------- a few tokens (few_tokens.cu)
+unsigned long long bounds_violations_few_tokens();  // see moe_internal.cuh
 int64_t few_tokens_bytes(const moe_config &c);
 int32_t launch_few_tokens(const moe_config &c, const void *x, const float *Wg, const void *W1, const void *b1, const void *W2, const void *b2, void *y,
                           int32_t *topk_idx, float *gates, void *ws, cudaStream_t st);
