@@ -10,6 +10,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include <cuda_fp8.h>
 
 #include "block.cuh"
@@ -21,6 +23,9 @@ namespace {
 constexpr int THREADS = 256, EACH = 8;            // elements a thread holds at a time
 constexpr int STEP = THREADS * EACH;              // elements a block holds at a time: 16 blocks of codes, 16 lanes each
 constexpr int CHUNK = 4 * STEP;                   // elements of a block of the grid
+#ifndef EIGHT_BLOCKS
+#define EIGHT_BLOCKS 4
+#endif
 constexpr int MAX_LIST = 96;                      // tensors of a launch (a launch's parameters hold them: 9 KiB)
 
 struct Entry {
@@ -31,7 +36,7 @@ struct Entry {
     float *m_scale, *v_scale;
     int64_t count, first;
     float decay;
-    int32_t kind;  // bit 0: bf16 weights, 1: bf16 gradients, 2: float masters, 3: 8-bit moments
+    int32_t kind;  // bit 0: bf16 weights, 1: bf16 gradients, 2: float masters
 };
 struct Batch {
     Entry t[MAX_LIST];
@@ -40,22 +45,54 @@ struct Batch {
 };
 struct Constants { float beta1, one_beta1, beta2, one_beta2, eps; };
 
-// The low-bias hash of 32 bits of C. Wellons ("Prospecting for Hash Functions", 2018): two multiplications between three shifts
-__device__ __forceinline__ uint32_t mix(uint32_t x) {
+// The low-bias hash of 32 bits of C. Wellons ("Prospecting for Hash Functions", 2018): two multiplications between three shifts. Without the last shift, which changes the lower half alone
+__device__ __forceinline__ uint32_t mix_but_last(uint32_t x) {
     x = (x ^ (x >> 16)) * 0x7feb352du;
-    x = (x ^ (x >> 15)) * 0x846ca68bu;
+    return (x ^ (x >> 15)) * 0x846ca68bu;
+}
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+    x = mix_but_last(x);
     return x ^ (x >> 16);
 }
 
-// |q| <= 448 up or down to a multiple of its code's unit: the 20 bits below e4m3's three are added a dither (at most 2^20 - 8) and cut off. Below 2^-6
-// the unit stays 2^-9, which is that of the numbers from 2^-6 to 2^-5.
-__device__ __forceinline__ float dithered(float q, uint32_t bits16) {
-    const float size = fabsf(q);
-    const bool small = size < 0.015625f;
-    const float up = small ? size + 0.015625f : size;
-    float z = __uint_as_float((__float_as_uint(up) + bits16 * 16u + 8u) & ~0xfffffu);
-    z = small ? z - 0.015625f : z;
-    return fminf(z, 448.0f);
+// The hardware's root and reciprocal, within two units of the last place: of the divisor, and of a second moment that is kept in four bits
+__device__ __forceinline__ float root_of(float v) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float normal_root_of(float v) {  // 0 of what is below float's smallest normal number: four instructions less
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {  // of normal numbers; 0 beyond 2^126
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// Two at a time: one instruction for two products or sums, each rounded as by itself
+__device__ __forceinline__ float2 mul_two(float2 a, float2 b) {
+    float2 r;
+    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 c, a, b;\n mov.b64 {%0, %1}, c;\n}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 add_two(float2 a, float2 b) {
+    float2 r;
+    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 c, a, b;\n mov.b64 {%0, %1}, c;\n}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma_two(float2 a, float2 b, float2 d) {
+    float2 r;
+    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 c, a, b, c;\n mov.b64 {%0, %1}, c;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(d.x), "f"(d.y));
+    return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
 template <typename T> __device__ __forceinline__ void load8(const T *p, int64_t at, int64_t live, float (&v)[EACH]) {
@@ -94,62 +131,71 @@ template <typename T> __device__ __forceinline__ void store8(T *p, int64_t at, i
     for (int i = 0; i < EACH; ++i)
         if (i < live) p[at + i] = from_f32<T>(v[i]);
 }
-__device__ __forceinline__ void load_codes(const uint8_t *p, int64_t at, int64_t live, float scale, float (&v)[EACH]) {
+__device__ __forceinline__ uint2 load_codes(const uint8_t *p, int64_t at, int64_t live) {
+    if (live >= EACH) return *reinterpret_cast<const uint2 *>(p + at);
     uint32_t c[2] = {0u, 0u};
-    if (live >= EACH) {
-        const uint2 two = *reinterpret_cast<const uint2 *>(p + at);
-        c[0] = two.x; c[1] = two.y;
-    } else {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (i < live) c[i / 4] |= (uint32_t)p[at + i] << (8 * (i % 4));
-    }
+    for (int i = 0; i < EACH; ++i)
+        if (i < live) c[i / 4] |= (uint32_t)p[at + i] << (8 * (i % 4));
+    return make_uint2(c[0], c[1]);
+}
+__device__ __forceinline__ void decode(const uint2 &two, float (&v)[EACH]) {
+    const uint32_t c[2] = {two.x, two.y};
 #pragma unroll
     for (int i = 0; i < EACH; i += 2) {
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c[i / 4] >> (8 * (i % 4))), __NV_E4M3);
         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-        v[i] = f.x * scale;
-        v[i + 1] = f.y * scale;
+        v[i] = f.x;
+        v[i + 1] = f.y;
     }
 }
-// The codes of a block and its scale; an element that is no finite number is held as a NaN and has no part in the scale
-template <bool ROOT>
-__device__ __forceinline__ void store_codes(uint8_t *p, float *scales, int64_t at, int64_t live, const float (&v)[EACH], const uint32_t (&bits)[EACH]) {
+// The codes of a block and its scale; an element that is no finite number is held as a NaN and has no part in the scale. ROOT: values of 0 and more, whose codes stay above 0 (they
+// divide). bits: the hash without its last shift; its upper half is that of the hash, the lower half changes
+template <bool ROOT, bool FULL>
+__device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, int64_t live, const float (&v)[EACH], const uint32_t (&bits)[EACH]) {
     float largest = 0.0f;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const float a = fabsf(v[i]);
-        largest = a <= FLT_MAX ? fmaxf(largest, a) : largest;
-    }
+    for (int i = 0; i < EACH; ++i) largest = max_nan(largest, fabsf(v[i]));
 #pragma unroll
-    for (int off = 8; off > 0; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, off));
-    const float scale = largest > 0.0f ? fmaxf(largest * (1.0f / 448.0f), FLT_MIN) : 0.0f, by = scale > 0.0f ? scale : 1.0f;
+    for (int off = 8; off > 0; off >>= 1) largest = max_nan(largest, __shfl_xor_sync(0xffffffffu, largest, off));
+    const bool odd = __any_sync(0xffffffffu, !(largest <= FLT_MAX));  // rare: the largest of the others
+    if (odd) {
+        largest = 0.0f;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) largest = fabsf(v[i]) <= FLT_MAX ? fmaxf(largest, fabsf(v[i])) : largest;
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, off));
+    }
+    const float scale = largest > 0.0f ? fmaxf(largest * (1.0f / 448.0f), FLT_MIN) : 0.0f, by = largest > 0.0f ? reciprocal(scale) : 0.0f;
     uint32_t c[2] = {0u, 0u};
+    // Up or down to a multiple of the code's unit: the 20 bits below e4m3's three are added a dither (16 random bits in bits 4 to 19, and 8) and cut off. Below 2^-6
+    // the unit stays 2^-9, which is that of the numbers from 2^-6 to 2^-5. (Up from 448 gives 480, which the conversion takes for 448.)
 #pragma unroll
     for (int i = 0; i < EACH; i += 2) {
-        float z[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float q = v[i + j] / by;
-            float t = dithered(q, ROOT ? bits[i + j] >> 16 : bits[i + j] & 0xffffu);
-            if (ROOT) t = q > 0.0f ? fmaxf(t, 0.001953125f) : t;  // a second moment that is not 0 stays above 0: it divides
-            t = fabsf(v[i + j]) <= FLT_MAX ? t : __int_as_float(0x7fffffff);
-            z[j] = copysignf(t, q);
-        }
-        const __nv_fp8x2_storage_t two = __nv_cvt_float2_to_fp8x2(make_float2(z[0], z[1]), __NV_SATFINITE, __NV_E4M3);
+        const float2 size = mul_two(make_float2(fabsf(v[i]), fabsf(v[i + 1])), both(by));
+        const float2 shift = make_float2(size.x < 0.015625f ? 0.015625f : 0.0f, size.y < 0.015625f ? 0.015625f : 0.0f), up = add_two(size, shift);
+        auto cut = [&](float u, uint32_t x) { return __uint_as_float((__float_as_uint(u) + (((ROOT ? x >> 12 : (x ^ (x >> 16)) << 4) & 0xffff0u) | 8u)) & ~0xfffffu); };
+        float2 z = add_two(make_float2(cut(up.x, bits[i]), cut(up.y, bits[i + 1])), make_float2(-shift.x, -shift.y));
+        if (ROOT) z = make_float2(fmaxf(z.x, size.x > 0.0f ? 0.001953125f : 0.0f), fmaxf(z.y, size.y > 0.0f ? 0.001953125f : 0.0f));
+        else z = make_float2(copysignf(z.x, v[i]), copysignf(z.y, v[i + 1]));
+        const __nv_fp8x2_storage_t two = __nv_cvt_float2_to_fp8x2(z, __NV_SATFINITE, __NV_E4M3);
         c[i / 4] |= (uint32_t)two << (8 * (i % 4));
     }
-    if (live >= EACH) {
-        *reinterpret_cast<uint2 *>(p + at) = make_uint2(c[0], c[1]);
+    if (odd)
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (!(fabsf(v[i]) <= FLT_MAX)) c[i / 4] |= 0x7fu << (8 * (i % 4));
+    if (FULL || live >= EACH) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(c[0], c[1]);
     } else {
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            if (i < live) p[at + i] = (uint8_t)(c[i / 4] >> (8 * (i % 4)));
+            if (i < live) p[i] = (uint8_t)(c[i / 4] >> (8 * (i % 4)));
     }
-    if (at % MOE_ADAMW_BLOCK == 0 && live > 0) scales[at / MOE_ADAMW_BLOCK] = scale;
+    if (threadIdx.x % (MOE_ADAMW_BLOCK / EACH) == 0 && (FULL || live > 0)) *scale_at = scale;
 }
 
-template <typename WT, typename GT, bool MASTER, bool EIGHT>
+template <typename WT, typename GT, bool MASTER>
 __device__ __forceinline__ void update(const Entry &t, int64_t chunk, const Constants &k, const moe_adamw_rates &r) {
     const float step = r.lr / r.bias1, root_by = 1.0f / sqrtf(r.bias2), keep = r.lr * t.decay;
     const int64_t end = min(t.count, (chunk + 1) * CHUNK);
@@ -159,46 +205,84 @@ __device__ __forceinline__ void update(const Entry &t, int64_t chunk, const Cons
         if constexpr (MASTER) load8(t.master, at, live, w);
         else load8(static_cast<const WT *>(t.w), at, live, w);
         load8(static_cast<const GT *>(t.g), at, live, g);
-        uint32_t bits[EACH];
-        if constexpr (EIGHT) {
-            const int64_t number = t.first + at;
-            const uint32_t key = mix(r.seed + (uint32_t)(number >> 32) * 0x9e3779b9u);  // a multiple of EACH: the upper half is that of all eight
-            const float ms = live > 0 ? t.m_scale[at / MOE_ADAMW_BLOCK] : 0.0f, vs = live > 0 ? t.v_scale[at / MOE_ADAMW_BLOCK] : 0.0f;
-            load_codes(static_cast<const uint8_t *>(t.m), at, live, ms, m);
-            load_codes(static_cast<const uint8_t *>(t.v), at, live, vs, v);
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                bits[i] = mix(((uint32_t)number + i) ^ key);
-                v[i] *= v[i];
-            }
-        } else {
-            load8(static_cast<const float *>(t.m), at, live, m);
-            load8(static_cast<const float *>(t.v), at, live, v);
-        }
-        float root[EACH];
+        load8(static_cast<const float *>(t.m), at, live, m);
+        load8(static_cast<const float *>(t.v), at, live, v);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const float gi = g[i] * r.grad_scale;
             m[i] = k.beta1 * m[i] + k.one_beta1 * gi;
             v[i] = k.beta2 * v[i] + k.one_beta2 * (gi * gi);
-            root[i] = sqrtf(v[i]);
-            w[i] = w[i] - (step * (m[i] / (root[i] * root_by + k.eps)) + keep * w[i]);
+            w[i] = w[i] - (step * __fdividef(m[i], fmaf(root_of(v[i]), root_by, k.eps)) + keep * w[i]);
         }
         if constexpr (MASTER) store8(t.master, at, live, w);
         store8(static_cast<WT *>(t.w), at, live, w);
-        if constexpr (EIGHT) {
-            __syncwarp();  // a block's scales have been read by all of its lanes
-            store_codes<false>(static_cast<uint8_t *>(t.m), t.m_scale, at, live, m, bits);
-            store_codes<true>(static_cast<uint8_t *>(t.v), t.v_scale, at, live, root, bits);
-        } else {
-            store8(static_cast<float *>(t.m), at, live, m);
-            store8(static_cast<float *>(t.v), at, live, v);
-        }
+        store8(static_cast<float *>(t.m), at, live, m);
+        store8(static_cast<float *>(t.v), at, live, v);
     }
 }
 
-// A block finds its tensor in the list and takes CHUNK elements of it.
-__global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Batch b, Constants k, moe_adamw_rates given, const moe_adamw_rates *read) {
+// With 8-bit moments the arithmetic is as much as the memory: 93 instructions an element as it was written first, 1218 us for 268 million elements, whose bytes take 415. FULL: a chunk
+// without a tensor's end
+template <typename WT, typename GT, bool MASTER, bool FULL>
+__device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, const Constants &k, const moe_adamw_rates &r) {
+    using MT = typename std::conditional<MASTER, float, WT>::type;  // of what the step is taken on
+    const float down = -r.lr / r.bias1, root_by = 1.0f / sqrtf(r.bias2), keep = 1.0f - r.lr * t.decay;
+    const float by_g = k.one_beta1 * r.grad_scale, by_gg = k.one_beta2 * r.grad_scale * r.grad_scale;
+    const int64_t at = chunk * CHUNK + threadIdx.x * EACH;
+    WT *w_at = static_cast<WT *>(t.w) + at;
+    MT *from = MASTER ? reinterpret_cast<MT *>(t.master) + at : reinterpret_cast<MT *>(w_at);
+    const GT *g_at = static_cast<const GT *>(t.g) + at;
+    uint8_t *m_at = static_cast<uint8_t *>(t.m) + at, *v_at = static_cast<uint8_t *>(t.v) + at;
+    float *ms_at = t.m_scale + at / MOE_ADAMW_BLOCK, *vs_at = t.v_scale + at / MOE_ADAMW_BLOCK;
+    int64_t live = FULL ? EACH : t.count - at;  // at most 0 behind the end
+    uint64_t number = (uint64_t)(t.first + at);  // a multiple of EACH: adding is setting bits
+    const uint32_t seed = r.seed;
+#pragma unroll 1
+    for (int i = 0; i < CHUNK / STEP; ++i) {
+        if (!FULL && chunk * CHUNK + i * STEP >= t.count) break;  // the whole block
+        float g[EACH], m[EACH], root[EACH], w[EACH];
+        load8(from, 0, live, w);
+        load8(g_at, 0, live, g);
+        const uint2 m_codes = load_codes(m_at, 0, live), v_codes = load_codes(v_at, 0, live);
+        const float ms = FULL || live > 0 ? *ms_at : 0.0f, vs = FULL || live > 0 ? *vs_at : 0.0f;
+        const uint32_t key = mix(seed + (uint32_t)(number >> 32) * 0x9e3779b9u) ^ (uint32_t)number;
+        uint32_t bits[EACH];
+        decode(m_codes, m);
+        decode(v_codes, root);
+        const float by_m = k.beta1 * ms;
+#pragma unroll
+        for (int e = 0; e < EACH; e += 2) {
+            bits[e] = mix_but_last(key ^ e);
+            bits[e + 1] = mix_but_last(key ^ (e + 1));
+            const float2 gg = make_float2(g[e], g[e + 1]);
+            const float2 mm = fma_two(make_float2(m[e], m[e + 1]), both(by_m), mul_two(both(by_g), gg));
+            const float2 old = mul_two(make_float2(root[e], root[e + 1]), both(vs));
+            const float2 vv = fma_two(mul_two(both(k.beta2), old), old, mul_two(mul_two(both(by_gg), gg), gg));
+            const float2 rt = make_float2(normal_root_of(vv.x), normal_root_of(vv.y)), den = fma_two(rt, both(root_by), both(k.eps));
+            const float2 ww = fma_two(mul_two(mm, both(down)), make_float2(reciprocal(den.x), reciprocal(den.y)), mul_two(make_float2(w[e], w[e + 1]), both(keep)));
+            m[e] = mm.x; m[e + 1] = mm.y;
+            root[e] = rt.x; root[e + 1] = rt.y;
+            w[e] = ww.x; w[e + 1] = ww.y;
+        }
+        if constexpr (MASTER) store8(from, 0, live, w);
+        store8(w_at, 0, live, w);
+        __syncwarp();  // a block's scales have been read by all of its lanes
+        store_codes<false, FULL>(m_at, ms_at, live, m, bits);
+        store_codes<true, FULL>(v_at, vs_at, live, root, bits);
+        w_at += STEP; from += STEP; g_at += STEP; m_at += STEP; v_at += STEP; ms_at += STEP / MOE_ADAMW_BLOCK; vs_at += STEP / MOE_ADAMW_BLOCK;
+        number += STEP;
+        if (!FULL) live -= STEP;
+    }
+}
+template <typename WT, typename GT, bool MASTER>
+__device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, const Constants &k, const moe_adamw_rates &r) {
+    if ((chunk + 1) * CHUNK <= t.count) update_eight<WT, GT, MASTER, true>(t, chunk, k, r);
+    else update_eight<WT, GT, MASTER, false>(t, chunk, k, r);
+}
+
+// A block finds its tensor in the list and takes CHUNK elements of it. Tensors with 8-bit moments are launched apart from those with float ones, whose kernel needs fewer registers.
+template <bool EIGHT>
+__global__ void __launch_bounds__(THREADS, EIGHT ? EIGHT_BLOCKS : 3) adamw_kernel(const __grid_constant__ Batch b, Constants k, moe_adamw_rates given, const moe_adamw_rates *read) {
     wait_previous_kernel();
     const moe_adamw_rates r = read ? *read : given;
     int32_t lo = 0, hi = b.n;
@@ -208,19 +292,24 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
     }
     const Entry &t = b.t[lo];
     const int64_t chunk = (int32_t)blockIdx.x - b.chunks_before[lo];
-    switch (t.kind) {
-        case 0: update<float, float, false, false>(t, chunk, k, r); break;
-        case 1: update<bf16, float, false, false>(t, chunk, k, r); break;
-        case 2: update<float, bf16, false, false>(t, chunk, k, r); break;
-        case 3: update<bf16, bf16, false, false>(t, chunk, k, r); break;
-        case 5: update<bf16, float, true, false>(t, chunk, k, r); break;
-        case 7: update<bf16, bf16, true, false>(t, chunk, k, r); break;
-        case 8: update<float, float, false, true>(t, chunk, k, r); break;
-        case 9: update<bf16, float, false, true>(t, chunk, k, r); break;
-        case 10: update<float, bf16, false, true>(t, chunk, k, r); break;
-        case 11: update<bf16, bf16, false, true>(t, chunk, k, r); break;
-        case 13: update<bf16, float, true, true>(t, chunk, k, r); break;
-        case 15: update<bf16, bf16, true, true>(t, chunk, k, r); break;
+    if constexpr (EIGHT) {
+        switch (t.kind) {
+            case 0: update_eight<float, float, false>(t, chunk, k, r); break;
+            case 1: update_eight<bf16, float, false>(t, chunk, k, r); break;
+            case 2: update_eight<float, bf16, false>(t, chunk, k, r); break;
+            case 3: update_eight<bf16, bf16, false>(t, chunk, k, r); break;
+            case 5: update_eight<bf16, float, true>(t, chunk, k, r); break;
+            case 7: update_eight<bf16, bf16, true>(t, chunk, k, r); break;
+        }
+    } else {
+        switch (t.kind) {
+            case 0: update<float, float, false>(t, chunk, k, r); break;
+            case 1: update<bf16, float, false>(t, chunk, k, r); break;
+            case 2: update<float, bf16, false>(t, chunk, k, r); break;
+            case 3: update<bf16, bf16, false>(t, chunk, k, r); break;
+            case 5: update<bf16, float, true>(t, chunk, k, r); break;
+            case 7: update<bf16, bf16, true>(t, chunk, k, r); break;
+        }
     }
 }
 
@@ -246,27 +335,30 @@ int32_t launch_adamw(const moe_adamw_tensor *tensors, int32_t count, const moe_a
     const Constants k = {(float)p.beta1, (float)(1.0 - p.beta1), (float)p.beta2, (float)(1.0 - p.beta2), (float)p.eps};
     moe_adamw_rates given = {};
     if (!rates) given = {(float)p.lr, (float)(1.0 - pow(p.beta1, p.step)), (float)(1.0 - pow(p.beta2, p.step)), (float)p.grad_scale, p.seed};
-    Batch b;
-    b.n = 0;
-    b.chunks_before[0] = 0;
-    auto flush = [&]() -> int32_t {
+    Batch lists[2];  // of float moments, of 8-bit ones
+    auto flush = [&](int eight) -> int32_t {
+        Batch &b = lists[eight];
         if (b.n == 0) return MOE_OK;
-        launch_kernel(adamw_kernel, dim3((unsigned)b.chunks_before[b.n]), dim3(THREADS), 0, st, b, k, given, rates);
+        launch_kernel(eight ? adamw_kernel<true> : adamw_kernel<false>, dim3((unsigned)b.chunks_before[b.n]), dim3(THREADS), 0, st, b, k, given, rates);
         MOE_LAUNCHED();
         b.n = 0;
         return MOE_OK;
     };
+    for (Batch &b : lists) b.n = b.chunks_before[0] = 0;
     for (int32_t i = 0; i < count; ++i) {
         const moe_adamw_tensor &t = tensors[i];
         if (t.count == 0) continue;
+        const int eight = t.moment_bits == 8;
+        Batch &b = lists[eight];
         const int64_t chunks = cdiv(t.count, CHUNK);  // at most 2^27
-        if (b.n == MAX_LIST || (b.n > 0 && b.chunks_before[b.n] + chunks > (1 << 30))) MOE_TRY(flush());
+        if (b.n == MAX_LIST || (b.n > 0 && b.chunks_before[b.n] + chunks > (1 << 30))) MOE_TRY(flush(eight));
         b.t[b.n] = {t.w, t.g, t.master, t.m, t.v, t.m_scale, t.v_scale, t.count, t.first, t.weight_decay,
-                    (t.w_type == MOE_BF16 ? 1 : 0) | (t.g_type == MOE_BF16 ? 2 : 0) | (t.master ? 4 : 0) | (t.moment_bits == 8 ? 8 : 0)};
+                    (t.w_type == MOE_BF16 ? 1 : 0) | (t.g_type == MOE_BF16 ? 2 : 0) | (t.master ? 4 : 0)};
         b.chunks_before[b.n + 1] = b.chunks_before[b.n] + (int32_t)chunks;
         ++b.n;
     }
-    return flush();
+    MOE_TRY(flush(0));
+    return flush(1);
 }
 
 }  // namespace moe
