@@ -77,15 +77,15 @@ __device__ __forceinline__ float2 mul_two(float2 a, float2 b) {
     asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 c, a, b;\n mov.b64 {%0, %1}, c;\n}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
-__device__ __forceinline__ float2 add_two(float2 a, float2 b) {
-    float2 r;
-    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 c, a, b;\n mov.b64 {%0, %1}, c;\n}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
 __device__ __forceinline__ float2 fma_two(float2 a, float2 b, float2 d) {
     float2 r;
     asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 c, a, b, c;\n mov.b64 {%0, %1}, c;\n}"
         : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(d.x), "f"(d.y));
+    return r;
+}
+__device__ __forceinline__ float is_below(float a, float b) {  // 1 or 0
+    float r;
+    asm("set.lt.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
@@ -95,17 +95,24 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return r;
 }
 
+// Eight elements as they stand in memory
+template <typename T> struct Raw8 {
+    uint4 q[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = reinterpret_cast<const uint4 *>(p)[i];
+    }
+    __device__ __forceinline__ void floats(float (&v)[EACH]) const {
+        const uint32_t *u = reinterpret_cast<const uint32_t *>(q);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) v[i] = sizeof(T) == 4 ? __uint_as_float(u[i * sizeof(T) / 4]) : __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+    }
+};
 template <typename T> __device__ __forceinline__ void load8(const T *p, int64_t at, int64_t live, float (&v)[EACH]) {
     if (live >= EACH) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = *reinterpret_cast<const float4 *>(p + at), b = *reinterpret_cast<const float4 *>(p + at + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 a = *reinterpret_cast<const uint4 *>(p + at);
-            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-        }
+        Raw8<T> raw;
+        raw.load(p + at);
+        raw.floats(v);
         return;
     }
 #pragma unroll
@@ -173,11 +180,14 @@ __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, int64_t
 #pragma unroll
     for (int i = 0; i < EACH; i += 2) {
         const float2 size = mul_two(make_float2(fabsf(v[i]), fabsf(v[i + 1])), both(by));
-        const float2 shift = make_float2(size.x < 0.015625f ? 0.015625f : 0.0f, size.y < 0.015625f ? 0.015625f : 0.0f), up = add_two(size, shift);
+        const float2 small = make_float2(is_below(size.x, 0.015625f), is_below(size.y, 0.015625f)), up = fma_two(small, both(0.015625f), size);
         auto cut = [&](float u, uint32_t x) { return __uint_as_float((__float_as_uint(u) + (((ROOT ? x >> 12 : (x ^ (x >> 16)) << 4) & 0xffff0u) | 8u)) & ~0xfffffu); };
-        float2 z = add_two(make_float2(cut(up.x, bits[i]), cut(up.y, bits[i + 1])), make_float2(-shift.x, -shift.y));
-        if (ROOT) z = make_float2(fmaxf(z.x, size.x > 0.0f ? 0.001953125f : 0.0f), fmaxf(z.y, size.y > 0.0f ? 0.001953125f : 0.0f));
-        else z = make_float2(copysignf(z.x, v[i]), copysignf(z.y, v[i + 1]));
+        float2 z = fma_two(small, both(-0.015625f), make_float2(cut(up.x, bits[i]), cut(up.y, bits[i + 1])));
+        if (ROOT) {  // the smallest code at least for what is not 0: of normal numbers over the largest, 2^127 times as much is above it
+            const float2 least = mul_two(size, both(1.7014118e38f));
+            z = make_float2(fmaxf(z.x, fminf(least.x, 0.001953125f)), fmaxf(z.y, fminf(least.y, 0.001953125f)));
+        }
+        if (!ROOT) z = make_float2(copysignf(z.x, v[i]), copysignf(z.y, v[i + 1]));
         const __nv_fp8x2_storage_t two = __nv_cvt_float2_to_fp8x2(z, __NV_SATFINITE, __NV_E4M3);
         c[i / 4] |= (uint32_t)two << (8 * (i % 4));
     }
@@ -237,14 +247,40 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
     int64_t live = FULL ? EACH : t.count - at;  // at most 0 behind the end
     uint64_t number = (uint64_t)(t.first + at);  // a multiple of EACH: adding is setting bits
     const uint32_t seed = r.seed;
+    struct Held {
+        Raw8<MT> w;
+        Raw8<GT> g;
+        uint2 m, v;
+        float ms, vs;
+    } held;
+    auto fetch = [&](int i) {
+        held.w.load(from + i * STEP);
+        held.g.load(g_at + i * STEP);
+        held.m = *reinterpret_cast<const uint2 *>(m_at + i * STEP);
+        held.v = *reinterpret_cast<const uint2 *>(v_at + i * STEP);
+        held.ms = ms_at[i * (STEP / MOE_ADAMW_BLOCK)];
+        held.vs = vs_at[i * (STEP / MOE_ADAMW_BLOCK)];
+    };
+    if constexpr (FULL) fetch(0);
 #pragma unroll 1
     for (int i = 0; i < CHUNK / STEP; ++i) {
         if (!FULL && chunk * CHUNK + i * STEP >= t.count) break;  // the whole block
         float g[EACH], m[EACH], root[EACH], w[EACH];
-        load8(from, 0, live, w);
-        load8(g_at, 0, live, g);
-        const uint2 m_codes = load_codes(m_at, 0, live), v_codes = load_codes(v_at, 0, live);
-        const float ms = FULL || live > 0 ? *ms_at : 0.0f, vs = FULL || live > 0 ? *vs_at : 0.0f;
+        uint2 m_codes, v_codes;
+        float ms, vs;
+        if constexpr (FULL) {
+            held.w.floats(w);
+            held.g.floats(g);
+            m_codes = held.m; v_codes = held.v; ms = held.ms; vs = held.vs;
+            if (i + 1 < CHUNK / STEP) fetch(1);
+        } else {
+            load8(from, 0, live, w);
+            load8(g_at, 0, live, g);
+            m_codes = load_codes(m_at, 0, live);
+            v_codes = load_codes(v_at, 0, live);
+            ms = live > 0 ? *ms_at : 0.0f;
+            vs = live > 0 ? *vs_at : 0.0f;
+        }
         const uint32_t key = mix(seed + (uint32_t)(number >> 32) * 0x9e3779b9u) ^ (uint32_t)number;
         uint32_t bits[EACH];
         decode(m_codes, m);
