@@ -334,22 +334,43 @@ def moe_norm_workspace_bytes(cfg) -> int:
     return _one_size("moe_norm_workspace_bytes", cfg)
 
 
+_bound_functions = {}
+
+
+def _bound(name, kinds):
+    """The function of the library with its argument types: c a configuration, p a pointer, i an int, f a float; the stream comes last. Calls of a few microseconds
+    go this way: sorting out a call's fifteen arguments by their types took as long as the launch."""
+    fn = _bound_functions.get(name)
+    if fn is None:
+        types = dict(c=ctypes.POINTER(moe_config), p=ctypes.c_void_p, i=ctypes.c_int32, f=ctypes.c_float)
+        raw = ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
+        fn = _bound_functions[name] = ctypes.CFUNCTYPE(ctypes.c_int32, *[types[k] for k in kinds], ctypes.c_void_p)(raw)
+    return fn
+
+
+def _checked(name, status):
+    if status != 0:
+        raise MoeError(name, status)
+
+
 def moe_norm_in(cfg, x, w, eps, xn, rstd):
-    _call("moe_norm_in", cfg, x, w, float(eps), xn, rstd)
+    _checked("moe_norm_in", _bound("moe_norm_in", "cppfpp")(cfg, _p(x), _p(w), eps, _p(xn), _p(rstd), _stream()))
 
 
 def moe_norm_in_bwd(cfg, dxn, x, w, rstd, dres, dX, dw, ws):
-    _call("moe_norm_in_bwd", cfg, dxn, x, w, rstd, dres, dX, dw, ws)
+    _checked("moe_norm_in_bwd", _bound("moe_norm_in_bwd", "cpppppppp")(cfg, _p(dxn), _p(x), _p(w), _p(rstd), _p(dres), _p(dX), _p(dw), _p(ws), _stream()))
 
 
 def moe_norm_out(cfg, x, y, w, gate, rows_per_gate, residual_scale, w_next, eps, out, next, rstd, rstd_next):
-    _call("moe_norm_out", cfg, x, y, w, gate, int(rows_per_gate), float(residual_scale), w_next, float(eps), out, next, rstd, rstd_next)
+    _checked("moe_norm_out", _bound("moe_norm_out", "cppppifpfpppp")(cfg, _p(x), _p(y), _p(w), _p(gate), rows_per_gate, residual_scale, _p(w_next), eps, _p(out),
+                                                                     _p(next), _p(rstd), _p(rstd_next), _stream()))
 
 
 def moe_norm_out_bwd(cfg, dOut, dNext, out, y, w, gate, rows_per_gate, residual_scale, w_next, rstd, rstd_next, dX, dY, dw, dgate, dw_next,
                      ws):
-    _call("moe_norm_out_bwd", cfg, dOut, dNext, out, y, w, gate, int(rows_per_gate), float(residual_scale), w_next, rstd, rstd_next, dX, dY,
-          dw, dgate, dw_next, ws)
+    _checked("moe_norm_out_bwd", _bound("moe_norm_out_bwd", "cppppppifppppppppp")(cfg, _p(dOut), _p(dNext), _p(out), _p(y), _p(w), _p(gate), rows_per_gate, residual_scale,
+                                                                                  _p(w_next), _p(rstd), _p(rstd_next), _p(dX), _p(dY), _p(dw), _p(dgate), _p(dw_next), _p(ws),
+                                                                                  _stream()))
 
 
 def moe_few_workspace_bytes(cfg) -> int:
@@ -357,7 +378,8 @@ def moe_few_workspace_bytes(cfg) -> int:
 
 
 def moe_forward_few(cfg, x, Wg, W1, b1, W2, b2, y, topk_idx, gates, ws):
-    _call("moe_forward_few", cfg, x, Wg, W1, b1, W2, b2, y, topk_idx, gates, ws)
+    _checked("moe_forward_few", _bound("moe_forward_few", "cpppppppppp")(cfg, _p(x), _p(Wg), _p(W1), _p(b1), _p(W2), _p(b2), _p(y), _p(topk_idx), _p(gates), _p(ws),
+                                                                         _stream()))
 
 
 class moe_adamw_list:

@@ -15,6 +15,7 @@
 #include <cuda_fp8.h>
 
 #include "block.cuh"
+#include "pairs.cuh"
 
 namespace moe {
 
@@ -71,24 +72,11 @@ __device__ __forceinline__ float reciprocal(float v) {  // of normal numbers; 0 
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// Two at a time: one instruction for two products or sums, each rounded as by itself
-__device__ __forceinline__ float2 mul_two(float2 a, float2 b) {
-    float2 r;
-    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 c, a, b;\n mov.b64 {%0, %1}, c;\n}" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-__device__ __forceinline__ float2 fma_two(float2 a, float2 b, float2 d) {
-    float2 r;
-    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 c, a, b, c;\n mov.b64 {%0, %1}, c;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(d.x), "f"(d.y));
-    return r;
-}
 __device__ __forceinline__ float is_below(float a, float b) {  // 1 or 0
     float r;
     asm("set.lt.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -179,12 +167,12 @@ __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, int64_t
     // the unit stays 2^-9, which is that of the numbers from 2^-6 to 2^-5. (Up from 448 gives 480, which the conversion takes for 448.)
 #pragma unroll
     for (int i = 0; i < EACH; i += 2) {
-        const float2 size = mul_two(make_float2(fabsf(v[i]), fabsf(v[i + 1])), both(by));
-        const float2 small = make_float2(is_below(size.x, 0.015625f), is_below(size.y, 0.015625f)), up = fma_two(small, both(0.015625f), size);
+        const float2 size = mul2(make_float2(fabsf(v[i]), fabsf(v[i + 1])), both(by));
+        const float2 small = make_float2(is_below(size.x, 0.015625f), is_below(size.y, 0.015625f)), up = fma2(small, both(0.015625f), size);
         auto cut = [&](float u, uint32_t x) { return __uint_as_float((__float_as_uint(u) + (((ROOT ? x >> 12 : (x ^ (x >> 16)) << 4) & 0xffff0u) | 8u)) & ~0xfffffu); };
-        float2 z = fma_two(small, both(-0.015625f), make_float2(cut(up.x, bits[i]), cut(up.y, bits[i + 1])));
+        float2 z = fma2(small, both(-0.015625f), make_float2(cut(up.x, bits[i]), cut(up.y, bits[i + 1])));
         if (ROOT) {  // the smallest code at least for what is not 0: of normal numbers over the largest, 2^127 times as much is above it
-            const float2 least = mul_two(size, both(1.7014118e38f));
+            const float2 least = mul2(size, both(1.7014118e38f));
             z = make_float2(fmaxf(z.x, fminf(least.x, 0.001953125f)), fmaxf(z.y, fminf(least.y, 0.001953125f)));
         }
         if (!ROOT) z = make_float2(copysignf(z.x, v[i]), copysignf(z.y, v[i + 1]));
@@ -291,11 +279,11 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
             bits[e] = mix_but_last(key ^ e);
             bits[e + 1] = mix_but_last(key ^ (e + 1));
             const float2 gg = make_float2(g[e], g[e + 1]);
-            const float2 mm = fma_two(make_float2(m[e], m[e + 1]), both(by_m), mul_two(both(by_g), gg));
-            const float2 old = mul_two(make_float2(root[e], root[e + 1]), both(vs));
-            const float2 vv = fma_two(mul_two(both(k.beta2), old), old, mul_two(mul_two(both(by_gg), gg), gg));
-            const float2 rt = make_float2(normal_root_of(vv.x), normal_root_of(vv.y)), den = fma_two(rt, both(root_by), both(k.eps));
-            const float2 ww = fma_two(mul_two(mm, both(down)), make_float2(reciprocal(den.x), reciprocal(den.y)), mul_two(make_float2(w[e], w[e + 1]), both(keep)));
+            const float2 mm = fma2(make_float2(m[e], m[e + 1]), both(by_m), mul2(both(by_g), gg));
+            const float2 old = mul2(make_float2(root[e], root[e + 1]), both(vs));
+            const float2 vv = fma2(mul2(both(k.beta2), old), old, mul2(mul2(both(by_gg), gg), gg));
+            const float2 rt = make_float2(normal_root_of(vv.x), normal_root_of(vv.y)), den = fma2(rt, both(root_by), both(k.eps));
+            const float2 ww = fma2(mul2(mm, both(down)), make_float2(reciprocal(den.x), reciprocal(den.y)), mul2(make_float2(w[e], w[e + 1]), both(keep)));
             m[e] = mm.x; m[e + 1] = mm.y;
             root[e] = rt.x; root[e + 1] = rt.y;
             w[e] = ww.x; w[e + 1] = ww.y;

@@ -7,17 +7,33 @@
 //   dY = r (dt gate w - n mean(dt gate w n)),   dgate = w times the sum of dt n over the rows of the gate,   dw = sum of dt gate n
 // All of it is bound by memory: a row stays in registers between its sums and what is made of it. Sums are float, over rows first by
 // threads that keep their columns, then in double over what blocks have left, in a fixed order.
+#include "async_copy.cuh"
 #include "block.cuh"
+#include "pairs.cuh"
 
 namespace moe {
 
 namespace {
 
+// 16 bytes of a row, as pairs of floats
 template <typename T> struct Vec {
     static constexpr int N = 16 / sizeof(T);
     uint4 raw;
-    __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T *>(&raw)[i]); }
-    __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T *>(&raw)[i] = from_f32<T>(v); }
+    __device__ __forceinline__ float2 get(int i) const {  // elements i, i + 1
+        const uint32_t *u = reinterpret_cast<const uint32_t *>(&raw);
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(u[i]), __uint_as_float(u[i + 1]));
+        else return make_float2(__uint_as_float(u[i / 2] << 16), __uint_as_float(u[i / 2] & 0xffff0000u));
+    }
+    __device__ __forceinline__ void set(int i, float2 v) {
+        uint32_t *u = reinterpret_cast<uint32_t *>(&raw);
+        if constexpr (sizeof(T) == 4) {
+            u[i] = __float_as_uint(v.x);
+            u[i + 1] = __float_as_uint(v.y);
+        } else {
+            const __nv_bfloat162 two = __floats2bfloat162_rn(v.x, v.y);
+            u[i / 2] = *reinterpret_cast<const uint32_t *>(&two);
+        }
+    }
 };
 template <typename T> __device__ __forceinline__ Vec<T> load_vec(const void *base, int64_t row, int32_t d, int32_t q) {
     Vec<T> v;
@@ -27,42 +43,69 @@ template <typename T> __device__ __forceinline__ Vec<T> load_vec(const void *bas
 template <typename T> __device__ __forceinline__ void store_vec(void *base, int64_t row, int32_t d, int32_t q, const Vec<T> &v) {
     *reinterpret_cast<uint4 *>(static_cast<T *>(base) + row * d + (int64_t)q * Vec<T>::N) = v.raw;
 }
-template <int N> __device__ __forceinline__ void load_floats(const float *p, float (&v)[N]) {
+template <int N> __device__ __forceinline__ void load_floats(const float *p, float2 (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        const float4 a = *reinterpret_cast<const float4 *>(p + i);
-        v[i] = a.x; v[i + 1] = a.y; v[i + 2] = a.z; v[i + 3] = a.w;
+    for (int i = 0; i < N; i += 2) {
+        const float4 a = *reinterpret_cast<const float4 *>(p + 2 * i);
+        v[i] = make_float2(a.x, a.y);
+        v[i + 1] = make_float2(a.z, a.w);
     }
 }
 
-// A row belongs to a team of `warps` warps of the block. Sums over the team's threads; `sh` has a place per team, warp and sum, twice, so that one
+// A row belongs to a team of `warps` warps of the block. Sums over the team's threads; `sh` has a place per warp and sum, twice, so that one
 // barrier a row is enough: who writes the next row's sums does so on the other side, and the barrier of that row keeps it from coming round.
 constexpr int MAX_SUMS = 4;
-template <int K> __device__ __forceinline__ void team_sums(float (&s)[K], int warps, float *sh, int &side) {
+__device__ __forceinline__ void over_warps(float *mine, int warps, int team) {
+    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
+    (void)mine;
+}
+__device__ __forceinline__ float team_sum(float s, int warps, float *sh, int &side) {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-        for (int i = 0; i < K; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], off);
-    if (warps == 1) return;
-    const int warp = threadIdx.x >> 5, team = warp / warps, lane = threadIdx.x & 31;
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    if (warps == 1) return s;
+    const int warp = threadIdx.x >> 5, team = warp / warps;
     float *mine = sh + side * (32 * MAX_SUMS);
     side ^= 1;
-    if (lane == 0)
+    if ((threadIdx.x & 31) == 0) mine[warp] = s;
+    over_warps(mine, warps, team);
+    s = 0.0f;
+    for (int q = 0; q < warps; ++q) s += mine[team * warps + q];
+    return s;
+}
+// Four at once: lanes give away half of their sums in the first two steps, so that six exchanges do instead of twenty. Lane l then has sum l / 8.
+__device__ __forceinline__ void team_sums(float (&s)[4], int warps, float *sh, int &side) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = warp / warps;
+    const bool hi = lane & 16, up = lane & 8;
+    float a = hi ? s[2] : s[0], b = hi ? s[3] : s[1];
+    a += __shfl_xor_sync(0xffffffffu, hi ? s[0] : s[2], 16);
+    b += __shfl_xor_sync(0xffffffffu, hi ? s[1] : s[3], 16);
+    float t = up ? b : a;
+    t += __shfl_xor_sync(0xffffffffu, up ? a : b, 8);
 #pragma unroll
-        for (int i = 0; i < K; ++i) mine[warp * MAX_SUMS + i] = s[i];
-    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
+    for (int off = 4; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
+    if (warps == 1) {
 #pragma unroll
-    for (int i = 0; i < K; ++i) s[i] = 0.0f;
-    for (int q = 0; q < warps; ++q)
-#pragma unroll
-        for (int i = 0; i < K; ++i) s[i] += mine[(team * warps + q) * MAX_SUMS + i];
+        for (int i = 0; i < 4; ++i) s[i] = __shfl_sync(0xffffffffu, t, 8 * i);
+        return;
+    }
+    float4 *mine = reinterpret_cast<float4 *>(sh + side * (32 * MAX_SUMS));
+    side ^= 1;
+    if ((lane & 7) == 0) reinterpret_cast<float *>(mine + warp)[lane >> 3] = t;
+    over_warps(nullptr, warps, team);
+    float4 all = mine[team * warps];
+    for (int q = 1; q < warps; ++q) {
+        const float4 f = mine[team * warps + q];
+        all.x += f.x; all.y += f.y; all.z += f.z; all.w += f.w;
+    }
+    s[0] = all.x; s[1] = all.y; s[2] = all.z; s[3] = all.w;
 }
 
-// Y: the block's output goes through its norm and the gate onto x; NEXT: a norm of the result (without Y: of x)
-template <typename T, int V, bool Y, bool NEXT>
+// Y: the block's output goes through its norm and the gate onto x; NEXT: a norm of the result (without Y: of x). Arithmetic in pairs: element by element it was 31 instructions an element
+// and kept memory waiting, 28.2 us for 32768 x 512.
+template <typename T, int V, bool Y, bool NEXT, bool GATE>
 __global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, int warps) {
     wait_previous_kernel();
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Vec<T>::N, P = N / 2;
     __shared__ float sh[2 * 32 * MAX_SUMS];
     int side = 0;
     const int threads = warps * 32, teams = blockDim.x / threads, lane = threadIdx.x % threads;
@@ -78,34 +121,33 @@ __global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, int wa
         if constexpr (Y) yv[v] = load_vec<T>(a.y, row, a.d, q);
         xv[v] = load_vec<T>(a.x, row, a.d, q);
     }
-    float o[V][N];
-    float sum[1] = {0.0f};
+    float2 o[V][P];
+    float2 sum = both(0.0f);
     if constexpr (Y) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
             if (lane + v * threads < pieces)
 #pragma unroll
-                for (int i = 0; i < N; ++i) { const float f = yv[v].get(i); sum[0] = fmaf(f, f, sum[0]); }
-        team_sums(sum, warps, sh, side);
-        const float r = 1.0f / sqrtf(sum[0] * by + a.eps);
+                for (int i = 0; i < P; ++i) { const float2 f = yv[v].get(2 * i); sum = fma2(f, f, sum); }
+        const float r = 1.0f / sqrtf(team_sum(sum.x + sum.y, warps, sh, side) * by + a.eps);
         if (lane == 0) a.rstd[row] = r;
-        const int64_t gate_row = a.gate ? (int64_t)((uint32_t)row / (uint32_t)a.rows_per_gate) : 0;
-        sum[0] = 0.0f;
+        const int64_t gate_row = GATE ? (int64_t)((uint32_t)row / (uint32_t)a.rows_per_gate) : 0;
+        sum = both(0.0f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
             if (q >= pieces) break;
-            float w[N];
+            float2 w[P];
             load_floats(a.w + (int64_t)q * N, w);
             Vec<T> g, res;
-            if (a.gate) g = load_vec<T>(a.gate, gate_row, a.d, q);
+            if constexpr (GATE) g = load_vec<T>(a.gate, gate_row, a.d, q);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float u = yv[v].get(i) * r * w[i];
-                if (a.gate) u *= g.get(i);
-                o[v][i] = fmaf(a.residual_scale, xv[v].get(i), u);
-                sum[0] = fmaf(o[v][i], o[v][i], sum[0]);
-                res.set(i, o[v][i]);
+            for (int i = 0; i < P; ++i) {
+                float2 u = mul2(mul2(yv[v].get(2 * i), both(r)), w[i]);
+                if constexpr (GATE) u = mul2(u, g.get(2 * i));
+                o[v][i] = fma2(both(a.residual_scale), xv[v].get(2 * i), u);
+                sum = fma2(o[v][i], o[v][i], sum);
+                res.set(2 * i, o[v][i]);
             }
             store_vec<T>(a.out, row, a.d, q, res);
         }
@@ -114,21 +156,20 @@ __global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, int wa
         for (int v = 0; v < V; ++v)
             if (lane + v * threads < pieces)
 #pragma unroll
-                for (int i = 0; i < N; ++i) { o[v][i] = xv[v].get(i); sum[0] = fmaf(o[v][i], o[v][i], sum[0]); }
+                for (int i = 0; i < P; ++i) { o[v][i] = xv[v].get(2 * i); sum = fma2(o[v][i], o[v][i], sum); }
     }
     if constexpr (NEXT) {  // of what was not rounded yet
-        team_sums(sum, warps, sh, side);
-        const float r = 1.0f / sqrtf(sum[0] * by + a.eps);
+        const float r = 1.0f / sqrtf(team_sum(sum.x + sum.y, warps, sh, side) * by + a.eps);
         if (lane == 0 && a.rstd_next) a.rstd_next[row] = r;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
             if (q >= pieces) break;
-            float w[N];
+            float2 w[P];
             load_floats(a.w_next + (int64_t)q * N, w);
             Vec<T> res;
 #pragma unroll
-            for (int i = 0; i < N; ++i) res.set(i, o[v][i] * r * w[i]);
+            for (int i = 0; i < P; ++i) res.set(2 * i, mul2(mul2(o[v][i], both(r)), w[i]));
             store_vec<T>(a.next, row, a.d, q, res);
         }
     }
@@ -137,11 +178,13 @@ __global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, int wa
 // How the backward pass shares out its rows. With one gate (or none) a block has `rows` rows of one group and leaves partial sums (chunks of a
 // group: `chunks`); with groups of a few rows a team has whole groups and writes their gate's gradient itself (chunks 0).
 struct Share {
-    int warps, teams, V;
+    int warps, teams, V, ring;  // ring: rows that a warp holds in shared memory (0: a row of several warps, in registers)
     int64_t group, groups, chunks, rows, per_team, blocks;  // per_team: groups a team takes (chunks == 0)
 };
 constexpr int TEAM_ROWS = 4;
-int64_t team_rows(int64_t T, int teams) { return imax(TEAM_ROWS, cdiv(T, (int64_t)teams * 148 * 6)); }
+// rows of a team: blocks for two waves, of one block an SM where blocks are large (131072 x 1024: one wave 293 us, two 295, three 298, six 322) and of three where not
+int64_t team_rows(int64_t T, int teams) { return imax(TEAM_ROWS, cdiv(T, (int64_t)teams * 148 * (teams > 8 ? 2 : 6))); }
+// Forward: a warp has a row up to 32 vectors a lane, else several do
 void team_of(int32_t d, int32_t act, int *warps, int *teams, int *V) {
     const int64_t pieces = d / (16 / (int64_t)act_bytes(act));
     *V = pieces <= 32 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8;  // at most 512 threads
@@ -150,9 +193,30 @@ void team_of(int32_t d, int32_t act, int *warps, int *teams, int *V) {
     *warps = w;
     *teams = w >= 8 ? 1 : 8 / w;
 }
-Share share_of(int64_t T, int32_t d, int32_t act, int64_t rows_per_gate) {
+// Backward: a warp has a row of up to 128 vectors, and the next one on its way to shared memory; wider rows are a vector a thread while 512 threads do
+constexpr int STREAM_PIECES = 128, RING_ROWS = 2, SHARED_MOST = 200 * 1024, SHARED_ALLOWED = 216 * 1024;  // beside the rings: w and w_next, 8 KiB at most
+// warps of a block: eight where three blocks or two have room, else as many as one has
+int64_t stream_warps(int64_t row) { return row * 8 <= SHARED_MOST / 2 ? 8 : imin(12, SHARED_MOST / row); }
+void grad_team_of(int32_t d, int32_t act, int tensors, int *warps, int *teams, int *V, int *ring) {
+    const int64_t pieces = d / (16 / (int64_t)act_bytes(act));
+    if (pieces <= STREAM_PIECES) {
+        const int64_t row = (int64_t)tensors * d * (int64_t)act_bytes(act) * RING_ROWS;
+        *V = pieces <= 32 ? 1 : pieces <= 64 ? 2 : 4;
+        *warps = 1;
+        *ring = RING_ROWS;
+        *teams = (int)stream_warps(row);
+        return;
+    }
+    *ring = 0;
+    *V = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8;
+    int w = 1;
+    while (w * 32 * *V < pieces) w *= 2;
+    *warps = w;
+    *teams = w >= 8 ? 1 : 8 / w;
+}
+Share share_of(int64_t T, int32_t d, int32_t act, int tensors, int64_t rows_per_gate) {
     Share s = {};
-    team_of(d, act, &s.warps, &s.teams, &s.V);
+    grad_team_of(d, act, tensors, &s.warps, &s.teams, &s.V, &s.ring);
     const int64_t each = team_rows(T, s.teams);
     s.group = rows_per_gate > 0 ? imin(rows_per_gate, imax(T, 1)) : imax(T, 1);
     s.groups = cdiv(T, s.group);
@@ -173,126 +237,130 @@ int64_t most_blocks(int64_t T, int teams) {
     return 2 * cdiv(T, each * teams) + T / (2 * each) + 3;
 }
 
-template <typename T, int V, bool Y, bool NEXT, bool GATE>
-__global__ void __launch_bounds__(V == 1 ? 256 : 512) norm_grads_kernel(const NormGradArgs a, const Share s, float *part_w, float *part_next, float *part_gate) {
+// GATE: 0 none, 1 a block's rows have one, 2 groups of a few rows (chunks 0)
+template <typename T, int V, bool Y, bool NEXT, int GATE>
+__global__ void __maxnreg__(V == 1 ? 80 : 128) norm_grads_kernel(const NormGradArgs a, const Share s, float *part_w, float *part_next, float *part_gate) {
     wait_previous_kernel();
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Vec<T>::N, P = N / 2;
     extern __shared__ float columns[];  // [teams][d], where a block has several teams
-    __shared__ float sh[2 * 32 * MAX_SUMS];
+    __shared__ __align__(16) float sh[2 * 32 * MAX_SUMS];
     int side = 0;
     const int threads = s.warps * 32, team = threadIdx.x / threads, lane = threadIdx.x % threads;
     const int32_t pieces = a.d / N;
     const float by = 1.0f / (float)a.d;
-    float sum_n[V][N], sum_w[V][N], sum_next[V][N];  // of dt n over the group's rows so far; of dt gate n; of dNext n2
+    float2 sum_n[Y ? V : 1][P], sum_w[GATE == 2 ? V : 1][P], sum_next[NEXT ? V : 1][P];  // of dt n over the group's rows so far; of dt gate n; of dNext n2
+    float2 gw[Y ? V : 1][P], wn[NEXT ? V : 1][P];                                           // gate times w of the group; w_next
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
+        const int32_t q = lane + v * threads;
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum_n[v][i] = sum_w[v][i] = sum_next[v][i] = 0.0f;
-
-    auto one_row = [&](int64_t row, int64_t gate_row) {
-        Vec<T> dov[V], dnv[V], ov[V], yv[V], gv[V];
+        for (int i = 0; i < P; ++i) {
+            if constexpr (Y) sum_n[v][i] = both(0.0f);
+            if constexpr (GATE == 2) sum_w[v][i] = both(0.0f);
+            if constexpr (NEXT) sum_next[v][i] = both(0.0f);
+        }
+        if (q >= pieces) continue;
+        if constexpr (Y && GATE == 0) load_floats(a.w + (int64_t)q * N, gw[v]);
+        if constexpr (NEXT) load_floats(a.w_next + (int64_t)q * N, wn[v]);
+    }
+    auto begin_group = [&](int64_t gate_row) {
+        if (GATE > 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int32_t q = lane + v * threads;
+                if (q >= pieces) break;
+                load_floats(a.w + (int64_t)q * N, gw[v]);
+                const Vec<T> g = load_vec<T>(a.gate, gate_row, a.d, q);
+#pragma unroll
+                for (int i = 0; i < P; ++i) gw[v][i] = mul2(gw[v][i], g.get(2 * i));
+            }
+    };
+    struct Row { Vec<T> dout[V], dnext[NEXT ? V : 1], out[NEXT ? V : 1], y[Y ? V : 1]; float r, r2; };
+    auto fetch = [&](Row &f, int64_t row) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
             if (q >= pieces) break;
-            if (a.dOut) dov[v] = load_vec<T>(a.dOut, row, a.d, q);
-            else dov[v].raw = make_uint4(0u, 0u, 0u, 0u);
+            if (a.dOut) f.dout[v] = load_vec<T>(a.dOut, row, a.d, q);
+            else f.dout[v].raw = make_uint4(0u, 0u, 0u, 0u);
             if constexpr (NEXT) {
-                dnv[v] = load_vec<T>(a.dNext, row, a.d, q);
-                ov[v] = load_vec<T>(a.out, row, a.d, q);
+                f.dnext[v] = load_vec<T>(a.dNext, row, a.d, q);
+                f.out[v] = load_vec<T>(a.out, row, a.d, q);
             }
-            if constexpr (Y) yv[v] = load_vec<T>(a.y, row, a.d, q);
-            if constexpr (GATE) gv[v] = load_vec<T>(a.gate, gate_row, a.d, q);
+            if constexpr (Y) f.y[v] = load_vec<T>(a.y, row, a.d, q);
         }
-        const float r = Y ? a.rstd[row] : 0.0f, r2 = NEXT ? a.rstd_next[row] : 0.0f;
+        if constexpr (Y) f.r = a.rstd[row];
+        if constexpr (NEXT) f.r2 = a.rstd_next[row];
+    };
+    auto one_row = [&](const Row &f, int64_t row) {
         // c2 = mean(dn2 n2) decides dt, and c1 = mean(dt b) with b = gate w n the rest. Both are sums of one look at the row, since c1 is linear in dt:
         // mean(dOut b) + r2 (mean(dn2 b) - c2 mean(n2 b))
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float2 s0 = both(0.0f), s1 = s0, s2 = s0, s3 = s0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int32_t q = lane + v * threads;
-            if (q >= pieces) break;
-            float w[N], wn[N];
-            if constexpr (Y) load_floats(a.w + (int64_t)q * N, w);
-            if constexpr (NEXT) load_floats(a.w_next + (int64_t)q * N, wn);
+            if (lane + v * threads >= pieces) break;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float b = 0.0f;
+            for (int i = 0; i < P; ++i) {
+                float2 b;
                 if constexpr (Y) {
-                    b = yv[v].get(i) * r * w[i];
-                    if constexpr (GATE) b *= gv[v].get(i);
-                    sum[1] = fmaf(dov[v].get(i), b, sum[1]);
+                    b = mul2(mul2(f.y[v].get(2 * i), both(f.r)), gw[v][i]);
+                    s1 = fma2(f.dout[v].get(2 * i), b, s1);
                 }
                 if constexpr (NEXT) {
-                    const float n2 = ov[v].get(i) * r2, dn2 = dnv[v].get(i) * wn[i];
-                    sum[0] = fmaf(dn2, n2, sum[0]);
+                    const float2 n2 = mul2(f.out[v].get(2 * i), both(f.r2)), dn2 = mul2(f.dnext[v].get(2 * i), wn[v][i]);
+                    s0 = fma2(dn2, n2, s0);
                     if constexpr (Y) {
-                        sum[2] = fmaf(dn2, b, sum[2]);
-                        sum[3] = fmaf(n2, b, sum[3]);
+                        s2 = fma2(dn2, b, s2);
+                        s3 = fma2(n2, b, s3);
                     }
                 }
             }
         }
-        if constexpr (Y && NEXT) team_sums(sum, s.warps, sh, side);
-        else {
-            float one[1] = {sum[Y ? 1 : 0]};
-            team_sums(one, s.warps, sh, side);
-            sum[Y ? 1 : 0] = one[0];
+        float c1 = 0.0f, c2 = 0.0f;
+        if constexpr (Y && NEXT) {
+            float sum[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
+            team_sums(sum, s.warps, sh, side);
+            c2 = sum[0] * by;
+            c1 = (sum[1] + f.r2 * (sum[2] - c2 * sum[3])) * by;
+        } else if constexpr (Y) {
+            c1 = team_sum(s1.x + s1.y, s.warps, sh, side) * by;
+        } else {
+            c2 = team_sum(s0.x + s0.y, s.warps, sh, side) * by;
         }
-        const float c2 = sum[0] * by, c1 = (sum[1] + r2 * (sum[2] - c2 * sum[3])) * by;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
             if (q >= pieces) break;
-            float w[N], wn[N];
-            if constexpr (Y) load_floats(a.w + (int64_t)q * N, w);
-            if constexpr (NEXT) load_floats(a.w_next + (int64_t)q * N, wn);
             Vec<T> dx, dy;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float dt = dov[v].get(i);
+            for (int i = 0; i < P; ++i) {
+                float2 dt = f.dout[v].get(2 * i);
                 if constexpr (NEXT) {
-                    const float n2 = ov[v].get(i) * r2, g2 = dnv[v].get(i);
-                    dt = fmaf(r2, g2 * wn[i] - n2 * c2, dt);
-                    sum_next[v][i] = fmaf(g2, n2, sum_next[v][i]);
+                    const float2 n2 = mul2(f.out[v].get(2 * i), both(f.r2)), g2 = f.dnext[v].get(2 * i);
+                    dt = fma2(both(f.r2), fma2(n2, both(-c2), mul2(g2, wn[v][i])), dt);
+                    sum_next[v][i] = fma2(g2, n2, sum_next[v][i]);
                 }
-                dx.set(i, a.residual_scale * dt);
+                dx.set(2 * i, mul2(both(a.residual_scale), dt));
                 if constexpr (Y) {
-                    const float n = yv[v].get(i) * r;
-                    float dn = dt * w[i];
-                    if constexpr (GATE) dn *= gv[v].get(i);
-                    dy.set(i, r * (dn - n * c1));
-                    sum_n[v][i] = fmaf(dt, n, sum_n[v][i]);
+                    const float2 n = mul2(f.y[v].get(2 * i), both(f.r));
+                    dy.set(2 * i, mul2(both(f.r), fma2(n, both(-c1), mul2(dt, gw[v][i]))));
+                    sum_n[v][i] = fma2(dt, n, sum_n[v][i]);
                 }
             }
             store_vec<T>(a.dX, row, a.d, q, dx);
             if constexpr (Y) store_vec<T>(a.dY, row, a.d, q, dy);
         }
     };
-    // the end of a group: its gate's gradient, and the group's part of dw
-    auto end_group = [&](int64_t gate_row, bool write) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int32_t q = lane + v * threads;
-            if (q >= pieces) break;
-            const Vec<T> g = load_vec<T>(a.gate, gate_row, a.d, q);
-            float w[N];
-            load_floats(a.w + (int64_t)q * N, w);
-            Vec<T> dg;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                sum_w[v][i] = fmaf(g.get(i), sum_n[v][i], sum_w[v][i]);
-                dg.set(i, w[i] * sum_n[v][i]);
-            }
-            if (write) {
-                store_vec<T>(a.dgate, gate_row, a.d, q, dg);
-#pragma unroll
-                for (int i = 0; i < N; ++i) sum_n[v][i] = 0.0f;
-            }
+    auto some_rows = [&](int64_t row, int64_t end, int64_t step) {
+#pragma unroll 1
+        for (; row < end; row += step) {
+            Row now;
+            fetch(now, row);
+            one_row(now, row);
         }
     };
     // the block's sums of its teams' columns, in the order of the teams. done(vector of columns, its sums)
-    auto block_sums = [&](float (&mine)[V][N], auto done) {
+    auto block_sums = [&](auto &mine, auto done) {
         if (s.teams > 1) {
             __syncthreads();
 #pragma unroll
@@ -300,8 +368,8 @@ __global__ void __launch_bounds__(V == 1 ? 256 : 512) norm_grads_kernel(const No
                 const int32_t q = lane + v * threads;
                 if (q >= pieces) break;
 #pragma unroll
-                for (int i = 0; i < N; i += 4)
-                    *reinterpret_cast<float4 *>(columns + (int64_t)team * a.d + (int64_t)q * N + i) = make_float4(mine[v][i], mine[v][i + 1], mine[v][i + 2], mine[v][i + 3]);
+                for (int i = 0; i < P; i += 2)
+                    *reinterpret_cast<float4 *>(columns + (int64_t)team * a.d + (int64_t)q * N + 2 * i) = make_float4(mine[v][i].x, mine[v][i].y, mine[v][i + 1].x, mine[v][i + 1].y);
             }
             __syncthreads();
             if (team > 0) return;
@@ -310,53 +378,325 @@ __global__ void __launch_bounds__(V == 1 ? 256 : 512) norm_grads_kernel(const No
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
             if (q >= pieces) break;
-            float total[N];
+            float2 total[P];
 #pragma unroll
-            for (int i = 0; i < N; ++i) total[i] = mine[v][i];
+            for (int i = 0; i < P; ++i) total[i] = mine[v][i];
+#pragma unroll 1
             for (int t = 1; t < s.teams; ++t)
 #pragma unroll
-                for (int i = 0; i < N; ++i) total[i] += columns[(int64_t)t * a.d + (int64_t)q * N + i];
+                for (int i = 0; i < P; ++i) {
+                    const float2 f = *reinterpret_cast<const float2 *>(columns + (int64_t)t * a.d + (int64_t)q * N + 2 * i);
+                    total[i] = make_float2(total[i].x + f.x, total[i].y + f.y);
+                }
             done(q, total);
         }
     };
     auto to_part = [&](float *part) {
-        return [=](int32_t q, const float (&total)[N]) {
+        return [=](int32_t q, const float2 (&total)[P]) {
 #pragma unroll
-            for (int i = 0; i < N; i += 4)
-                *reinterpret_cast<float4 *>(part + (int64_t)blockIdx.x * a.d + (int64_t)q * N + i) = make_float4(total[i], total[i + 1], total[i + 2], total[i + 3]);
+            for (int i = 0; i < P; i += 2)
+                *reinterpret_cast<float4 *>(part + (int64_t)blockIdx.x * a.d + (int64_t)q * N + 2 * i) = make_float4(total[i].x, total[i].y, total[i + 1].x, total[i + 1].y);
         };
     };
 
-    if (GATE && s.chunks == 0) {
+    if constexpr (GATE == 2) {
         const int64_t first = ((int64_t)blockIdx.x * s.teams + team) * s.per_team;
+#pragma unroll 1
         for (int64_t g = first; g < min(first + s.per_team, s.groups); ++g) {
-            const int64_t end = min((g + 1) * s.group, a.T);
-            for (int64_t row = g * s.group; row < end; ++row) one_row(row, g);
-            if constexpr (GATE) end_group(g, true);
+            begin_group(g);
+            some_rows(g * s.group, min((g + 1) * s.group, a.T), 1);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {  // the group's gate gradient, and its part of dw
+                const int32_t q = lane + v * threads;
+                if (q >= pieces) break;
+                const Vec<T> gv = load_vec<T>(a.gate, g, a.d, q);
+                float2 w[P];
+                load_floats(a.w + (int64_t)q * N, w);
+                Vec<T> dg;
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    sum_w[v][i] = fma2(gv.get(2 * i), sum_n[v][i], sum_w[v][i]);
+                    dg.set(2 * i, mul2(w[i], sum_n[v][i]));
+                    sum_n[v][i] = both(0.0f);
+                }
+                store_vec<T>(a.dgate, g, a.d, q, dg);
+            }
         }
-        if constexpr (Y && GATE) block_sums(sum_w, to_part(part_w));
+        block_sums(sum_w, to_part(part_w));
     } else {
         const int64_t g = blockIdx.x / s.chunks, from = g * s.group + (blockIdx.x % s.chunks) * s.rows;
-        const int64_t end = min(min(from + s.rows, (g + 1) * s.group), a.T);
-        for (int64_t row = from + team; row < end; row += s.teams) one_row(row, g);
-        if constexpr (Y && GATE) {
-            end_group(g, false);
-            block_sums(sum_w, to_part(part_w));
-            if (s.chunks > 1) block_sums(sum_n, to_part(part_gate));
-            else
-                block_sums(sum_n, [&](int32_t q, const float (&total)[N]) {
-                    float w[N];
-                    load_floats(a.w + (int64_t)q * N, w);
-                    Vec<T> dg;
+        begin_group(g);
+        some_rows(from + team, min(min(from + s.rows, (g + 1) * s.group), a.T), s.teams);
+        if constexpr (GATE == 1) {
+            block_sums(sum_n, [&](int32_t q, const float2 (&total)[P]) {
+                const Vec<T> gv = load_vec<T>(a.gate, g, a.d, q);
+                float2 w[P], of_w[P];
+                load_floats(a.w + (int64_t)q * N, w);
+                Vec<T> dg;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) dg.set(i, w[i] * total[i]);
-                    store_vec<T>(a.dgate, g, a.d, q, dg);
-                });
+                for (int i = 0; i < P; ++i) {
+                    of_w[i] = mul2(gv.get(2 * i), total[i]);
+                    dg.set(2 * i, mul2(w[i], total[i]));
+                }
+                to_part(part_w)(q, of_w);
+                if (s.chunks > 1) to_part(part_gate)(q, total);
+                else store_vec<T>(a.dgate, g, a.d, q, dg);
+            });
         } else if constexpr (Y) {
             block_sums(sum_n, to_part(part_w));
         }
     }
     if constexpr (NEXT) block_sums(sum_next, to_part(part_next));
+}
+
+// The same where a warp has a row: rows come by asynchronous copies, each lane's own pieces two rows ahead, into the warp's ring, so that registers hold nothing but the columns' sums and
+// memory is kept busy whatever the warp is doing. (Rows in registers, four warps to a row of 1024: 331 us for 131072 rows, five tensors of whose bytes take 246.) w and w_next lie in shared
+// memory, with the gate in w where the block has one.
+template <typename T, int V, bool Y, bool NEXT, int GATE>
+__global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, const Share s, float *part_w, float *part_next, float *part_gate) {
+    wait_previous_kernel();
+    constexpr int N = Vec<T>::N, P = N / 2, TENSORS = (Y ? 2 : 1) + (NEXT ? 2 : 0);
+    extern __shared__ __align__(16) char norm_shared[];
+    const int32_t d = a.d, pieces = d / N;
+    float *gw = reinterpret_cast<float *>(norm_shared), *wn = gw + (Y ? d : 0);
+    uint4 *ring = reinterpret_cast<uint4 *>(wn + (NEXT ? d : 0));  // [warp][row][tensor][pieces]
+    float *columns = reinterpret_cast<float *>(ring);             // afterwards: [warp][d]
+    const int team = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint4 *mine = ring + (int64_t)team * RING_ROWS * TENSORS * pieces;
+    const float by = 1.0f / (float)d;
+    const int64_t block_group = GATE == 2 ? 0 : blockIdx.x / s.chunks;
+    for (int32_t q = threadIdx.x; q < pieces; q += blockDim.x) {
+        float2 f[P];
+        Vec<T> g;
+        if constexpr (GATE == 1) g = load_vec<T>(a.gate, block_group, d, q);
+        if constexpr (Y) {
+            load_floats(a.w + (int64_t)q * N, f);
+#pragma unroll
+            for (int i = 0; i < P; ++i) *reinterpret_cast<float2 *>(gw + q * N + 2 * i) = GATE == 1 ? mul2(f[i], g.get(2 * i)) : f[i];
+        }
+        if constexpr (NEXT) {
+            load_floats(a.w_next + (int64_t)q * N, f);
+#pragma unroll
+            for (int i = 0; i < P; ++i) *reinterpret_cast<float2 *>(wn + q * N + 2 * i) = f[i];
+        }
+    }
+    __syncthreads();
+    float2 sum_n[Y ? V : 1][P], sum_w[GATE == 2 ? V : 1][P], sum_next[NEXT ? V : 1][P];  // of dt n over the group's rows so far; of dt gate n; of dNext n2
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            if (Y) sum_n[Y ? v : 0][i] = both(0.0f);
+            if (GATE == 2) sum_w[GATE == 2 ? v : 0][i] = both(0.0f);
+            if (NEXT) sum_next[NEXT ? v : 0][i] = both(0.0f);
+        }
+    // a row's pieces of this lane, to place `at` of the ring; its factors go with it
+    auto ask = [&](int64_t row, int64_t end, int at) {
+        if (row < end)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int32_t q = lane + 32 * v;
+                if (q >= pieces) break;
+                uint4 *to = mine + at * TENSORS * pieces + q;
+                const int64_t from = row * d + (int64_t)q * N;
+                if (a.dOut) copy16(to, static_cast<const T *>(a.dOut) + from);
+                else zero16(to);
+                if (Y) copy16(to + pieces, static_cast<const T *>(a.y) + from);
+                if (NEXT) {
+                    copy16(to + (Y ? 2 : 1) * pieces, static_cast<const T *>(a.dNext) + from);
+                    copy16(to + (Y ? 3 : 2) * pieces, static_cast<const T *>(a.out) + from);
+                }
+            }
+        copies_commit();
+    };
+    auto one_row = [&](int64_t row, int at, int64_t gate_row) {
+        const uint4 *held = mine + at * TENSORS * pieces;
+        const float r = Y ? a.rstd[row] : 0.0f, r2 = NEXT ? a.rstd_next[row] : 0.0f;
+        auto weights = [&](const float *from, int32_t q, float2 (&f)[P]) {
+#pragma unroll
+            for (int i = 0; i < P; i += 2) {
+                const float4 x = *reinterpret_cast<const float4 *>(from + q * N + 2 * i);
+                f[i] = make_float2(x.x, x.y);
+                f[i + 1] = make_float2(x.z, x.w);
+            }
+        };
+        auto gated = [&](int32_t q, float2 (&f)[P]) {
+            weights(gw, q, f);
+            if (GATE == 2) {
+                const Vec<T> g = load_vec<T>(a.gate, gate_row, d, q);
+#pragma unroll
+                for (int i = 0; i < P; ++i) f[i] = mul2(f[i], g.get(2 * i));
+            }
+        };
+        float2 s0 = both(0.0f), s1 = s0, s2 = s0, s3 = s0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int32_t q = lane + 32 * v;
+            if (q >= pieces) break;
+            Vec<T> dout, y, dnext, out;
+            float2 b[P], f[P];
+            dout.raw = held[q];
+            if (Y) {
+                y.raw = held[pieces + q];
+                gated(q, b);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    b[i] = mul2(mul2(y.get(2 * i), both(r)), b[i]);
+                    s1 = fma2(dout.get(2 * i), b[i], s1);
+                }
+            }
+            if (NEXT) {
+                dnext.raw = held[(Y ? 2 : 1) * pieces + q];
+                out.raw = held[(Y ? 3 : 2) * pieces + q];
+                weights(wn, q, f);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const float2 n2 = mul2(out.get(2 * i), both(r2)), dn2 = mul2(dnext.get(2 * i), f[i]);
+                    s0 = fma2(dn2, n2, s0);
+                    if (Y) {
+                        s2 = fma2(dn2, b[i], s2);
+                        s3 = fma2(n2, b[i], s3);
+                    }
+                }
+            }
+        }
+        float c1 = 0.0f, c2 = 0.0f;  // see norm_grads_kernel
+        int side = 0;
+        if (Y && NEXT) {
+            float sum[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
+            team_sums(sum, 1, nullptr, side);
+            c2 = sum[0] * by;
+            c1 = (sum[1] + r2 * (sum[2] - c2 * sum[3])) * by;
+        } else if (Y) {
+            c1 = team_sum(s1.x + s1.y, 1, nullptr, side) * by;
+        } else {
+            c2 = team_sum(s0.x + s0.y, 1, nullptr, side) * by;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int32_t q = lane + 32 * v;
+            if (q >= pieces) break;
+            Vec<T> dout, y, dnext, out, dx, dy;
+            float2 b[P], f[P];
+            dout.raw = held[q];
+            if (Y) {
+                y.raw = held[pieces + q];
+                gated(q, b);
+            }
+            if (NEXT) {
+                dnext.raw = held[(Y ? 2 : 1) * pieces + q];
+                out.raw = held[(Y ? 3 : 2) * pieces + q];
+                weights(wn, q, f);
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                float2 dt = dout.get(2 * i);
+                if (NEXT) {
+                    const float2 n2 = mul2(out.get(2 * i), both(r2)), g2 = dnext.get(2 * i);
+                    dt = fma2(both(r2), fma2(n2, both(-c2), mul2(g2, f[i])), dt);
+                    float2 &sum = sum_next[NEXT ? v : 0][i];
+                    sum = fma2(g2, n2, sum);
+                }
+                dx.set(2 * i, mul2(both(a.residual_scale), dt));
+                if (Y) {
+                    const float2 n = mul2(y.get(2 * i), both(r));
+                    dy.set(2 * i, mul2(both(r), fma2(n, both(-c1), mul2(dt, b[i]))));
+                    float2 &sum = sum_n[Y ? v : 0][i];
+                    sum = fma2(dt, n, sum);
+                }
+            }
+            store_vec<T>(a.dX, row, d, q, dx);
+            if (Y) store_vec<T>(a.dY, row, d, q, dy);
+        }
+    };
+    auto some_rows = [&](int64_t row, int64_t end, int64_t step, int64_t gate_row) {
+        ask(row, end, 0);
+        int at = 0;
+#pragma unroll 1
+        for (; row < end; row += step) {
+            ask(row + step, end, at ^ 1);
+            copies_wait<1>();
+            one_row(row, at, gate_row);
+            at ^= 1;
+        }
+        copies_wait<0>();
+    };
+    auto block_sums = [&](auto &sums, auto done) {
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int32_t q = lane + 32 * v;
+            if (q >= pieces) break;
+#pragma unroll
+            for (int i = 0; i < P; i += 2) *reinterpret_cast<float4 *>(columns + team * d + q * N + 2 * i) = make_float4(sums[v][i].x, sums[v][i].y, sums[v][i + 1].x, sums[v][i + 1].y);
+        }
+        __syncthreads();
+        for (int32_t q = threadIdx.x; q < pieces; q += blockDim.x) {  // in the order of the warps
+            float2 total[P];
+#pragma unroll
+            for (int i = 0; i < P; ++i) total[i] = both(0.0f);
+#pragma unroll 1
+            for (int t = 0; t < s.teams; ++t)
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const float2 f = *reinterpret_cast<const float2 *>(columns + t * d + q * N + 2 * i);
+                    total[i] = make_float2(total[i].x + f.x, total[i].y + f.y);
+                }
+            done(q, total);
+        }
+    };
+    auto put = [&](float *part, int32_t q, const float2 (&total)[P]) {
+#pragma unroll
+        for (int i = 0; i < P; i += 2)
+            *reinterpret_cast<float4 *>(part + (int64_t)blockIdx.x * d + (int64_t)q * N + 2 * i) = make_float4(total[i].x, total[i].y, total[i + 1].x, total[i + 1].y);
+    };
+
+    if (GATE == 2) {
+        const int64_t first = ((int64_t)blockIdx.x * s.teams + team) * s.per_team;
+#pragma unroll 1
+        for (int64_t g = first; g < min(first + s.per_team, s.groups); ++g) {
+            some_rows(g * s.group, min((g + 1) * s.group, a.T), 1, g);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {  // the group's gate gradient, and its part of dw
+                const int32_t q = lane + 32 * v;
+                if (q >= pieces) break;
+                const Vec<T> gv = load_vec<T>(a.gate, g, d, q);
+                Vec<T> dg;
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    float2 &n = sum_n[Y ? v : 0][i], &w = sum_w[GATE == 2 ? v : 0][i];
+                    w = fma2(gv.get(2 * i), n, w);
+                    dg.set(2 * i, mul2(*reinterpret_cast<const float2 *>(gw + q * N + 2 * i), n));
+                    n = both(0.0f);
+                }
+                store_vec<T>(a.dgate, g, d, q, dg);
+            }
+        }
+        block_sums(sum_w, [&](int32_t q, const float2 (&total)[P]) { put(part_w, q, total); });
+    } else {
+        const int64_t from = block_group * s.group + (blockIdx.x % s.chunks) * s.rows;
+        some_rows(from + team, min(min(from + s.rows, (block_group + 1) * s.group), a.T), s.teams, block_group);
+        if (Y)
+            block_sums(sum_n, [&](int32_t q, const float2 (&total)[P]) {
+                if (GATE == 0) {
+                    put(part_w, q, total);
+                    return;
+                }
+                const Vec<T> gv = load_vec<T>(a.gate, block_group, d, q);
+                float2 w[P], of_w[P];
+                load_floats(a.w + (int64_t)q * N, w);
+                Vec<T> dg;
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    of_w[i] = mul2(gv.get(2 * i), total[i]);
+                    dg.set(2 * i, mul2(w[i], total[i]));
+                }
+                put(part_w, q, of_w);
+                if (s.chunks > 1) put(part_gate, q, total);
+                else store_vec<T>(a.dgate, block_group, d, q, dg);
+            });
+    }
+    if (NEXT) block_sums(sum_next, [&](int32_t q, const float2 (&total)[P]) { put(part_next, q, total); });
 }
 
 // The blocks' sums added up, 32 columns a block, eight runs of blocks side by side, in double. Blocks of the grid: those of dw, of dw_next, then of every
@@ -403,9 +743,13 @@ __global__ void __launch_bounds__(256) norm_sums_kernel(const NormGradArgs a, co
 
 template <typename T, int V> int32_t launch_rows(const NormArgs &a, int warps, int teams, cudaStream_t st) {
     const dim3 grid((unsigned)cdiv(a.T, teams)), block(warps * 32 * teams);
-    if (a.y && a.next) launch_kernel(norm_rows_kernel<T, V, true, true>, grid, block, 0, st, a, warps);
-    else if (a.y) launch_kernel(norm_rows_kernel<T, V, true, false>, grid, block, 0, st, a, warps);
-    else launch_kernel(norm_rows_kernel<T, V, false, true>, grid, block, 0, st, a, warps);
+#define MOE_NORM_ROWS(Y, NEXT, GATE) launch_kernel(norm_rows_kernel<T, V, Y, NEXT, GATE>, grid, block, 0, st, a, warps)
+    if (a.y && a.next && a.gate) MOE_NORM_ROWS(true, true, true);
+    else if (a.y && a.next) MOE_NORM_ROWS(true, true, false);
+    else if (a.y && a.gate) MOE_NORM_ROWS(true, false, true);
+    else if (a.y) MOE_NORM_ROWS(true, false, false);
+    else MOE_NORM_ROWS(false, true, false);
+#undef MOE_NORM_ROWS
     MOE_LAUNCHED();
     return MOE_OK;
 }
@@ -415,13 +759,33 @@ template <typename T, int V> int32_t launch_grads(const NormGradArgs &a, const S
     float *part_w = a.ws, *part_next = part_w + most, *part_gate = part_next + most;
     if (s.blocks > 0) {
         const dim3 grid((unsigned)s.blocks), block(s.warps * 32 * s.teams);
-        const size_t shared = s.teams > 1 ? sizeof(float) * s.teams * a.d : 0;
-#define MOE_NORM_GRADS(Y, NEXT, GATE) launch_kernel(norm_grads_kernel<T, V, Y, NEXT, GATE>, grid, block, shared, st, a, s, part_w, part_next, part_gate)
-        if (a.y && a.dNext && a.gate) MOE_NORM_GRADS(true, true, true);
-        else if (a.y && a.dNext) MOE_NORM_GRADS(true, true, false);
-        else if (a.y && a.gate) MOE_NORM_GRADS(true, false, true);
-        else if (a.y) MOE_NORM_GRADS(true, false, false);
-        else MOE_NORM_GRADS(false, true, false);
+        const bool few = a.gate && s.chunks == 0;
+        const int tensors = (a.y ? 2 : 1) + (a.dNext ? 2 : 0);
+        size_t shared = s.teams > 1 ? sizeof(float) * s.teams * a.d : 0;
+        if (s.ring) shared = sizeof(float) * a.d * ((a.y ? 1 : 0) + (a.dNext ? 1 : 0)) + (size_t)s.teams * RING_ROWS * tensors * a.d * sizeof(T);
+        auto launch = [&](auto *kernel, PerDevice &allowed) -> int32_t {
+            if (s.ring && !allow_shared(allowed, kernel, SHARED_ALLOWED)) return MOE_ERR_CUDA;
+            launch_kernel(kernel, grid, block, shared, st, a, s, part_w, part_next, part_gate);
+            return MOE_OK;
+        };
+#define MOE_NORM_GRADS(Y, NEXT, GATE)                                                     \
+    do {                                                                                  \
+        static PerDevice allowed;                                                         \
+        if constexpr (V <= 4) {                                                           \
+            if (s.ring) {                                                                 \
+                MOE_TRY(launch(norm_stream_kernel<T, V, Y, NEXT, GATE>, allowed));        \
+                break;                                                                    \
+            }                                                                             \
+        }                                                                                 \
+        MOE_TRY(launch(norm_grads_kernel<T, V, Y, NEXT, GATE>, allowed));                 \
+    } while (0)
+        if (a.y && a.dNext && few) MOE_NORM_GRADS(true, true, 2);
+        else if (a.y && a.dNext && a.gate) MOE_NORM_GRADS(true, true, 1);
+        else if (a.y && a.dNext) MOE_NORM_GRADS(true, true, 0);
+        else if (a.y && few) MOE_NORM_GRADS(true, false, 2);
+        else if (a.y && a.gate) MOE_NORM_GRADS(true, false, 1);
+        else if (a.y) MOE_NORM_GRADS(true, false, 0);
+        else MOE_NORM_GRADS(false, true, 0);
 #undef MOE_NORM_GRADS
         MOE_LAUNCHED();
     }
@@ -434,9 +798,13 @@ template <typename T, int V> int32_t launch_grads(const NormGradArgs &a, const S
 }  // namespace
 
 int64_t norm_grad_floats(int64_t T, int32_t d, int32_t act) {
-    int warps, teams, V;
-    team_of(d, act, &warps, &teams, &V);
-    return 3 * most_blocks(T, teams) * d;
+    int64_t most = 0;
+    for (int tensors = 2; tensors <= 4; ++tensors) {
+        int warps, teams, V, ring;
+        grad_team_of(d, act, tensors, &warps, &teams, &V, &ring);
+        most = imax(most, most_blocks(T, teams));
+    }
+    return 3 * most * d;
 }
 
 int32_t launch_norms(const NormArgs &a, cudaStream_t st) {
@@ -448,7 +816,7 @@ int32_t launch_norms(const NormArgs &a, cudaStream_t st) {
 }
 
 int32_t launch_norm_grads(const NormGradArgs &a, cudaStream_t st) {
-    const Share s = share_of(a.T, a.d, a.act, a.gate ? a.rows_per_gate : 0);
+    const Share s = share_of(a.T, a.d, a.act, (a.y ? 2 : 1) + (a.dNext ? 2 : 0), a.gate ? a.rows_per_gate : 0);
     if (a.act == MOE_BF16) return s.V == 1 ? launch_grads<bf16, 1>(a, s, st) : s.V == 2 ? launch_grads<bf16, 2>(a, s, st) : launch_grads<bf16, 4>(a, s, st);
     return s.V == 1 ? launch_grads<float, 1>(a, s, st) : s.V == 2 ? launch_grads<float, 2>(a, s, st) : s.V == 4 ? launch_grads<float, 4>(a, s, st) : launch_grads<float, 8>(a, s, st);
 }
