@@ -181,7 +181,7 @@ struct Share {
     int warps, teams, V, ring;  // ring: rows that a warp holds in shared memory (0: a row of several warps, in registers)
     int64_t group, groups, chunks, rows, per_team, blocks;  // per_team: groups a team takes (chunks == 0)
 };
-constexpr int TEAM_ROWS = 4;
+constexpr int TEAM_ROWS = 4;  // 8192 x 512, main and sums: 10.3 us; 1, 2 and 3 rows 14.2, 14.5 and 11.9
 // rows of a team: blocks for two waves, of one block an SM where blocks are large (131072 x 1024: one wave 293 us, two 295, three 298, six 322) and of three where not
 int64_t team_rows(int64_t T, int teams) { return imax(TEAM_ROWS, cdiv(T, (int64_t)teams * 148 * (teams > 8 ? 2 : 6))); }
 // Forward: a warp has a row up to 32 vectors a lane, else several do
@@ -465,6 +465,30 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
     uint4 *mine = ring + (int64_t)team * RING_ROWS * TENSORS * pieces;
     const float by = 1.0f / (float)d;
     const int64_t block_group = GATE == 2 ? 0 : blockIdx.x / s.chunks;
+    // a row's pieces of this lane, to place `at` of the ring; its factors go with it
+    auto ask = [&](int64_t row, int64_t end, int at) {
+        if (row < end)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int32_t q = lane + 32 * v;
+                if (q >= pieces) break;
+                uint4 *to = mine + at * TENSORS * pieces + q;
+                const int64_t from = row * d + (int64_t)q * N;
+                if (a.dOut) copy16(to, static_cast<const T *>(a.dOut) + from);
+                else zero16(to);
+                if (Y) copy16(to + pieces, static_cast<const T *>(a.y) + from);
+                if (NEXT) {
+                    copy16(to + (Y ? 2 : 1) * pieces, static_cast<const T *>(a.dNext) + from);
+                    copy16(to + (Y ? 3 : 2) * pieces, static_cast<const T *>(a.out) + from);
+                }
+            }
+        copies_commit();
+    };
+    // the block's rows of this warp, or (GATE 2) its groups; the first row is on its way before everything else
+    const int64_t first_group = ((int64_t)blockIdx.x * s.teams + team) * s.per_team;
+    const int64_t first = GATE == 2 ? first_group * s.group : block_group * s.group + (blockIdx.x % s.chunks) * s.rows + team;
+    const int64_t last = GATE == 2 ? min((first_group + 1) * s.group, a.T) : min(min(first - team + s.rows, (block_group + 1) * s.group), a.T);
+    ask(first, last, 0);
     for (int32_t q = threadIdx.x; q < pieces; q += blockDim.x) {
         float2 f[P];
         Vec<T> g;
@@ -490,25 +514,6 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
             if (GATE == 2) sum_w[GATE == 2 ? v : 0][i] = both(0.0f);
             if (NEXT) sum_next[NEXT ? v : 0][i] = both(0.0f);
         }
-    // a row's pieces of this lane, to place `at` of the ring; its factors go with it
-    auto ask = [&](int64_t row, int64_t end, int at) {
-        if (row < end)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int32_t q = lane + 32 * v;
-                if (q >= pieces) break;
-                uint4 *to = mine + at * TENSORS * pieces + q;
-                const int64_t from = row * d + (int64_t)q * N;
-                if (a.dOut) copy16(to, static_cast<const T *>(a.dOut) + from);
-                else zero16(to);
-                if (Y) copy16(to + pieces, static_cast<const T *>(a.y) + from);
-                if (NEXT) {
-                    copy16(to + (Y ? 2 : 1) * pieces, static_cast<const T *>(a.dNext) + from);
-                    copy16(to + (Y ? 3 : 2) * pieces, static_cast<const T *>(a.out) + from);
-                }
-            }
-        copies_commit();
-    };
     auto one_row = [&](int64_t row, int at, int64_t gate_row) {
         const uint4 *held = mine + at * TENSORS * pieces;
         const float r = Y ? a.rstd[row] : 0.0f, r2 = NEXT ? a.rstd_next[row] : 0.0f;
@@ -609,8 +614,7 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
             if (Y) store_vec<T>(a.dY, row, d, q, dy);
         }
     };
-    auto some_rows = [&](int64_t row, int64_t end, int64_t step, int64_t gate_row) {
-        ask(row, end, 0);
+    auto some_rows = [&](int64_t row, int64_t end, int64_t step, int64_t gate_row) {  // the first one has been asked for
         int at = 0;
 #pragma unroll 1
         for (; row < end; row += step) {
@@ -652,9 +656,9 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
     };
 
     if (GATE == 2) {
-        const int64_t first = ((int64_t)blockIdx.x * s.teams + team) * s.per_team;
 #pragma unroll 1
-        for (int64_t g = first; g < min(first + s.per_team, s.groups); ++g) {
+        for (int64_t g = first_group; g < min(first_group + s.per_team, s.groups); ++g) {
+            if (g > first_group) ask(g * s.group, a.T, 0);
             some_rows(g * s.group, min((g + 1) * s.group, a.T), 1, g);
 #pragma unroll
             for (int v = 0; v < V; ++v) {  // the group's gate gradient, and its part of dw
@@ -674,8 +678,7 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
         }
         block_sums(sum_w, [&](int32_t q, const float2 (&total)[P]) { put(part_w, q, total); });
     } else {
-        const int64_t from = block_group * s.group + (blockIdx.x % s.chunks) * s.rows;
-        some_rows(from + team, min(min(from + s.rows, (block_group + 1) * s.group), a.T), s.teams, block_group);
+        some_rows(first, last, s.teams, block_group);
         if (Y)
             block_sums(sum_n, [&](int32_t q, const float2 (&total)[P]) {
                 if (GATE == 0) {
@@ -699,12 +702,13 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
     if (NEXT) block_sums(sum_next, [&](int32_t q, const float2 (&total)[P]) { put(part_next, q, total); });
 }
 
-// The blocks' sums added up, 32 columns a block, eight runs of blocks side by side, in double. Blocks of the grid: those of dw, of dw_next, then of every
-// gate that several blocks share.
+// The blocks' sums added up, 32 columns a block, RUNS runs of blocks side by side, eight loads of each in flight, in double and in a fixed order. Blocks of the grid: those of dw, of
+// dw_next, then of every gate that several blocks share.
+constexpr int RUNS = 32;
 template <typename T>
-__global__ void __launch_bounds__(256) norm_sums_kernel(const NormGradArgs a, const Share s, const float *part_w, const float *part_next, const float *part_gate) {
+__global__ void __launch_bounds__(RUNS * 32) norm_sums_kernel(const NormGradArgs a, const Share s, const float *part_w, const float *part_next, const float *part_gate) {
     wait_previous_kernel();
-    __shared__ double sh[8][32];
+    __shared__ double sh[RUNS][32];
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
     const int32_t slabs = (a.d + 31) / 32;
     const int64_t job = blockIdx.x / slabs;
@@ -720,23 +724,21 @@ __global__ void __launch_bounds__(256) norm_sums_kernel(const NormGradArgs a, co
         from = gate_row * s.chunks;
         count = s.chunks;
     }
-    const int64_t each = (count + 7) / 8, lo = from + run * each, hi = min(lo + each, from + count);
+    const int64_t each = (count + RUNS - 1) / RUNS, lo = from + run * each, hi = min(lo + each, from + count);
     double sum = 0.0;
-    if (col < a.d) {
-        float f[4];
-        int64_t b = lo;
-        for (; b + 4 <= hi; b += 4) {
+    if (col < a.d)
+        for (int64_t b = lo; b < hi; b += 8) {
+            float f[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = part[(b + i) * a.d + col];
+            for (int i = 0; i < 8; ++i) f[i] = b + i < hi ? part[(b + i) * a.d + col] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum += f[i];
+            for (int i = 0; i < 8; ++i) sum += f[i];
         }
-        for (; b < hi; ++b) sum += part[b * a.d + col];
-    }
     sh[run][lane] = sum;
     __syncthreads();
     if (run > 0 || col >= a.d) return;
-    for (int i = 1; i < 8; ++i) sum += sh[i][lane];
+#pragma unroll 8
+    for (int i = 1; i < RUNS; ++i) sum += sh[i][lane];
     if (to) to[col] = (float)sum;
     else static_cast<T *>(a.dgate)[gate_row * a.d + col] = from_f32<T>((float)(a.w[col] * sum));
 }
@@ -790,7 +792,7 @@ template <typename T, int V> int32_t launch_grads(const NormGradArgs &a, const S
         MOE_LAUNCHED();
     }
     const int64_t jobs = (a.y ? 1 : 0) + (a.dNext ? 1 : 0) + (a.gate && s.chunks > 1 ? s.groups : 0);
-    launch_kernel(norm_sums_kernel<T>, dim3((unsigned)(jobs * cdiv(a.d, 32))), dim3(256), 0, st, a, s, (const float *)part_w, (const float *)part_next, (const float *)part_gate);
+    launch_kernel(norm_sums_kernel<T>, dim3((unsigned)(jobs * cdiv(a.d, 32))), dim3(RUNS * 32), 0, st, a, s, (const float *)part_w, (const float *)part_next, (const float *)part_gate);
     MOE_LAUNCHED();
     return MOE_OK;
 }
