@@ -24,9 +24,6 @@ namespace {
 constexpr int THREADS = 256, EACH = 8;            // elements a thread holds at a time
 constexpr int STEP = THREADS * EACH;              // elements a block holds at a time: 16 blocks of codes, 16 lanes each
 constexpr int CHUNK = 4 * STEP;                   // elements of a block of the grid
-#ifndef EIGHT_BLOCKS
-#define EIGHT_BLOCKS 4
-#endif
 constexpr int MAX_LIST = 96;                      // tensors of a launch (a launch's parameters hold them: 9 KiB)
 
 struct Entry {
@@ -306,7 +303,7 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
 
 // A block finds its tensor in the list and takes CHUNK elements of it. Tensors with 8-bit moments are launched apart from those with float ones, whose kernel needs fewer registers.
 template <bool EIGHT>
-__global__ void __launch_bounds__(THREADS, EIGHT ? EIGHT_BLOCKS : 3) adamw_kernel(const __grid_constant__ Batch b, Constants k, moe_adamw_rates given, const moe_adamw_rates *read) {
+__global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) adamw_kernel(const __grid_constant__ Batch b, Constants k, moe_adamw_rates given, const moe_adamw_rates *read) {
     wait_previous_kernel();
     const moe_adamw_rates r = read ? *read : given;
     int32_t lo = 0, hi = b.n;

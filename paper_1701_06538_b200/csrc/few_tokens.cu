@@ -1,7 +1,7 @@
 // The whole layer for a few tokens (serving): two launches, three with more than 256 experts. The experts' weights are read once, by tensor copies that run ahead
 // of everything else, and that is what bounds it: a matrix of 512 x 1024 in bf16 is 1 MB for two or three rows.
 //
-//   few_logits_kernel   the logits of every token by the fixed chain of multiply-adds of moe_gate, and the second launch's counters set to 0. The blocks of eight tokens are a
+//   few_logits_kernel   the logits of every token by the fixed chain of multiply-adds of moe_gate, and the second launch's counters set to 0. The blocks of four tokens are a
 //                       cluster, whose first block gets all their logits and picks the experts (top k, softmax)
 //   few_select_kernel   picks them from logits in memory, where a cluster does not hold the gate (more than 256 experts)
 //   few_experts_kernel  one block per SM. Every block sorts the slots by expert. The products then are
@@ -26,9 +26,6 @@ namespace moe {
 
 namespace {
 
-#ifndef FEW_TASKS
-#define FEW_TASKS 6
-#endif
 constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
 constexpr int TILE_K = 64, TILE_BYTES = TILE_K * 128, RING = 3;
 constexpr int MAX_ROWS = MOE_FEW_MAX_TOKENS * MOE_MAX_K;
@@ -183,9 +180,9 @@ __device__ __forceinline__ float logit_step(float acc, uint32_t ws, uint32_t xt)
 template <typename T, bool FOURS, bool ROUTE>
 __global__ void __launch_bounds__(256) few_logits_kernel(const T *__restrict__ x, const float *__restrict__ Wg, int32_t tokens, int32_t d, int32_t n, int32_t k,
                                                          float *__restrict__ logits, const Routing r, bf16 *copy, int32_t dw, int32_t *clear, int32_t clear_count, int32_t *status) {
-#ifdef FEW_TRIGGER
+    // The experts' blocks may come as soon as there is room for them: they set up barriers and tables meanwhile and wait for this launch's end before they read of it.
+    // 29.7 -> 27.8 us (1 token, 1024 x 4096), 36.6 -> 34.4 (24 tokens, 32 experts of 512 x 1024). L2 asked for the weights from there as well cost 2 to 3 us again.
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-#endif
     wait_previous_kernel();
     __shared__ float all[ROUTE ? LOGIT_TOKENS : 1][ROUTE ? LOGIT_BLOCKS * 32 : 1];
     __shared__ __align__(16) float xf[2][LOGIT_TOKENS][LOGIT_STEP];
@@ -286,6 +283,7 @@ struct FewShared {
     float gate[MAX_ROWS];                                   // of a slot
     int16_t rows[MAX_ROWS];                                 // slots by expert
     int16_t seg_expert[MAX_ROWS], seg_first[MAX_ROWS], seg_count[MAX_ROWS];
+    int32_t known_ready[MAX_ROWS];                          // a warp of this block has seen a segment's hid complete
     int32_t queue[FEW_WARPS][8];                            // a warp's tasks from the one at hand to the one whose tiles are being asked for
 };
 // Tables by expert, in the place of the rings before the first copy: the tokens that have picked it, a bit each; where its rows begin
@@ -312,7 +310,7 @@ __device__ __forceinline__ void add_release(int32_t *p, int32_t by) {
     asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(by) : "memory");
 }
 
-// The segments: the experts in use by their first slots, an expert's slots in ascending order, 32 of them at most in a segment. The same in every block. By the whole block.
+// The segments: the experts in use by their first slots, an expert's slots in ascending order, 16 of them at most in a segment. The same in every block. By the whole block.
 __device__ __forceinline__ void make_segments(const Few &a, FewShared &S, FewTables &tab, int warp, int lane) {
     const int32_t R = a.T * a.k, tid = threadIdx.x;
     // two slots a thread
@@ -508,6 +506,9 @@ template <typename T> struct Worker {
     }
     __device__ bool wait_ready(int32_t segment) {
         bool ok = true;
+        int32_t known;  // what the other warp has acquired reaches this one through the block's memory
+        asm volatile("ld.acquire.cta.shared.s32 %0, [%1];" : "=r"(known) : "r"(smem_u32(&S.known_ready[segment])) : "memory");
+        if (__all_sync(0xffffffffu, known)) return true;
         if (lane == 0) {
             unsigned long long t0 = 0;
             while (load_relaxed(a.ready + segment * READY_STEP) < a.cols1) {
@@ -524,7 +525,9 @@ template <typename T> struct Worker {
             }
         }
         __threadfence();
-        return __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok && lane == 0) asm volatile("st.release.cta.shared.s32 [%0], %1;" ::"r"(smem_u32(&S.known_ready[segment])), "r"(1) : "memory");
+        return ok;
     }
 
     // hid of one row, four columns of it, from its sums
@@ -832,6 +835,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_experts_kernel(const __gri
     }
     FewTables &tab = *reinterpret_cast<FewTables *>(base);
     for (int32_t i = threadIdx.x; i < a.n; i += FEW_THREADS) tab.tokens[i] = make_uint2(0u, 0u);
+    for (int32_t i = threadIdx.x; i < MAX_ROWS; i += FEW_THREADS) S.known_ready[i] = 0;
     if (threadIdx.x < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(threadIdx.x ? &w2 : &w1) : "memory");
     wait_previous_kernel();
     const int32_t first = lane == 0 ? atomicAdd(a.ticket, 1) : 0;  // on its way meanwhile
@@ -854,10 +858,10 @@ struct FewPlan {
     int32_t cols1, pieces1, piece_tiles1, cols2, pieces2, piece_tiles2;
     int64_t done1, done2, counters;
 };
-// Pieces of a contraction of `tiles` tiles for `cols` tiles of columns of `segments` experts: three tasks for every SM, so that their rings together keep memory busy, and none of
-// more than `most` tiles
+// Pieces of a contraction of `tiles` tiles for `cols` tiles of columns of `segments` experts: six tasks for every SM, so that their rings together keep memory busy, and none of
+// more than `most` tiles: of y 8 (1 / 24 / 64 tokens as above: 29.7 / 36.6 / 84.1 us; 4: 28.5 / 35.2 / 86.2; 16: 30.1 / 37.2 / 90.0)
 void pieces_of(int64_t segments, int64_t cols, int64_t tiles, int64_t most, int32_t *pieces, int32_t *piece_tiles) {
-    int64_t n = imin(tiles, cdiv(FEW_TASKS * 148, segments * cols));
+    int64_t n = imin(tiles, cdiv(6 * 148, segments * cols));
     n = imax(n, cdiv(tiles, most));
     *piece_tiles = (int32_t)cdiv(tiles, n);
     *pieces = (int32_t)cdiv(tiles, *piece_tiles);
@@ -871,8 +875,7 @@ FewPlan plan_of(const moe_config &c) {
     p.cols1 = (int32_t)cdiv(c.h, width);
     p.cols2 = (int32_t)cdiv(c.d, width);
     pieces_of(segments, p.cols1, cdiv(c.d, TILE_K), 16, &p.pieces1, &p.piece_tiles1);
-    // the last tasks of a call: a warp gets through a tile in 1.5 us when all are busy
-    pieces_of(segments, p.cols2, cdiv(c.h, TILE_K), segments * p.cols2 > 148 * FEW_WARPS / 2 ? 4 : 8, &p.pieces2, &p.piece_tiles2);
+    pieces_of(segments, p.cols2, cdiv(c.h, TILE_K), 8, &p.pieces2, &p.piece_tiles2);
     p.done1 = 64 + R * READY_STEP;  // behind the ticket and the segments' columns
     p.done2 = p.done1 + (p.pieces1 > 1 ? R * p.cols1 : 0);
     p.counters = p.done2 + (int64_t)c.T * p.cols2;
