@@ -41,7 +41,7 @@ struct Batch {
     int32_t chunks_before[MAX_LIST + 1];
     int32_t n;
 };
-struct Constants { float beta1, one_beta1, beta2, one_beta2, eps; };
+struct Constants { float beta1, one_beta1, beta2, one_beta2, eps, one; };
 
 // The low-bias hash of 32 bits of C. Wellons ("Prospecting for Hash Functions", 2018): two multiplications between three shifts. Without the last shift, which changes the lower half alone
 __device__ __forceinline__ uint32_t mix_but_last(uint32_t x) {
@@ -53,16 +53,21 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// The hardware's root and reciprocal, within two units of the last place: of the divisor, and of a second moment that is kept in four bits
+// The hardware's root and reciprocal, within two units of the last place: of the divisor of a step
 __device__ __forceinline__ float root_of(float v) {
     float r;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float normal_root_of(float v) {  // 0 of what is below float's smallest normal number: four instructions less
-    float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
+// Minus the roots of two second moments, which are given as minus v: the hardware's reciprocal root y, s = v y and a Newton step s + (v - s s) y / 2, whose rounding is that of
+// the root itself but for one in a million or so. What goes into a code has to be exact: a unit of the last place turns a code over in one element of 600,000, and a code is 6 to 12 %.
+// Of v below float's smallest normal number it is off, but still between 0 and that number's root; of an infinite v it is a NaN, which it is held as too.
+__device__ __forceinline__ float2 minus_roots(float2 minus_v) {
+    float2 y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(-minus_v.x, FLT_MIN)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(-minus_v.y, FLT_MIN)));
+    const float2 s = mul2(minus_v, y);
+    return fma2(fma2(s, s, minus_v), mul2(y, both(0.5f)), s);
 }
 __device__ __forceinline__ float reciprocal(float v) {  // of normal numbers; 0 beyond 2^126
     float r;
@@ -77,6 +82,11 @@ __device__ __forceinline__ float is_below(float a, float b) {  // 1 or 0
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max_size(float a, float b, float c) {  // of three magnitudes
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 
@@ -141,13 +151,12 @@ __device__ __forceinline__ void decode(const uint2 &two, float (&v)[EACH]) {
         v[i + 1] = f.y;
     }
 }
-// The codes of a block and its scale; an element that is no finite number is held as a NaN and has no part in the scale. ROOT: values of 0 and more, whose codes stay above 0 (they
+// The codes of a block and its scale; an element that is no finite number is held as a NaN and has no part in the scale. ROOT: minus values of 0 and more, whose codes stay above 0 (they
 // divide). bits: the hash without its last shift; its upper half is that of the hash, the lower half changes
 template <bool ROOT, bool FULL>
 __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, int64_t live, const float (&v)[EACH], const uint32_t (&bits)[EACH]) {
-    float largest = 0.0f;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) largest = max_nan(largest, fabsf(v[i]));
+    static_assert(EACH == 8, "its magnitudes, two at a time behind the first");
+    float largest = max_size(max_size(max_size(max_size(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) largest = max_nan(largest, __shfl_xor_sync(0xffffffffu, largest, off));
     const bool odd = __any_sync(0xffffffffu, !(largest <= FLT_MAX));  // rare: the largest of the others
@@ -158,24 +167,35 @@ __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, int64_t
 #pragma unroll
         for (int off = 8; off > 0; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, off));
     }
-    const float scale = largest > 0.0f ? fmaxf(largest * (1.0f / 448.0f), FLT_MIN) : 0.0f, by = largest > 0.0f ? reciprocal(scale) : 0.0f;
+    const float scale = largest > 0.0f ? fmaxf(largest * (1.0f / 448.0f), FLT_MIN) : 0.0f, guess = reciprocal(scale);
+    // Values over the scale, rounded as a division rounds: a product with the reciprocal, its remainder, and the product corrected by it (Markstein, 1990)
+    const float by = largest > 0.0f ? fmaf(fmaf(-scale, guess, 1.0f), guess, guess) : 0.0f;
     uint32_t c[2] = {0u, 0u};
-    // Up or down to a multiple of the code's unit: the 20 bits below e4m3's three are added a dither (16 random bits in bits 4 to 19, and 8) and cut off. Below 2^-6
+    // Up or down to a multiple of the code's unit: the 20 bits below e4m3's three are added a dither (16 random bits in bits 4 to 19, and 8) and cut off, whatever the sign. Below 2^-6
     // the unit stays 2^-9, which is that of the numbers from 2^-6 to 2^-5. (Up from 448 gives 480, which the conversion takes for 448.)
+    const float near = ROOT ? -by : by, off_by = ROOT ? scale : -scale;
 #pragma unroll
     for (int i = 0; i < EACH; i += 2) {
-        const float2 size = mul2(make_float2(fabsf(v[i]), fabsf(v[i + 1])), both(by));
-        const float2 small = make_float2(is_below(size.x, 0.015625f), is_below(size.y, 0.015625f)), up = fma2(small, both(0.015625f), size);
-        auto cut = [&](float u, uint32_t x) { return __uint_as_float((__float_as_uint(u) + (((ROOT ? x >> 12 : (x ^ (x >> 16)) << 4) & 0xffff0u) | 8u)) & ~0xfffffu); };
-        float2 z = fma2(small, both(-0.015625f), make_float2(cut(up.x, bits[i]), cut(up.y, bits[i + 1])));
-        if (ROOT) {  // the smallest code at least for what is not 0: of normal numbers over the largest, 2^127 times as much is above it
-            const float2 least = mul2(size, both(1.7014118e38f));
-            z = make_float2(fmaxf(z.x, fminf(least.x, 0.001953125f)), fmaxf(z.y, fminf(least.y, 0.001953125f)));
-        }
-        if (!ROOT) z = make_float2(copysignf(z.x, v[i]), copysignf(z.y, v[i + 1]));
+        const float2 of = make_float2(v[i], v[i + 1]), first = mul2(of, both(near)), q = fma2(fma2(first, both(off_by), of), both(near), first);
+        float2 small = make_float2(is_below(fabsf(q.x), 0.015625f), is_below(fabsf(q.y), 0.015625f));
+        if (!ROOT) small = make_float2(copysignf(small.x, q.x), copysignf(small.y, q.y));
+        const float2 up = fma2(small, both(0.015625f), q);
+        auto cut = [&](float u, uint32_t x) {
+            const uint32_t dither = ROOT ? (x & 0xffff0000u) | 0x8000u : (x * 0x10000u + 0x8000u) ^ (x & 0xffff0000u);  // 12 bits up: the hash's upper half, or its lower half
+            return __uint_as_float((__float_as_uint(u) + (dither >> 12)) & ~0xfffffu);
+        };
+        const float2 z = fma2(small, both(-0.015625f), make_float2(cut(up.x, bits[i]), cut(up.y, bits[i + 1])));
         const __nv_fp8x2_storage_t two = __nv_cvt_float2_to_fp8x2(z, __NV_SATFINITE, __NV_E4M3);
         c[i / 4] |= (uint32_t)two << (8 * (i % 4));
     }
+    // the smallest code at least for a root that is not 0. Few codes are 0: one test for four of them
+    if (ROOT)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if ((c[j] - 0x01010101u) & ~c[j] & 0x80808080u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if ((c[j] >> (8 * i) & 0xffu) == 0 && v[4 * j + i] != 0.0f) c[j] |= 1u << (8 * i);
     if (odd)
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
@@ -222,7 +242,7 @@ template <typename WT, typename GT, bool MASTER, bool FULL>
 __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, const Constants &k, const moe_adamw_rates &r) {
     using MT = typename std::conditional<MASTER, float, WT>::type;  // of what the step is taken on
     const float down = -r.lr / r.bias1, root_by = 1.0f / sqrtf(r.bias2), keep = 1.0f - r.lr * t.decay;
-    const float by_g = k.one_beta1 * r.grad_scale, by_gg = k.one_beta2 * r.grad_scale * r.grad_scale;
+    const float by_g = k.one_beta1 * r.grad_scale, minus_by_gg = -k.one_beta2 * r.grad_scale * r.grad_scale;
     const int64_t at = chunk * CHUNK + threadIdx.x * EACH;
     WT *w_at = static_cast<WT *>(t.w) + at;
     MT *from = MASTER ? reinterpret_cast<MT *>(t.master) + at : reinterpret_cast<MT *>(w_at);
@@ -270,16 +290,16 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
         uint32_t bits[EACH];
         decode(m_codes, m);
         decode(v_codes, root);
-        const float by_m = k.beta1 * ms;
 #pragma unroll
         for (int e = 0; e < EACH; e += 2) {
             bits[e] = mix_but_last(key ^ e);
             bits[e + 1] = mix_but_last(key ^ (e + 1));
             const float2 gg = make_float2(g[e], g[e + 1]);
-            const float2 mm = fma2(make_float2(m[e], m[e + 1]), both(by_m), mul2(both(by_g), gg));
+            // Every product and sum rounded by itself, as the formulas have them: other roundings are as good, but turn codes over (minus_roots()). A sum is a
+            // multiply-add by a 1 that the compiler does not know: of a packed product and a packed sum the assembler makes one multiply-add
+            const float2 mm = fma2(both(k.one), mul2(both(k.beta1), mul2(make_float2(m[e], m[e + 1]), both(ms))), mul2(both(by_g), gg));
             const float2 old = mul2(make_float2(root[e], root[e + 1]), both(vs));
-            const float2 vv = fma2(mul2(both(k.beta2), old), old, mul2(mul2(both(by_gg), gg), gg));
-            const float2 rt = make_float2(normal_root_of(vv.x), normal_root_of(vv.y)), den = fma2(rt, both(root_by), both(k.eps));
+            const float2 rt = minus_roots(fma2(both(k.one), mul2(both(-k.beta2), mul2(old, old)), mul2(both(minus_by_gg), mul2(gg, gg)))), den = fma2(rt, both(-root_by), both(k.eps));
             const float2 ww = fma2(mul2(mm, both(down)), make_float2(reciprocal(den.x), reciprocal(den.y)), mul2(make_float2(w[e], w[e + 1]), both(keep)));
             m[e] = mm.x; m[e + 1] = mm.y;
             root[e] = rt.x; root[e + 1] = rt.y;
@@ -353,7 +373,7 @@ int32_t check_tensor(const moe_adamw_tensor &t) {
 
 int32_t launch_adamw(const moe_adamw_tensor *tensors, int32_t count, const moe_adamw_params &p, const moe_adamw_rates *rates, cudaStream_t st) {
     for (int32_t i = 0; i < count; ++i) MOE_TRY(check_tensor(tensors[i]));
-    const Constants k = {(float)p.beta1, (float)(1.0 - p.beta1), (float)p.beta2, (float)(1.0 - p.beta2), (float)p.eps};
+    const Constants k = {(float)p.beta1, (float)(1.0 - p.beta1), (float)p.beta2, (float)(1.0 - p.beta2), (float)p.eps, 1.0f};
     moe_adamw_rates given = {};
     if (!rates) given = {(float)p.lr, (float)(1.0 - pow(p.beta1, p.step)), (float)(1.0 - pow(p.beta2, p.step)), (float)p.grad_scale, p.seed};
     Batch lists[2];  // of float moments, of 8-bit ones
