@@ -16,6 +16,7 @@
 
 #include "block.cuh"
 #include "pairs.cuh"
+#include "tc.cuh"
 
 namespace moe {
 
@@ -23,7 +24,9 @@ namespace {
 
 constexpr int THREADS = 256, EACH = 8;            // elements a thread holds at a time
 constexpr int STEP = THREADS * EACH;              // elements a block holds at a time: 16 blocks of codes, 16 lanes each
-constexpr int CHUNK = 4 * STEP;                   // elements of a block of the grid
+constexpr int FLOAT_STEPS = 4, MOST_STEPS = 16;   // steps of a block of the grid: with float moments (16 of them: 163 us for 33 million elements, not 144); with 8-bit ones at most,
+                                                  // which have more to do before the first (268 million elements: 4, 8, 16 and 32 steps 635, 612, 605 and 609 us)
+constexpr int EIGHT_BLOCKS = 3;                   // blocks of an SM with 8-bit moments (4, whose 64 registers are too few: 642 us with 4 steps; 2: 763)
 constexpr int MAX_LIST = 96;                      // tensors of a launch (a launch's parameters hold them: 9 KiB)
 
 struct Entry {
@@ -39,17 +42,18 @@ struct Entry {
 struct Batch {
     Entry t[MAX_LIST];
     int32_t chunks_before[MAX_LIST + 1];
-    int32_t n;
+    int32_t n, steps;
 };
 struct Constants { float beta1, one_beta1, beta2, one_beta2, eps, one; };
 
-// The low-bias hash of 32 bits of C. Wellons ("Prospecting for Hash Functions", 2018): two multiplications between three shifts. Without the last shift, which changes the lower half alone
-__device__ __forceinline__ uint32_t mix_but_last(uint32_t x) {
-    x = (x ^ (x >> 16)) * 0x7feb352du;
+// The low-bias hash of 32 bits of C. Wellons ("Prospecting for Hash Functions", 2018): two multiplications between three shifts. mix_inner: without the first shift, which is the same for
+// numbers that differ in their lower half alone, and the last, which changes the lower half alone
+__device__ __forceinline__ uint32_t mix_inner(uint32_t x) {
+    x *= 0x7feb352du;
     return (x ^ (x >> 15)) * 0x846ca68bu;
 }
 __device__ __forceinline__ uint32_t mix(uint32_t x) {
-    x = mix_but_last(x);
+    x = mix_inner(x ^ (x >> 16));
     return x ^ (x >> 16);
 }
 
@@ -79,10 +83,13 @@ __device__ __forceinline__ float is_below(float a, float b) {  // 1 or 0
     asm("set.lt.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
+__device__ __forceinline__ float max_of_block(float v) {  // over the half of a warp that holds a block of codes; a NaN stays. (One redux.sync for the four steps: 687 us, not 647.)
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) {
+        const float o = __shfl_xor_sync(0xffffffffu, v, off);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(o));
+    }
+    return v;
 }
 __device__ __forceinline__ float max_size(float a, float b, float c) {  // of three magnitudes
     float r;
@@ -157,15 +164,13 @@ template <bool ROOT, bool FULL>
 __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, int64_t live, const float (&v)[EACH], const uint32_t (&bits)[EACH]) {
     static_assert(EACH == 8, "its magnitudes, two at a time behind the first");
     float largest = max_size(max_size(max_size(max_size(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) largest = max_nan(largest, __shfl_xor_sync(0xffffffffu, largest, off));
+    largest = max_of_block(largest);
     const bool odd = __any_sync(0xffffffffu, !(largest <= FLT_MAX));  // rare: the largest of the others
     if (odd) {
         largest = 0.0f;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) largest = fabsf(v[i]) <= FLT_MAX ? fmaxf(largest, fabsf(v[i])) : largest;
-#pragma unroll
-        for (int off = 8; off > 0; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, off));
+        largest = max_of_block(largest);
     }
     const float scale = largest > 0.0f ? fmaxf(largest * (1.0f / 448.0f), FLT_MIN) : 0.0f, guess = reciprocal(scale);
     // Values over the scale, rounded as a division rounds: a product with the reciprocal, its remainder, and the product corrected by it (Markstein, 1990)
@@ -213,6 +218,7 @@ __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, int64_t
 template <typename WT, typename GT, bool MASTER>
 __device__ __forceinline__ void update(const Entry &t, int64_t chunk, const Constants &k, const moe_adamw_rates &r) {
     const float step = r.lr / r.bias1, root_by = 1.0f / sqrtf(r.bias2), keep = r.lr * t.decay;
+    constexpr int CHUNK = FLOAT_STEPS * STEP;
     const int64_t end = min(t.count, (chunk + 1) * CHUNK);
     for (int64_t base = chunk * CHUNK; base < end; base += STEP) {
         const int64_t at = base + threadIdx.x * EACH, live = end - at;  // at most 0 behind the end
@@ -236,14 +242,14 @@ __device__ __forceinline__ void update(const Entry &t, int64_t chunk, const Cons
     }
 }
 
-// With 8-bit moments the arithmetic is as much as the memory: 93 instructions an element as it was written first, 1218 us for 268 million elements, whose bytes take 415. FULL: a chunk
-// without a tensor's end
+// With 8-bit moments the arithmetic is more than the memory: 66 instructions an element (93 as it was written first: 1218 us), issued in three cycles of four, 596 us for 268
+// million elements, whose bytes take 415. begin: the block's first element; FULL: none of its steps meets the tensor's end
 template <typename WT, typename GT, bool MASTER, bool FULL>
-__device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, const Constants &k, const moe_adamw_rates &r) {
+__device__ __forceinline__ void update_eight(const Entry &t, int64_t begin, int32_t steps, const Constants &k, const moe_adamw_rates &r) {
     using MT = typename std::conditional<MASTER, float, WT>::type;  // of what the step is taken on
     const float down = -r.lr / r.bias1, root_by = 1.0f / sqrtf(r.bias2), keep = 1.0f - r.lr * t.decay;
     const float by_g = k.one_beta1 * r.grad_scale, minus_by_gg = -k.one_beta2 * r.grad_scale * r.grad_scale;
-    const int64_t at = chunk * CHUNK + threadIdx.x * EACH;
+    const int64_t at = begin + threadIdx.x * EACH;
     WT *w_at = static_cast<WT *>(t.w) + at;
     MT *from = MASTER ? reinterpret_cast<MT *>(t.master) + at : reinterpret_cast<MT *>(w_at);
     const GT *g_at = static_cast<const GT *>(t.g) + at;
@@ -268,8 +274,8 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
     };
     if constexpr (FULL) fetch(0);
 #pragma unroll 1
-    for (int i = 0; i < CHUNK / STEP; ++i) {
-        if (!FULL && chunk * CHUNK + i * STEP >= t.count) break;  // the whole block
+    for (int32_t i = 0; i < steps; ++i) {
+        if (!FULL && begin + i * STEP >= t.count) break;  // the whole block
         float g[EACH], m[EACH], root[EACH], w[EACH];
         uint2 m_codes, v_codes;
         float ms, vs;
@@ -277,7 +283,7 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
             held.w.floats(w);
             held.g.floats(g);
             m_codes = held.m; v_codes = held.v; ms = held.ms; vs = held.vs;
-            if (i + 1 < CHUNK / STEP) fetch(1);
+            if (i + 1 < steps) fetch(1);
         } else {
             load8(from, 0, live, w);
             load8(g_at, 0, live, g);
@@ -286,14 +292,15 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
             ms = live > 0 ? *ms_at : 0.0f;
             vs = live > 0 ? *vs_at : 0.0f;
         }
-        const uint32_t key = mix(seed + (uint32_t)(number >> 32) * 0x9e3779b9u) ^ (uint32_t)number;
+        uint32_t key = mix(seed + (uint32_t)(number >> 32) * 0x9e3779b9u) ^ (uint32_t)number;
+        key ^= key >> 16;
         uint32_t bits[EACH];
         decode(m_codes, m);
         decode(v_codes, root);
 #pragma unroll
         for (int e = 0; e < EACH; e += 2) {
-            bits[e] = mix_but_last(key ^ e);
-            bits[e + 1] = mix_but_last(key ^ (e + 1));
+            bits[e] = mix_inner(key ^ e);
+            bits[e + 1] = mix_inner(key ^ (e + 1));
             const float2 gg = make_float2(g[e], g[e + 1]);
             // Every product and sum rounded by itself, as the formulas have them: other roundings are as good, but turn codes over (minus_roots()). A sum is a
             // multiply-add by a 1 that the compiler does not know: of a packed product and a packed sum the assembler makes one multiply-add
@@ -316,14 +323,14 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, cons
     }
 }
 template <typename WT, typename GT, bool MASTER>
-__device__ __forceinline__ void update_eight(const Entry &t, int64_t chunk, const Constants &k, const moe_adamw_rates &r) {
-    if ((chunk + 1) * CHUNK <= t.count) update_eight<WT, GT, MASTER, true>(t, chunk, k, r);
-    else update_eight<WT, GT, MASTER, false>(t, chunk, k, r);
+__device__ __forceinline__ void update_eight(const Entry &t, int64_t begin, int32_t steps, const Constants &k, const moe_adamw_rates &r) {
+    if (begin + steps * STEP <= t.count) update_eight<WT, GT, MASTER, true>(t, begin, steps, k, r);
+    else update_eight<WT, GT, MASTER, false>(t, begin, steps, k, r);
 }
 
-// A block finds its tensor in the list and takes CHUNK elements of it. Tensors with 8-bit moments are launched apart from those with float ones, whose kernel needs fewer registers.
+// A block finds its tensor in the list and takes b.steps steps of it. Tensors with 8-bit moments are launched apart from those with float ones, whose kernel needs fewer registers.
 template <bool EIGHT>
-__global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) adamw_kernel(const __grid_constant__ Batch b, Constants k, moe_adamw_rates given, const moe_adamw_rates *read) {
+__global__ void __launch_bounds__(THREADS, EIGHT ? EIGHT_BLOCKS : 3) adamw_kernel(const __grid_constant__ Batch b, Constants k, moe_adamw_rates given, const moe_adamw_rates *read) {
     wait_previous_kernel();
     const moe_adamw_rates r = read ? *read : given;
     int32_t lo = 0, hi = b.n;
@@ -334,13 +341,14 @@ __global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) adamw_kernel(const __g
     const Entry &t = b.t[lo];
     const int64_t chunk = (int32_t)blockIdx.x - b.chunks_before[lo];
     if constexpr (EIGHT) {
+        const int64_t begin = chunk * b.steps * STEP;
         switch (t.kind) {
-            case 0: update_eight<float, float, false>(t, chunk, k, r); break;
-            case 1: update_eight<bf16, float, false>(t, chunk, k, r); break;
-            case 2: update_eight<float, bf16, false>(t, chunk, k, r); break;
-            case 3: update_eight<bf16, bf16, false>(t, chunk, k, r); break;
-            case 5: update_eight<bf16, float, true>(t, chunk, k, r); break;
-            case 7: update_eight<bf16, bf16, true>(t, chunk, k, r); break;
+            case 0: update_eight<float, float, false>(t, begin, b.steps, k, r); break;
+            case 1: update_eight<bf16, float, false>(t, begin, b.steps, k, r); break;
+            case 2: update_eight<float, bf16, false>(t, begin, b.steps, k, r); break;
+            case 3: update_eight<bf16, bf16, false>(t, begin, b.steps, k, r); break;
+            case 5: update_eight<bf16, float, true>(t, begin, b.steps, k, r); break;
+            case 7: update_eight<bf16, bf16, true>(t, begin, b.steps, k, r); break;
         }
     } else {
         switch (t.kind) {
@@ -385,13 +393,17 @@ int32_t launch_adamw(const moe_adamw_tensor *tensors, int32_t count, const moe_a
         b.n = 0;
         return MOE_OK;
     };
+    int64_t all = 0;  // elements with 8-bit moments
+    for (int32_t i = 0; i < count; ++i) all = imin(all + (tensors[i].moment_bits == 8 ? tensors[i].count : 0), (int64_t)1 << 41);
     for (Batch &b : lists) b.n = b.chunks_before[0] = 0;
+    lists[0].steps = FLOAT_STEPS;
+    lists[1].steps = (int32_t)imax(1, imin(MOST_STEPS, all / ((int64_t)4 * EIGHT_BLOCKS * tc_sm_count() * STEP)));  // four blocks for each that an SM holds, if there are as many
     for (int32_t i = 0; i < count; ++i) {
         const moe_adamw_tensor &t = tensors[i];
         if (t.count == 0) continue;
         const int eight = t.moment_bits == 8;
         Batch &b = lists[eight];
-        const int64_t chunks = cdiv(t.count, CHUNK);  // at most 2^27
+        const int64_t chunks = cdiv(t.count, b.steps * STEP);  // at most 2^27
         if (b.n == MAX_LIST || (b.n > 0 && b.chunks_before[b.n] + chunks > (1 << 30))) MOE_TRY(flush(eight));
         b.t[b.n] = {t.w, t.g, t.master, t.m, t.v, t.m_scale, t.v_scale, t.count, t.first, t.weight_decay,
                     (t.w_type == MOE_BF16 ? 1 : 0) | (t.g_type == MOE_BF16 ? 2 : 0) | (t.master ? 4 : 0)};
