@@ -27,7 +27,8 @@ namespace moe {
 namespace {
 
 constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
-constexpr int TILE_K = 64, TILE_BYTES = TILE_K * 128, RING = 3;
+constexpr int TILE_K = 64, TILE_BYTES = TILE_K * 128;
+constexpr int WARP_BYTES = 3 * TILE_BYTES;  // shared memory of a warp: bf16 a ring of three tiles, float of two and two tiles of its rows
 constexpr int MAX_ROWS = MOE_FEW_MAX_TOKENS * MOE_MAX_K;
 constexpr int READY_STEP = 32;  // a line for a segment's count, so that those who wait for one do not hold up another's
 constexpr int SEG_ROWS = 16, NT = SEG_ROWS / 8;  // rows of a task: an expert with more is several segments, whose weights are read again, from L2. (32: the few experts with that many kept a call waiting)
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(256) few_logits_kernel(const T *__restrict__ x
 
 // ------------------------------------------------------------------------------------------ experts
 struct FewShared {
-    uint64_t full[FEW_WARPS][RING];
+    uint64_t full[FEW_WARPS][3];
     int32_t abort, segments, scan[FEW_WARPS];
     float gate[MAX_ROWS];                                   // of a slot
     int16_t rows[MAX_ROWS];                                 // slots by expert
@@ -291,10 +292,10 @@ struct FewTables {
     uint2 tokens[MOE_MAX_EXPERTS];
     int16_t start[MOE_MAX_EXPERTS];
 };
-static_assert(sizeof(FewTables) <= FEW_WARPS * RING * TILE_BYTES, "they fit");
-static_assert(RING + 2 <= 8, "tasks between the two");
+static_assert(sizeof(FewTables) <= FEW_WARPS * WARP_BYTES, "they fit");
+static_assert(WARP_BYTES / TILE_BYTES + 2 <= 8, "tasks between the two");
 static_assert(MOE_FEW_MAX_TOKENS <= 64, "a bit for a token");
-constexpr int FEW_SMEM = FEW_WARPS * RING * TILE_BYTES + 1024 + (int)sizeof(FewShared);
+constexpr int FEW_SMEM = FEW_WARPS * WARP_BYTES + 1024 + (int)sizeof(FewShared);
 
 __device__ __forceinline__ int32_t load_relaxed(const int32_t *p) {
     int32_t v;
@@ -424,6 +425,8 @@ struct Stream {
 template <typename T> struct Worker {
     static constexpr int COLS = 128 / (int)sizeof(T);
     static constexpr bool BF16 = sizeof(T) == 2;
+    static constexpr int RING = BF16 ? 3 : 2;
+    static_assert(SEG_ROWS * TILE_K * 4 * 2 == TILE_BYTES, "two tiles of rows in the place of one of weights");
     const Few &a;
     FewShared &S;
     const CUtensorMap *w1, *w2;
@@ -433,7 +436,7 @@ template <typename T> struct Worker {
 
     __device__ __forceinline__ Worker(const Few &a_, FewShared &S_, const CUtensorMap *w1_, const CUtensorMap *w2_, uint32_t ring, int32_t first, int warp_, int lane_)
         : a(a_), S(S_), w1(w1_), w2(w2_), warp(warp_), lane(lane_), segments(S_.segments), total(S_.segments * (a_.cols1 * a_.pieces1 + a_.cols2 * a_.pieces2)) {
-        s.ring = ring + warp * RING * TILE_BYTES;
+        s.ring = ring + warp * WARP_BYTES;
         s.bars = smem_u32(&S.full[warp][0]);
         s.flying = s.ask_slot = s.use_slot = s.phase = s.tasks = s.left = 0;
         s.number = 0;
@@ -503,6 +506,7 @@ template <typename T> struct Worker {
             const unsigned long long t0 = global_ns();
             while (!mbar_try_wait(s.bars + s.use_slot * 8, s.phase) && global_ns() - t0 < WAIT_LIMIT_NS) {}
         }
+        copies_wait<0>();
     }
     __device__ bool wait_ready(int32_t segment) {
         bool ok = true;
@@ -746,37 +750,52 @@ template <typename T> struct Worker {
         return true;
     }
 
-    // Float: a lane has four columns and every fourth run of four k
+    // Float: a lane has four columns and every fourth run of four k. The rows' values are copied a tile ahead (loaded where they are used, each load was waited for: 117 us for
+    // 15 tokens of 13 experts of 1288 x 1696, of k = 4)
     __device__ __forceinline__ bool run_f32(const Task &t, const int16_t *rows, int32_t m, int32_t expert) {
         const int cg = lane & 7, ph = lane >> 3;
         const int32_t width = t.second ? a.h : a.d;
+        const float *x = t.second ? a.hid : static_cast<const float *>(a.x);
+        char *const mine = static_cast<char *>(__cvta_shared_to_generic(s.ring));
+        float *const xs = reinterpret_cast<float *>(mine + RING * TILE_BYTES);  // [2][SEG_ROWS][TILE_K]
+        auto copy = [&](int32_t i) {
+            if (i < t.tiles) {
+                const int32_t k = t.k0 + i * TILE_K + (lane & 15) * 4;
+#pragma unroll 1
+                for (int q = lane >> 4; q < m; q += 2) {
+                    const int32_t p = rows[q], row = t.second ? p : token_of(p);
+                    copy16(xs + (i % 2 * SEG_ROWS + q) * TILE_K + (lane & 15) * 4, x + (k < width ? (int64_t)row * width + k : 0), k < width);
+                }
+            }
+            copies_commit();
+        };
         float acc[NT * 8][4];
 #pragma unroll
         for (int q = 0; q < NT * 8; ++q)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
+        copy(0);
         for (int32_t i = 0; i < t.tiles; ++i) {
-            if (!arrived()) return false;
-            const char *at = static_cast<const char *>(__cvta_shared_to_generic(tile()));
+            copy(i + 1);
+            copies_wait<1>();
+            if (!arrived()) return false;  // and all lanes' copies
+            const char *at = mine + s.use_slot * TILE_BYTES;
 #pragma unroll 1
             for (int j = 0; j < TILE_K / 16; ++j) {
                 const int kk = 16 * j + 4 * ph;
-                const int32_t k = t.k0 + i * TILE_K + kk;
+                const float *from = xs + i % 2 * (SEG_ROWS * TILE_K) + kk;
                 float4 w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = *reinterpret_cast<const float4 *>(at + (kk + e) * 128 + ((cg ^ ((kk + e) & 7)) << 4));
 #pragma unroll
                 for (int q = 0; q < NT * 8; ++q) {
                     if (q >= m) break;
-                    const int32_t p = rows[q];
-                    const float *x = t.second ? a.hid + (int64_t)p * a.h : static_cast<const float *>(a.x) + (int64_t)token_of(p) * a.d;
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if (k < width) v = t.second ? __ldcg(reinterpret_cast<const float4 *>(x + k)) : __ldg(reinterpret_cast<const float4 *>(x + k));
+                    const float4 v = *reinterpret_cast<const float4 *>(from + q * TILE_K);
                     const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        fma_two(acc[q][0], acc[q][1], f[e], w[e].x, w[e].y);
-                        fma_two(acc[q][2], acc[q][3], f[e], w[e].z, w[e].w);
+                    for (int c = 0; c < 4; ++c) {
+                        fma_two(acc[q][0], acc[q][1], f[c], w[c].x, w[c].y);
+                        fma_two(acc[q][2], acc[q][3], f[c], w[c].z, w[c].w);
                     }
                 }
             }
@@ -826,10 +845,10 @@ template <typename T>
 __global__ void __launch_bounds__(FEW_THREADS, 1) few_experts_kernel(const __grid_constant__ CUtensorMap w1, const __grid_constant__ CUtensorMap w2, const Few a) {
     extern __shared__ char few_raw[];
     char *base = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(few_raw) + 1023) & ~uintptr_t(1023));
-    FewShared &S = *reinterpret_cast<FewShared *>(base + FEW_WARPS * RING * TILE_BYTES);
+    FewShared &S = *reinterpret_cast<FewShared *>(base + FEW_WARPS * WARP_BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < FEW_WARPS * RING; ++i) mbar_init(smem_u32(&S.full[0][i]), 1);
+        for (int i = 0; i < FEW_WARPS * 3; ++i) mbar_init(smem_u32(&S.full[0][i]), 1);
         S.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -858,13 +877,23 @@ struct FewPlan {
     int32_t cols1, pieces1, piece_tiles1, cols2, pieces2, piece_tiles2;
     int64_t done1, done2, counters;
 };
-// Pieces of a contraction of `tiles` tiles for `cols` tiles of columns of `segments` experts: six tasks for every SM, so that their rings together keep memory busy, and none of
-// more than `most` tiles: of y 8 (1 / 24 / 64 tokens as above: 29.7 / 36.6 / 84.1 us; 4: 28.5 / 35.2 / 86.2; 16: 30.1 / 37.2 / 90.0)
-void pieces_of(int64_t segments, int64_t cols, int64_t tiles, int64_t most, int32_t *pieces, int32_t *piece_tiles) {
-    int64_t n = imin(tiles, cdiv(6 * 148, segments * cols));
-    n = imax(n, cdiv(tiles, most));
-    *piece_tiles = (int32_t)cdiv(tiles, n);
-    *pieces = (int32_t)cdiv(tiles, *piece_tiles);
+// Pieces of a contraction of `tiles` tiles for `cols` tiles of columns of `segments` experts: at most six tasks for every SM, whose rings together keep memory busy, and none of
+// more than `most` tiles. Among these the number for which a task's tiles and the sum of the pieces behind the last of them take least: `each` pieces of the sum are read at a time, by
+// turns of TURN tiles' time.
+#ifndef TURN
+#define TURN 1.0
+#endif
+void pieces_of(int64_t segments, int64_t cols, int64_t tiles, int64_t most, int64_t turns, int64_t each, int64_t sums, int32_t *pieces, int32_t *piece_tiles) {
+    const int64_t least = cdiv(tiles, most), highest = imax(least, imin(tiles, cdiv(6 * 148, segments * cols)));
+    int64_t best = 0;
+    for (int64_t n = highest; n >= least; --n) {
+        const int64_t of = cdiv(tiles, n), now = cdiv(tiles, of);
+        const int64_t cost = of + turns * cdiv(sums * now, each);
+        if (n < highest && cost >= best) continue;
+        best = cost;
+        *piece_tiles = (int32_t)of;
+        *pieces = (int32_t)now;
+    }
 }
 FewPlan plan_of(const moe_config &c) {
     FewPlan p;
@@ -874,8 +903,9 @@ FewPlan plan_of(const moe_config &c) {
     const int64_t segments = imax(1, imin(R, (int64_t)(used + 0.5)));
     p.cols1 = (int32_t)cdiv(c.h, width);
     p.cols2 = (int32_t)cdiv(c.d, width);
-    pieces_of(segments, p.cols1, cdiv(c.d, TILE_K), 16, &p.pieces1, &p.piece_tiles1);
-    pieces_of(segments, p.cols2, cdiv(c.h, TILE_K), 8, &p.pieces2, &p.piece_tiles2);
+    const int64_t turns = cdiv(imin(SEG_ROWS, cdiv(R, segments)), 2);  // of a segment's rows, two at a time
+    pieces_of(segments, p.cols1, cdiv(c.d, TILE_K), 16, turns, 8, 1, &p.pieces1, &p.piece_tiles1);
+    pieces_of(segments, p.cols2, cdiv(c.h, TILE_K), 8, turns, 16, c.k, &p.pieces2, &p.piece_tiles2);
     p.done1 = 64 + R * READY_STEP;  // behind the ticket and the segments' columns
     p.done2 = p.done1 + (p.pieces1 > 1 ? R * p.cols1 : 0);
     p.counters = p.done2 + (int64_t)c.T * p.cols2;
