@@ -55,10 +55,7 @@ template <int N> __device__ __forceinline__ void load_floats(const float *p, flo
 // A row belongs to a team of `warps` warps of the block. Sums over the team's threads; `sh` has a place per warp and sum, twice, so that one
 // barrier a row is enough: who writes the next row's sums does so on the other side, and the barrier of that row keeps it from coming round.
 constexpr int MAX_SUMS = 4;
-__device__ __forceinline__ void over_warps(float *mine, int warps, int team) {
-    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
-    (void)mine;
-}
+__device__ __forceinline__ void team_barrier(int warps, int team) { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory"); }
 __device__ __forceinline__ float team_sum(float s, int warps, float *sh, int &side) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
@@ -67,7 +64,7 @@ __device__ __forceinline__ float team_sum(float s, int warps, float *sh, int &si
     float *mine = sh + side * (32 * MAX_SUMS);
     side ^= 1;
     if ((threadIdx.x & 31) == 0) mine[warp] = s;
-    over_warps(mine, warps, team);
+    team_barrier(warps, team);
     s = 0.0f;
     for (int q = 0; q < warps; ++q) s += mine[team * warps + q];
     return s;
@@ -91,7 +88,7 @@ __device__ __forceinline__ void team_sums(float (&s)[4], int warps, float *sh, i
     float4 *mine = reinterpret_cast<float4 *>(sh + side * (32 * MAX_SUMS));
     side ^= 1;
     if ((lane & 7) == 0) reinterpret_cast<float *>(mine + warp)[lane >> 3] = t;
-    over_warps(nullptr, warps, team);
+    team_barrier(warps, team);
     float4 all = mine[team * warps];
     for (int q = 1; q < warps; ++q) {
         const float4 f = mine[team * warps + q];
@@ -221,7 +218,7 @@ Share share_of(int64_t T, int32_t d, int32_t act, int tensors, int64_t rows_per_
     s.group = rows_per_gate > 0 ? imin(rows_per_gate, imax(T, 1)) : imax(T, 1);
     s.groups = cdiv(T, s.group);
     s.rows = each * s.teams;
-    if (rows_per_gate > 0 && s.group <= 2 * each) {
+    if (rows_per_gate > 0 && s.group <= 3 * each) {
         s.per_team = imax(1, each / s.group);
         s.blocks = cdiv(s.groups, s.per_team * s.teams);
     } else {
@@ -231,10 +228,10 @@ Share share_of(int64_t T, int32_t d, int32_t act, int tensors, int64_t rows_per_
     return s;
 }
 // more blocks than any rows_per_gate gives: whole groups fill at least half of a block's rows, and beside the chunks of `rows` rows there is at most one
-// that is not full for every group, of more than 2 * each rows
+// that is not full for every group, of more than 3 * each rows
 int64_t most_blocks(int64_t T, int teams) {
     const int64_t each = team_rows(T, teams);
-    return 2 * cdiv(T, each * teams) + T / (2 * each) + 3;
+    return 2 * cdiv(T, each * teams) + T / (3 * each) + 3;
 }
 
 // GATE: 0 none, 1 a block's rows have one, 2 groups of a few rows (chunks 0)

@@ -82,7 +82,7 @@ def norm_out_bwd(dOut, dNext, out, y, w, gate, rows_per_gate, scale, w_next, rst
 
 
 def few(x, Wg, W1, b1, W2, b2, k, idx):
-    """The layer for the given routing idx [T, k]: y, gates, and the bounds on how far float arithmetic with hid rounded to the weights' type may be off."""
+    """The layer for the given routing idx [T, k]: y, gates, and the bounds on how far float arithmetic with hid in two terms of the weights' type may be off."""
     dt = W1.dtype
     f = lambda t: t.detach().double().cpu()
     xd, Wgd, idx = f(x), f(Wg), idx.cpu().long()
@@ -105,7 +105,7 @@ def few(x, Wg, W1, b1, W2, b2, k, idx):
             hid = pre.clamp(min=0.0)
             hid_slack = steps * (d + 16) * U * (xd[t].abs() @ W1d[e].abs() + b1d[e].abs())
             if dt == torch.bfloat16:
-                hid_slack = hid_slack + half_step(dt) * (hid + hid_slack)
+                hid_slack = hid_slack + 2.0 ** -17 * (hid + hid_slack)  # two bf16 terms: the first is off by 2^-9 of hid at most, the second by 2^-9 of that
             ys, terms = hid @ W2d[e] + b2d[e], hid @ W2d[e].abs() + b2d[e].abs()
             ys_slack = hid_slack @ W2d[e].abs() + steps * (h + 32) * U * (terms + hid_slack @ W2d[e].abs())
             y[t] += gates[t, s] * ys

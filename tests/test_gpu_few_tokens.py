@@ -58,6 +58,19 @@ def test_against_64_bits(T, d, h, n, k, act):
     check(B.make_config(T, d, h, n, k, act), layer(T, d, h, n, k, act))
 
 
+@pytest.mark.parametrize("T,d,h,n,k,act", [(64, 2048, 2056, 9, 8, "bf16"), (64, 1024, 4104, 8, 8, "f32"), (64, 8192, 200, 8, 8, "bf16")])
+def test_parts_of_y_of_several_slices(T, d, h, n, k, act):
+    """Parts of y for every 64 hidden units would be more than 64 MiB: a task has several of them."""
+    check(B.make_config(T, d, h, n, k, act), layer(T, d, h, n, k, act))
+
+
+# one to four tiles of either product, for every number of warps in a team; a single slice and many
+@pytest.mark.parametrize("T,d,h,n,k,act", [(1, 64, 40, 2, 1, "bf16"), (60, 64, 2048, 200, 4, "bf16"), (64, 128, 1024, 256, 8, "bf16"), (64, 72, 512, 512, 8, "bf16"), (20, 520, 64, 100, 2, "bf16"),
+                                           (64, 32, 1024, 128, 8, "f32"), (50, 100, 260, 300, 4, "f32"), (16, 36, 4096, 20, 2, "f32")])
+def test_teams_of_all_sizes(T, d, h, n, k, act):
+    check(B.make_config(T, d, h, n, k, act), layer(T, d, h, n, k, act))
+
+
 def test_every_number_of_rows():
     """T tokens that all pick the same expert, T = 1 .. 64: expert 1 has T rows, the other none."""
     d, h = 64, 72
