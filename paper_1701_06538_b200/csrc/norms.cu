@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, int wa
 // group: `chunks`); with groups of a few rows a team has whole groups and writes their gate's gradient itself (chunks 0).
 struct Share {
     int warps, teams, V, ring;  // ring: rows that a warp holds in shared memory (0: a row of several warps, in registers)
-    int64_t group, groups, chunks, rows, per_team, blocks;  // per_team: groups a team takes (chunks == 0)
+    int64_t group, groups, chunks, rows, per_team, blocks, most;  // per_team: groups a team takes (chunks == 0); most: blocks that the workspace has room for
 };
 constexpr int TEAM_ROWS = 4;  // 8192 x 512, main and sums: 10.3 us; 1, 2 and 3 rows 14.2, 14.5 and 11.9
 // rows of a team: blocks for two waves, of one block an SM where blocks are large (131072 x 1024: one wave 293 us, two 295, three 298, six 322) and of three where not
@@ -211,27 +211,52 @@ void grad_team_of(int32_t d, int32_t act, int tensors, int *warps, int *teams, i
     *warps = w;
     *teams = w >= 8 ? 1 : 8 / w;
 }
-Share share_of(int64_t T, int32_t d, int32_t act, int tensors, int64_t rows_per_gate) {
-    Share s = {};
-    grad_team_of(d, act, tensors, &s.warps, &s.teams, &s.V, &s.ring);
-    const int64_t each = team_rows(T, s.teams);
-    s.group = rows_per_gate > 0 ? imin(rows_per_gate, imax(T, 1)) : imax(T, 1);
-    s.groups = cdiv(T, s.group);
-    s.rows = each * s.teams;
-    if (rows_per_gate > 0 && s.group <= 3 * each) {
-        s.per_team = imax(1, each / s.group);
-        s.blocks = cdiv(s.groups, s.per_team * s.teams);
-    } else {
-        s.chunks = cdiv(s.group, s.rows);
-        s.blocks = s.groups * s.chunks;
-    }
-    return s;
-}
-// more blocks than any rows_per_gate gives: whole groups fill at least half of a block's rows, and beside the chunks of `rows` rows there is at most one
+// more blocks than share_of() takes: whole groups fill at least half of a block's rows, and beside the chunks of `rows` rows there is at most one
 // that is not full for every group, of more than 3 * each rows
 int64_t most_blocks(int64_t T, int teams) {
     const int64_t each = team_rows(T, teams);
     return 2 * cdiv(T, each * teams) + T / (3 * each) + 3;
+}
+// Blocks all have the same work and run in waves of as many as the SMs hold (two each where three have room: the third gains less than its start costs); each costs START rows' time
+// before and behind its rows. Of the shares of one wave to sixteen, and of whole groups to three quarters of the teams (five warps an SM: 482 us), the one that takes least: 131072 x 1024 with a gate for every 64
+// rows 520 us where groups stayed whole and 1.2 waves of blocks had them, with one for every 512 373 in chunks of 444 and 68 rows.
+constexpr int64_t START = 16;
+Share share_of(int64_t T, int32_t d, int32_t act, int tensors, int64_t rows_per_gate) {
+    Share chunks = {}, whole = {};
+    grad_team_of(d, act, tensors, &chunks.warps, &chunks.teams, &chunks.V, &chunks.ring);
+    grad_team_of(d, act, tensors + 1, &whole.warps, &whole.teams, &whole.V, &whole.ring);  // their gates go through the ring too
+    chunks.most = most_blocks(T, chunks.teams);
+    whole.most = most_blocks(T, whole.teams);
+    chunks.group = whole.group = rows_per_gate > 0 ? imin(rows_per_gate, imax(T, 1)) : imax(T, 1);
+    chunks.groups = whole.groups = cdiv(T, chunks.group);
+    const int64_t at_once = 148 * (chunks.teams > 8 ? 1 : 2), whole_at_once = 148 * (whole.teams > 8 ? 1 : 2);
+    const int teams = whole.teams;
+    int64_t best = INT64_MAX, best_whole = INT64_MAX;
+    for (int64_t waves = 1; waves <= 16; ++waves) {
+        Share s = chunks;
+        const int64_t rows = cdiv(s.group, imax(1, waves * at_once / imax(1, s.groups)));
+        s.rows = imin(s.group, imax(cdiv(rows, s.teams), TEAM_ROWS) * s.teams);
+        s.chunks = cdiv(s.group, s.rows);
+        s.blocks = s.groups * s.chunks;
+        const int64_t cost = cdiv(s.blocks, at_once) * (s.rows + START);
+        if (cost < best && s.blocks <= s.most) {
+            best = cost;
+            chunks = s;
+        }
+        if (rows_per_gate <= 0) continue;
+        for (int t = teams; 4 * t >= 3 * teams; --t) {
+            Share u = whole;
+            u.teams = t;
+            u.per_team = imax(imax(1, TEAM_ROWS / u.group), cdiv(u.groups, waves * whole_at_once * t));
+            u.blocks = cdiv(u.groups, u.per_team * t);
+            const int64_t of = cdiv(u.blocks, whole_at_once) * (t * u.per_team * u.group + START);
+            if (of < best_whole && u.blocks <= u.most) {
+                best_whole = of;
+                whole = u;
+            }
+        }
+    }
+    return rows_per_gate > 0 && best_whole <= best ? whole : chunks;
 }
 
 // GATE: 0 none, 1 a block's rows have one, 2 groups of a few rows (chunks 0)
@@ -452,24 +477,24 @@ __global__ void __maxnreg__(V == 1 ? 80 : 128) norm_grads_kernel(const NormGradA
 template <typename T, int V, bool Y, bool NEXT, int GATE>
 __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, const Share s, float *part_w, float *part_next, float *part_gate) {
     wait_previous_kernel();
-    constexpr int N = Vec<T>::N, P = N / 2, TENSORS = (Y ? 2 : 1) + (NEXT ? 2 : 0);
+    constexpr int N = Vec<T>::N, P = N / 2, TENSORS = (Y ? 2 : 1) + (NEXT ? 2 : 0), HELD = TENSORS + (GATE == 2 ? 1 : 0);  // HELD: of a row in the ring; GATE 2: its gate is the last
     extern __shared__ __align__(16) char norm_shared[];
     const int32_t d = a.d, pieces = d / N;
     float *gw = reinterpret_cast<float *>(norm_shared), *wn = gw + (Y ? d : 0);
-    uint4 *ring = reinterpret_cast<uint4 *>(wn + (NEXT ? d : 0));  // [warp][row][tensor][pieces]
+    uint4 *ring = reinterpret_cast<uint4 *>(wn + (NEXT ? d : 0));  // [warp][row][HELD][pieces]
     float *columns = reinterpret_cast<float *>(ring);             // afterwards: [warp][d]
     const int team = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint4 *mine = ring + (int64_t)team * RING_ROWS * TENSORS * pieces;
+    uint4 *mine = ring + (int64_t)team * RING_ROWS * HELD * pieces;
     const float by = 1.0f / (float)d;
     const int64_t block_group = GATE == 2 ? 0 : blockIdx.x / s.chunks;
     // a row's pieces of this lane, to place `at` of the ring; its factors go with it
-    auto ask = [&](int64_t row, int64_t end, int at) {
+    auto ask = [&](int64_t row, int64_t end, int at, int64_t gate_row) {
         if (row < end)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int32_t q = lane + 32 * v;
                 if (q >= pieces) break;
-                uint4 *to = mine + at * TENSORS * pieces + q;
+                uint4 *to = mine + at * HELD * pieces + q;
                 const int64_t from = row * d + (int64_t)q * N;
                 if (a.dOut) copy16(to, static_cast<const T *>(a.dOut) + from);
                 else zero16(to);
@@ -478,14 +503,15 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
                     copy16(to + (Y ? 2 : 1) * pieces, static_cast<const T *>(a.dNext) + from);
                     copy16(to + (Y ? 3 : 2) * pieces, static_cast<const T *>(a.out) + from);
                 }
+                if (GATE == 2) copy16(to + TENSORS * pieces, static_cast<const T *>(a.gate) + gate_row * d + (int64_t)q * N);
             }
         copies_commit();
     };
     // the block's rows of this warp, or (GATE 2) its groups; the first row is on its way before everything else
     const int64_t first_group = ((int64_t)blockIdx.x * s.teams + team) * s.per_team;
     const int64_t first = GATE == 2 ? first_group * s.group : block_group * s.group + (blockIdx.x % s.chunks) * s.rows + team;
-    const int64_t last = GATE == 2 ? min((first_group + 1) * s.group, a.T) : min(min(first - team + s.rows, (block_group + 1) * s.group), a.T);
-    ask(first, last, 0);
+    const int64_t last = GATE == 2 ? min((first_group + s.per_team) * s.group, a.T) : min(min(first - team + s.rows, (block_group + 1) * s.group), a.T);
+    ask(first, last, 0, first_group);
     for (int32_t q = threadIdx.x; q < pieces; q += blockDim.x) {
         float2 f[P];
         Vec<T> g;
@@ -511,8 +537,8 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
             if (GATE == 2) sum_w[GATE == 2 ? v : 0][i] = both(0.0f);
             if (NEXT) sum_next[NEXT ? v : 0][i] = both(0.0f);
         }
-    auto one_row = [&](int64_t row, int at, int64_t gate_row) {
-        const uint4 *held = mine + at * TENSORS * pieces;
+    auto one_row = [&](int64_t row, int at) {
+        const uint4 *held = mine + at * HELD * pieces;
         const float r = Y ? a.rstd[row] : 0.0f, r2 = NEXT ? a.rstd_next[row] : 0.0f;
         auto weights = [&](const float *from, int32_t q, float2 (&f)[P]) {
 #pragma unroll
@@ -525,7 +551,8 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
         auto gated = [&](int32_t q, float2 (&f)[P]) {
             weights(gw, q, f);
             if (GATE == 2) {
-                const Vec<T> g = load_vec<T>(a.gate, gate_row, d, q);
+                Vec<T> g;
+                g.raw = held[TENSORS * pieces + q];
 #pragma unroll
                 for (int i = 0; i < P; ++i) f[i] = mul2(f[i], g.get(2 * i));
             }
@@ -611,13 +638,35 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
             if (Y) store_vec<T>(a.dY, row, d, q, dy);
         }
     };
-    auto some_rows = [&](int64_t row, int64_t end, int64_t step, int64_t gate_row) {  // the first one has been asked for
+    // rows one behind the other, the next on its way; the first one has been asked for. GATE 2: from group to group, each with its end
+    auto some_rows = [&](int64_t row, int64_t end, int64_t step) {
         int at = 0;
+        int64_t g = first_group, group_end = GATE == 2 ? row + s.group : 0;
 #pragma unroll 1
         for (; row < end; row += step) {
-            ask(row + step, end, at ^ 1);
+            const bool ends = GATE == 2 && (row + 1 == group_end || row + 1 == end);
+            ask(row + step, end, at ^ 1, ends ? g + 1 : g);
             copies_wait<1>();
-            one_row(row, at, gate_row);
+            one_row(row, at);
+            if (ends) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {  // the group's gate gradient, and its part of dw
+                    const int32_t q = lane + 32 * v;
+                    if (q >= pieces) break;
+                    Vec<T> gv, dg;
+                    gv.raw = mine[at * HELD * pieces + TENSORS * pieces + q];
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        float2 &n = sum_n[Y ? v : 0][i], &w = sum_w[GATE == 2 ? v : 0][i];
+                        w = fma2(gv.get(2 * i), n, w);
+                        dg.set(2 * i, mul2(*reinterpret_cast<const float2 *>(gw + q * N + 2 * i), n));
+                        n = both(0.0f);
+                    }
+                    store_vec<T>(a.dgate, g, d, q, dg);
+                }
+                ++g;
+                group_end += s.group;
+            }
             at ^= 1;
         }
         copies_wait<0>();
@@ -652,30 +701,10 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
             *reinterpret_cast<float4 *>(part + (int64_t)blockIdx.x * d + (int64_t)q * N + 2 * i) = make_float4(total[i].x, total[i].y, total[i + 1].x, total[i + 1].y);
     };
 
+    some_rows(first, last, GATE == 2 ? 1 : s.teams);
     if (GATE == 2) {
-#pragma unroll 1
-        for (int64_t g = first_group; g < min(first_group + s.per_team, s.groups); ++g) {
-            if (g > first_group) ask(g * s.group, a.T, 0);
-            some_rows(g * s.group, min((g + 1) * s.group, a.T), 1, g);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {  // the group's gate gradient, and its part of dw
-                const int32_t q = lane + 32 * v;
-                if (q >= pieces) break;
-                const Vec<T> gv = load_vec<T>(a.gate, g, d, q);
-                Vec<T> dg;
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    float2 &n = sum_n[Y ? v : 0][i], &w = sum_w[GATE == 2 ? v : 0][i];
-                    w = fma2(gv.get(2 * i), n, w);
-                    dg.set(2 * i, mul2(*reinterpret_cast<const float2 *>(gw + q * N + 2 * i), n));
-                    n = both(0.0f);
-                }
-                store_vec<T>(a.dgate, g, d, q, dg);
-            }
-        }
         block_sums(sum_w, [&](int32_t q, const float2 (&total)[P]) { put(part_w, q, total); });
     } else {
-        some_rows(first, last, s.teams, block_group);
         if (Y)
             block_sums(sum_n, [&](int32_t q, const float2 (&total)[P]) {
                 if (GATE == 0) {
@@ -701,13 +730,29 @@ __global__ void __launch_bounds__(384) norm_stream_kernel(const NormGradArgs a, 
 
 // The blocks' sums added up, 32 columns a block, RUNS runs of blocks side by side, eight loads of each in flight, in double and in a fixed order. Blocks of the grid: those of dw, of
 // dw_next, then of every gate that several blocks share.
-constexpr int RUNS = 32;
+constexpr int RUNS = 32, FEW_CHUNKS = 32;  // gates of few chunks: a block has 32 sums of one run
 template <typename T>
 __global__ void __launch_bounds__(RUNS * 32) norm_sums_kernel(const NormGradArgs a, const Share s, const float *part_w, const float *part_next, const float *part_gate) {
     wait_previous_kernel();
     __shared__ double sh[RUNS][32];
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
     const int32_t slabs = (a.d + 31) / 32;
+    const int64_t own = (a.y ? 1 : 0) + (a.dNext ? 1 : 0), gates_at = own * slabs;
+    if (s.chunks <= FEW_CHUNKS && blockIdx.x >= gates_at) {  // a warp has 32 columns of a gate
+        const int64_t number = (blockIdx.x - gates_at) * RUNS + run, g = number / slabs;
+        const int32_t at = (int32_t)(number % slabs) * 32 + lane;
+        if (g >= s.groups || at >= a.d) return;
+        double sum = 0.0;
+        for (int64_t b = 0; b < s.chunks; b += 8) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = b + i < s.chunks ? part_gate[(g * s.chunks + b + i) * a.d + at] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += f[i];
+        }
+        static_cast<T *>(a.dgate)[g * a.d + at] = from_f32<T>((float)(a.w[at] * sum));
+        return;
+    }
     const int64_t job = blockIdx.x / slabs;
     const int32_t col = (blockIdx.x % slabs) * 32 + lane;
     const float *part = nullptr;
@@ -716,7 +761,7 @@ __global__ void __launch_bounds__(RUNS * 32) norm_sums_kernel(const NormGradArgs
     if (a.y && job == 0) { part = part_w; to = a.dw; }
     else if (a.dNext && job == (a.y ? 1 : 0)) { part = part_next; to = a.dw_next; }
     else {
-        gate_row = job - (a.y ? 1 : 0) - (a.dNext ? 1 : 0);
+        gate_row = job - own;
         part = part_gate;
         from = gate_row * s.chunks;
         count = s.chunks;
@@ -754,14 +799,14 @@ template <typename T, int V> int32_t launch_rows(const NormArgs &a, int warps, i
 }
 
 template <typename T, int V> int32_t launch_grads(const NormGradArgs &a, const Share &s, cudaStream_t st) {
-    const int64_t most = most_blocks(a.T, s.teams) * a.d;
+    const int64_t most = s.most * a.d;
     float *part_w = a.ws, *part_next = part_w + most, *part_gate = part_next + most;
     if (s.blocks > 0) {
         const dim3 grid((unsigned)s.blocks), block(s.warps * 32 * s.teams);
         const bool few = a.gate && s.chunks == 0;
         const int tensors = (a.y ? 2 : 1) + (a.dNext ? 2 : 0);
         size_t shared = s.teams > 1 ? sizeof(float) * s.teams * a.d : 0;
-        if (s.ring) shared = sizeof(float) * a.d * ((a.y ? 1 : 0) + (a.dNext ? 1 : 0)) + (size_t)s.teams * RING_ROWS * tensors * a.d * sizeof(T);
+        if (s.ring) shared = sizeof(float) * a.d * ((a.y ? 1 : 0) + (a.dNext ? 1 : 0)) + (size_t)s.teams * RING_ROWS * (tensors + (few ? 1 : 0)) * a.d * sizeof(T);
         auto launch = [&](auto *kernel, PerDevice &allowed) -> int32_t {
             if (s.ring && !allow_shared(allowed, kernel, SHARED_ALLOWED)) return MOE_ERR_CUDA;
             launch_kernel(kernel, grid, block, shared, st, a, s, part_w, part_next, part_gate);
@@ -788,8 +833,8 @@ template <typename T, int V> int32_t launch_grads(const NormGradArgs &a, const S
 #undef MOE_NORM_GRADS
         MOE_LAUNCHED();
     }
-    const int64_t jobs = (a.y ? 1 : 0) + (a.dNext ? 1 : 0) + (a.gate && s.chunks > 1 ? s.groups : 0);
-    launch_kernel(norm_sums_kernel<T>, dim3((unsigned)(jobs * cdiv(a.d, 32))), dim3(RUNS * 32), 0, st, a, s, (const float *)part_w, (const float *)part_next, (const float *)part_gate);
+    const int64_t slabs = cdiv(a.d, 32), gates = a.gate && s.chunks > 1 ? s.groups * slabs : 0;
+    launch_kernel(norm_sums_kernel<T>, dim3((unsigned)(((a.y ? 1 : 0) + (a.dNext ? 1 : 0)) * slabs + (s.chunks <= FEW_CHUNKS ? cdiv(gates, RUNS) : gates))), dim3(RUNS * 32), 0, st, a, s, (const float *)part_w, (const float *)part_next, (const float *)part_gate);
     MOE_LAUNCHED();
     return MOE_OK;
 }
@@ -798,7 +843,7 @@ template <typename T, int V> int32_t launch_grads(const NormGradArgs &a, const S
 
 int64_t norm_grad_floats(int64_t T, int32_t d, int32_t act) {
     int64_t most = 0;
-    for (int tensors = 2; tensors <= 4; ++tensors) {
+    for (int tensors = 2; tensors <= 5; ++tensors) {
         int warps, teams, V, ring;
         grad_team_of(d, act, tensors, &warps, &teams, &V, &ring);
         most = imax(most, most_blocks(T, teams));
