@@ -179,7 +179,7 @@ struct Share {
     int64_t group, groups, chunks, rows, per_team, blocks, most;  // per_team: groups a team takes (chunks == 0); most: blocks that the workspace has room for
 };
 constexpr int TEAM_ROWS = 4;  // 8192 x 512, main and sums: 10.3 us; 1, 2 and 3 rows 14.2, 14.5 and 11.9
-// rows of a team: blocks for two waves, of one block an SM where blocks are large (131072 x 1024: one wave 293 us, two 295, three 298, six 322) and of three where not
+// rows of a team when blocks are two waves of one an SM (where blocks are large) or of three: what the workspace has room for goes by it
 int64_t team_rows(int64_t T, int teams) { return imax(TEAM_ROWS, cdiv(T, (int64_t)teams * 148 * (teams > 8 ? 2 : 6))); }
 // Forward: a warp has a row up to 32 vectors a lane, else several do
 void team_of(int32_t d, int32_t act, int *warps, int *teams, int *V) {
@@ -206,10 +206,8 @@ void grad_team_of(int32_t d, int32_t act, int tensors, int *warps, int *teams, i
     }
     *ring = 0;
     *V = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8;
-    int w = 1;
-    while (w * 32 * *V < pieces) w *= 2;
-    *warps = w;
-    *teams = w >= 8 ? 1 : 8 / w;
+    *warps = (int)cdiv(pieces, 32 * *V);
+    *teams = (int)imax(1, 8 / *warps);
 }
 // more blocks than share_of() takes: whole groups fill at least half of a block's rows, and beside the chunks of `rows` rows there is at most one
 // that is not full for every group, of more than 3 * each rows
@@ -218,8 +216,8 @@ int64_t most_blocks(int64_t T, int teams) {
     return 2 * cdiv(T, each * teams) + T / (3 * each) + 3;
 }
 // Blocks all have the same work and run in waves of as many as the SMs hold (two each where three have room: the third gains less than its start costs); each costs START rows' time
-// before and behind its rows. Of the shares of one wave to sixteen, and of whole groups to three quarters of the teams (five warps an SM: 482 us), the one that takes least: 131072 x 1024 with a gate for every 64
-// rows 520 us where groups stayed whole and 1.2 waves of blocks had them, with one for every 512 373 in chunks of 444 and 68 rows.
+// before and behind its rows. Of the shares of one wave to sixteen, and of whole groups to three quarters of the teams, the one that takes least. 131072 x 1024:
+// with a gate for 64 rows 342 us, 520 where 1.2 waves of blocks had them; for 512 rows 295, 373 in chunks of 444 and 68 rows; for 200 rows 300, 482 with five teams a block.
 constexpr int64_t START = 16;
 Share share_of(int64_t T, int32_t d, int32_t act, int tensors, int64_t rows_per_gate) {
     Share chunks = {}, whole = {};
@@ -261,7 +259,7 @@ Share share_of(int64_t T, int32_t d, int32_t act, int tensors, int64_t rows_per_
 
 // GATE: 0 none, 1 a block's rows have one, 2 groups of a few rows (chunks 0)
 template <typename T, int V, bool Y, bool NEXT, int GATE>
-__global__ void __maxnreg__(V == 1 ? 80 : 128) norm_grads_kernel(const NormGradArgs a, const Share s, float *part_w, float *part_next, float *part_gate) {
+__global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const Share s, float *part_w, float *part_next, float *part_gate) {
     wait_previous_kernel();
     constexpr int N = Vec<T>::N, P = N / 2;
     extern __shared__ float columns[];  // [teams][d], where a block has several teams
@@ -374,11 +372,21 @@ __global__ void __maxnreg__(V == 1 ? 80 : 128) norm_grads_kernel(const NormGradA
         }
     };
     auto some_rows = [&](int64_t row, int64_t end, int64_t step) {
+        // a vector a thread: the next row is on its way meanwhile (32768 x 2048: 150 us, 199 without; with two vectors a thread it is more than the registers hold: 8192 x 8192 190
+        // without, 290 with it)
+        Row now;
+        if (V == 1 && row < end) fetch(now, row);
 #pragma unroll 1
         for (; row < end; row += step) {
-            Row now;
-            fetch(now, row);
-            one_row(now, row);
+            if constexpr (V == 1) {
+                Row next = now;
+                if (row + step < end) fetch(next, row + step);
+                one_row(now, row);
+                now = next;
+            } else {
+                fetch(now, row);
+                one_row(now, row);
+            }
         }
     };
     // the block's sums of its teams' columns, in the order of the teams. done(vector of columns, its sums)
