@@ -461,7 +461,7 @@ int32_t moe_norm_workspace_bytes(const moe_config *cfg, size_t *host_bytes);
  * backward pass), in two launches (three with more than 256 experts): what moe_forward with noise 0 computes,
  *     logits = x.W_g by the fixed chain of moe_gate, topk_idx / gates as moe_gate chooses them,
  *     hid = relu(x.W1 + b1) (float; bf16 layers: two bf16 terms), y = sum_s gates_s * (hid_s.W2 + b2) in float, one rounding.
- * The routing is moe_gate's without its screen bit for bit. T larger or a hierarchical layer: MOE_ERR_UNSUPPORTED.
+ * The routing is moe_gate's without its screen bit for bit. T larger or a hierarchical layer: MOE_ERR_UNSUPPORTED. y may not overlap an input.
  * in : x [T,d] act, Wg [d,n], W1, b1, W2, b2 as in moe_forward
  * out: y [T,d] act; topk_idx [T,k], gates [T,k] (each may be NULL).   ws: moe_few_workspace_bytes, its own in every call that may
  * run at the same time. MOE_ERR_TIMEOUT in its status word: see moe_check_status.
@@ -472,7 +472,7 @@ int32_t moe_forward_few(const moe_config *cfg, const void *x, const float *Wg, c
                         const void *b2, void *y, int32_t *topk_idx, float *gates, void *ws, void *stream);
 
 /* ------------------------------------------------------------------------------------------
- * AdamW over a list of tensors in one pass (a launch for every 96 of them), moments in float or in 8 bits. For every element
+ * AdamW over a list of tensors in one pass, moments in float or in 8 bits (a launch for every 96 tensors of either kind). For every element
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2      (g times grad_scale)
  *     w = w - lr * (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay * w)
  * in float, one rounding to w's type. With `master` (float, only beside bf16 weights) the step is taken on the master and w is
@@ -482,7 +482,8 @@ int32_t moe_forward_few(const moe_config *cfg, const void *x, const float *Wg, c
  * and 16-31 (sqrt(v)) of mix((first + i) mod 2^32 ^ mix(seed + floor((first + i) / 2^32) * 0x9e3779b9)) of element i, mix being
  * x ^= x >> 16, x *= 0x7feb352d, x ^= x >> 15, x *= 0x846ca68b, x ^= x >> 16: give every step its own seed and the tensors of a
  * step ranges of `first` that do not overlap. v above 0 keeps a code above 0. An element that is no finite number is held as
- * NaN and leaves its block's scale to the others. Zeroed codes and scales are the state before the first step.
+ * NaN and leaves its block's scale to the others (so is the root of a v beyond float's range, of a gradient beyond 2^64 or so; the weight becomes NaN
+ * with it). Zeroed codes and scales are the state before the first step. eps is at least float's smallest normal number.
  * All pointers but host_tensors, host_params are device pointers, w, g, master, m, v on 32-byte boundaries. The list is read before the call
  * returns; tensors of a list may not overlap. rates: NULL, or a moe_adamw_rates in device memory that takes the place of lr, step, grad_scale and
  * seed when the kernels run, for recorded graphs.

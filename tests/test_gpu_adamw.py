@@ -242,3 +242,15 @@ def test_codes_stay_those_of_the_formulas_in_float(g):
         assert torch.equal(ts[0][q], want[q])
     for q in ("m", "v"):
         assert (ts[0][q].float() == want[q].float()).all()
+
+
+@pytest.mark.parametrize("count", [8000003, 30000100])
+def test_codes_of_blocks_of_several_steps(count):
+    ts = [tensor(count, "bf16", "bf16", bits=8, seed=6)]
+    want = copy(ts)[0]
+    run(ts, 3, 9)
+    in_float(want, 3, 9)
+    for q in ("m_scale", "v_scale"):
+        assert torch.equal(ts[0][q], want[q])
+    for q in ("m", "v"):
+        assert (ts[0][q].float() == want[q].float()).all()

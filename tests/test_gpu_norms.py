@@ -201,3 +201,20 @@ def test_no_rows():
     B.moe_norm_in(cfg, t["x"], t["w"], EPS, dX, r)
     B.moe_norm_in_bwd(cfg, t["dNext"], t["x"], t["w"], r, None, dX, dw, ws)
     assert (dX == 7.0).all() and not dw.any()
+
+
+# Shares of many rows: groups whole in a team (one or several, blocks of fewer teams), in a block, in chunks; several waves; rows of one and of several warps. A thread adds up to some 400
+# rows one by one: 600 u instead of 160
+@pytest.mark.parametrize("T,d,act,per", [(40000, 72, "bf16", 1), (40000, 72, "bf16", 5), (40000, 72, "bf16", 37), (40000, 72, "bf16", 64), (40000, 72, "bf16", 301), (40000, 72, "bf16", 5000),
+                                         (40000, 72, "bf16", 0), (20000, 512, "f32", 1), (20000, 512, "f32", 67), (20000, 1024, "bf16", 33), (20000, 1024, "bf16", 200), (20000, 1024, "bf16", 1000),
+                                         (6000, 1544, "bf16", 70), (6000, 1544, "bf16", 1), (6000, 1544, "bf16", 0), (3000, 2064, "f32", 13), (2000, 8200, "bf16", 40)])
+def test_shares_of_many_rows(T, d, act, per):
+    t, cfg = tensors(T, d, act, 5, -(-T // per) if per else 0), config(T, d, act)
+    f = forward(cfg, t, per, 0.7)
+    o = backward(cfg, t, f, per, 0.7)
+    want = R.norm_out_bwd(t["dOut"], t["dNext"], f[0], t["y"], t["w"], t["gate"], per, 0.7, t["w_next"], f[2], f[3])
+    for q, (value, terms) in want.items():
+        R.within(o[q], value, 600 * R.U * terms, q)
+    again = backward(cfg, t, f, per, 0.7)
+    for q in want:
+        assert torch.equal(o[q], again[q]), q
