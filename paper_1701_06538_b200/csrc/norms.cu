@@ -206,8 +206,8 @@ void grad_team_of(int32_t d, int32_t act, int tensors, int *warps, int *teams, i
     }
     *ring = 0;
     *V = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8;
-    *warps = (int)cdiv(pieces, 32 * *V);
-    *teams = (int)imax(1, 8 / *warps);
+    *warps = (int)cdiv(pieces, 32 * *V);  // at least five
+    *teams = 1;
 }
 // more blocks than share_of() takes: whole groups fill at least half of a block's rows, and beside the chunks of `rows` rows there is at most one
 // that is not full for every group, of more than 3 * each rows
@@ -262,14 +262,13 @@ template <typename T, int V, bool Y, bool NEXT, int GATE>
 __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const Share s, float *part_w, float *part_next, float *part_gate) {
     wait_previous_kernel();
     constexpr int N = Vec<T>::N, P = N / 2;
-    extern __shared__ float columns[];  // [teams][d], where a block has several teams
     __shared__ __align__(16) float sh[2 * 32 * MAX_SUMS];
     int side = 0;
-    const int threads = s.warps * 32, team = threadIdx.x / threads, lane = threadIdx.x % threads;
+    const int threads = s.warps * 32, lane = threadIdx.x;  // one team
     const int32_t pieces = a.d / N;
     const float by = 1.0f / (float)a.d;
     float2 sum_n[Y ? V : 1][P], sum_w[GATE == 2 ? V : 1][P], sum_next[NEXT ? V : 1][P];  // of dt n over the group's rows so far; of dt gate n; of dNext n2
-    float2 gw[Y ? V : 1][P], wn[NEXT ? V : 1][P];                                           // gate times w of the group; w_next
+    float2 gw[Y ? V : 1][P], wn[NEXT ? V : 1][P];                                           // gate times w of the group (GATE 2: w); w_next
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int32_t q = lane + v * threads;
@@ -280,11 +279,11 @@ __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const S
             if constexpr (NEXT) sum_next[v][i] = both(0.0f);
         }
         if (q >= pieces) continue;
-        if constexpr (Y && GATE == 0) load_floats(a.w + (int64_t)q * N, gw[v]);
+        if constexpr (Y && GATE != 1) load_floats(a.w + (int64_t)q * N, gw[v]);
         if constexpr (NEXT) load_floats(a.w_next + (int64_t)q * N, wn[v]);
     }
     auto begin_group = [&](int64_t gate_row) {
-        if (GATE > 0)
+        if (GATE == 1)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int32_t q = lane + v * threads;
@@ -295,8 +294,8 @@ __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const S
                 for (int i = 0; i < P; ++i) gw[v][i] = mul2(gw[v][i], g.get(2 * i));
             }
     };
-    struct Row { Vec<T> dout[V], dnext[NEXT ? V : 1], out[NEXT ? V : 1], y[Y ? V : 1]; float r, r2; };
-    auto fetch = [&](Row &f, int64_t row) {
+    struct Row { Vec<T> dout[V], dnext[NEXT ? V : 1], out[NEXT ? V : 1], y[Y ? V : 1], gate[GATE == 2 ? V : 1]; float r, r2; };
+    auto fetch = [&](Row &f, int64_t row, int64_t gate_row) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
@@ -308,11 +307,17 @@ __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const S
                 f.out[v] = load_vec<T>(a.out, row, a.d, q);
             }
             if constexpr (Y) f.y[v] = load_vec<T>(a.y, row, a.d, q);
+            if constexpr (GATE == 2) f.gate[v] = load_vec<T>(a.gate, gate_row, a.d, q);
         }
         if constexpr (Y) f.r = a.rstd[row];
         if constexpr (NEXT) f.r2 = a.rstd_next[row];
     };
     auto one_row = [&](const Row &f, int64_t row) {
+        auto gated = [&](int v, int i) {
+            float2 w = gw[Y ? v : 0][i];
+            if constexpr (GATE == 2) w = mul2(w, f.gate[v].get(2 * i));
+            return w;
+        };
         // c2 = mean(dn2 n2) decides dt, and c1 = mean(dt b) with b = gate w n the rest. Both are sums of one look at the row, since c1 is linear in dt:
         // mean(dOut b) + r2 (mean(dn2 b) - c2 mean(n2 b))
         float2 s0 = both(0.0f), s1 = s0, s2 = s0, s3 = s0;
@@ -323,7 +328,7 @@ __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const S
             for (int i = 0; i < P; ++i) {
                 float2 b;
                 if constexpr (Y) {
-                    b = mul2(mul2(f.y[v].get(2 * i), both(f.r)), gw[v][i]);
+                    b = mul2(mul2(f.y[v].get(2 * i), both(f.r)), gated(v, i));
                     s1 = fma2(f.dout[v].get(2 * i), b, s1);
                 }
                 if constexpr (NEXT) {
@@ -363,7 +368,7 @@ __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const S
                 dx.set(2 * i, mul2(both(a.residual_scale), dt));
                 if constexpr (Y) {
                     const float2 n = mul2(f.y[v].get(2 * i), both(f.r));
-                    dy.set(2 * i, mul2(both(f.r), fma2(n, both(-c1), mul2(dt, gw[v][i]))));
+                    dy.set(2 * i, mul2(both(f.r), fma2(n, both(-c1), mul2(dt, gated(v, i)))));
                     sum_n[v][i] = fma2(dt, n, sum_n[v][i]);
                 }
             }
@@ -371,54 +376,51 @@ __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const S
             if constexpr (Y) store_vec<T>(a.dY, row, a.d, q, dy);
         }
     };
-    auto some_rows = [&](int64_t row, int64_t end, int64_t step) {
-        // a vector a thread: the next row is on its way meanwhile (32768 x 2048: 150 us, 199 without; with two vectors a thread it is more than the registers hold: 8192 x 8192 190
-        // without, 290 with it)
+    // rows one behind the other; GATE 2: from group to group, each with its end. With a vector a thread the next row is on its way meanwhile (32768 x 2048: 150 us, 199 without; with two
+    // it is more than the registers hold: 8192 x 8192 190 without, 290 with it)
+    auto some_rows = [&](int64_t row, int64_t end, int64_t g) {
+        int64_t group_end = row + s.group;
         Row now;
-        if (V == 1 && row < end) fetch(now, row);
+        if (V == 1 && row < end) fetch(now, row, g);
 #pragma unroll 1
-        for (; row < end; row += step) {
+        for (; row < end; ++row) {
+            const bool ends = GATE == 2 && (row + 1 == group_end || row + 1 == end);
+            Row next;
             if constexpr (V == 1) {
-                Row next = now;
-                if (row + step < end) fetch(next, row + step);
-                one_row(now, row);
-                now = next;
+                next = now;
+                if (row + 1 < end) fetch(next, row + 1, ends ? g + 1 : g);
             } else {
-                fetch(now, row);
-                one_row(now, row);
+                fetch(now, row, g);
             }
+            one_row(now, row);
+            if (ends) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {  // the group's gate gradient, and its part of dw
+                    const int32_t q = lane + v * threads;
+                    if (q >= pieces) break;
+                    Vec<T> dg;
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        float2 &n = sum_n[Y ? v : 0][i], &w = sum_w[GATE == 2 ? v : 0][i];
+                        w = fma2(now.gate[GATE == 2 ? v : 0].get(2 * i), n, w);
+                        dg.set(2 * i, mul2(gw[Y ? v : 0][i], n));
+                        n = both(0.0f);
+                    }
+                    store_vec<T>(a.dgate, g, a.d, q, dg);
+                }
+                ++g;
+                group_end += s.group;
+            }
+            if constexpr (V == 1) now = next;
         }
     };
-    // the block's sums of its teams' columns, in the order of the teams. done(vector of columns, its sums)
+    // done(vector of columns, their sums)
     auto block_sums = [&](auto &mine, auto done) {
-        if (s.teams > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int32_t q = lane + v * threads;
-                if (q >= pieces) break;
-#pragma unroll
-                for (int i = 0; i < P; i += 2)
-                    *reinterpret_cast<float4 *>(columns + (int64_t)team * a.d + (int64_t)q * N + 2 * i) = make_float4(mine[v][i].x, mine[v][i].y, mine[v][i + 1].x, mine[v][i + 1].y);
-            }
-            __syncthreads();
-            if (team > 0) return;
-        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
             if (q >= pieces) break;
-            float2 total[P];
-#pragma unroll
-            for (int i = 0; i < P; ++i) total[i] = mine[v][i];
-#pragma unroll 1
-            for (int t = 1; t < s.teams; ++t)
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const float2 f = *reinterpret_cast<const float2 *>(columns + (int64_t)t * a.d + (int64_t)q * N + 2 * i);
-                    total[i] = make_float2(total[i].x + f.x, total[i].y + f.y);
-                }
-            done(q, total);
+            done(q, mine[v]);
         }
     };
     auto to_part = [&](float *part) {
@@ -430,33 +432,13 @@ __global__ void __maxnreg__(128) norm_grads_kernel(const NormGradArgs a, const S
     };
 
     if constexpr (GATE == 2) {
-        const int64_t first = ((int64_t)blockIdx.x * s.teams + team) * s.per_team;
-#pragma unroll 1
-        for (int64_t g = first; g < min(first + s.per_team, s.groups); ++g) {
-            begin_group(g);
-            some_rows(g * s.group, min((g + 1) * s.group, a.T), 1);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {  // the group's gate gradient, and its part of dw
-                const int32_t q = lane + v * threads;
-                if (q >= pieces) break;
-                const Vec<T> gv = load_vec<T>(a.gate, g, a.d, q);
-                float2 w[P];
-                load_floats(a.w + (int64_t)q * N, w);
-                Vec<T> dg;
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    sum_w[v][i] = fma2(gv.get(2 * i), sum_n[v][i], sum_w[v][i]);
-                    dg.set(2 * i, mul2(w[i], sum_n[v][i]));
-                    sum_n[v][i] = both(0.0f);
-                }
-                store_vec<T>(a.dgate, g, a.d, q, dg);
-            }
-        }
+        const int64_t first = (int64_t)blockIdx.x * s.per_team;
+        some_rows(first * s.group, min((first + s.per_team) * s.group, a.T), first);
         block_sums(sum_w, to_part(part_w));
     } else {
         const int64_t g = blockIdx.x / s.chunks, from = g * s.group + (blockIdx.x % s.chunks) * s.rows;
         begin_group(g);
-        some_rows(from + team, min(min(from + s.rows, (g + 1) * s.group), a.T), s.teams);
+        some_rows(from, min(min(from + s.rows, (g + 1) * s.group), a.T), g);
         if constexpr (GATE == 1) {
             block_sums(sum_n, [&](int32_t q, const float2 (&total)[P]) {
                 const Vec<T> gv = load_vec<T>(a.gate, g, a.d, q);
@@ -813,7 +795,7 @@ template <typename T, int V> int32_t launch_grads(const NormGradArgs &a, const S
         const dim3 grid((unsigned)s.blocks), block(s.warps * 32 * s.teams);
         const bool few = a.gate && s.chunks == 0;
         const int tensors = (a.y ? 2 : 1) + (a.dNext ? 2 : 0);
-        size_t shared = s.teams > 1 ? sizeof(float) * s.teams * a.d : 0;
+        size_t shared = 0;
         if (s.ring) shared = sizeof(float) * a.d * ((a.y ? 1 : 0) + (a.dNext ? 1 : 0)) + (size_t)s.teams * RING_ROWS * (tensors + (few ? 1 : 0)) * a.d * sizeof(T);
         auto launch = [&](auto *kernel, PerDevice &allowed) -> int32_t {
             if (s.ring && !allow_shared(allowed, kernel, SHARED_ALLOWED)) return MOE_ERR_CUDA;
