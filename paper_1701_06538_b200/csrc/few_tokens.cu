@@ -526,14 +526,23 @@ template <typename T> struct Worker {
         for (int u = 0; u < NT; ++u) row[u] = static_cast<const bf16 *>(a.x) + (int64_t)token_of(rows[min(u * 8 + g, m - 1)]) * a.dw + 8 * c;  // lanes without a row: copies
         float acc[4][NT][4];
         clear(acc);
+        uint4 next[2][1][NT];
+        auto fetch = [&](int32_t i) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+                    if (i < a.tiles1 && (u == 0 || more)) next[j][0][u] = __ldg(reinterpret_cast<const uint4 *>(row[u] + i * TILE_K + 32 * j));
+        };
+        fetch(w);
 #pragma unroll 1
         for (int32_t i = w; i < a.tiles1; i += W) {
             uint4 x[2][1][NT];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int u = 0; u < NT; ++u)
-                    if (u == 0 || more) x[j][0][u] = __ldg(reinterpret_cast<const uint4 *>(row[u] + i * TILE_K + 32 * j));
+                for (int u = 0; u < NT; ++u) x[j][0][u] = next[j][0][u];
+            fetch(i + W);  // on its way during the products
             if (!arrived()) return;  // and all learn it at the next barrier
 #pragma unroll
             for (int j = 0; j < 2; ++j) multiply<1>(acc, at_hand() + j * (32 * 128), x[j], more);
