@@ -6,7 +6,7 @@
 //   few_select_kernel   picks them from logits in memory, where a cluster does not hold the gate (more than 256 experts)
 //   few_experts_kernel  one block per SM. Every block sorts the slots by expert; then its teams of warps draw tasks from a counter: an expert's rows (16 at most) and 64 hidden
 //                       units. The team makes hid of those units, which nobody else needs, and its part of y from them. (Tasks for hid and tasks for y, hid handed over through
-//                       memory: 27.8 us, not 21.6, for 1 token of 1024 x 4096, 35.4, not 25.7, for 24 tokens of 32 experts of 512 x 1024, of which a warp waited 3 to 7 us for hid
+//                       memory: 27.8 us, not 21.0, for 1 token of 1024 x 4096, 35.4, not 24.0, for 24 tokens of 32 experts of 512 x 1024, of which a warp waited 3 to 7 us for hid
 //                       and whoever came last summed up a token's y alone, for up to 7.) When all tasks are drawn, warps draw 16 columns of a token's y each, wait until its parts
 //                       are there and add them up in order: results do not depend on who does what, and whoever waits, waits for blocks that are running.
 //
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(256) few_select_kernel(const float *__restrict
 }
 
 // ------------------------------------------------------------------------------------------ logits
-constexpr int LOGIT_STEP = 128, LOGIT_STAGES = 6, LOGIT_TOKENS = 4, LOGIT_RUN = 16, LOGIT_BLOCKS = 8;
+constexpr int LOGIT_STEP = 128, LOGIT_STAGES = 5, LOGIT_TOKENS = 4, LOGIT_RUN = 16, LOGIT_BLOCKS = 8;
 // The chain over a step: while a feature's multiply-add waits for the one before it (four cycles), the values of LOGIT_RUN features later are loaded. Written out with volatile
 // instructions: left to itself the compiler loads next to the use, 13 cycles a feature.
 struct LogitRun {
@@ -698,11 +698,10 @@ template <typename T> struct Worker {
     __device__ __forceinline__ void make_hid(int32_t slice_, int32_t m, float bias) {
         const int tid = w * 32 + lane, col = tid % SLICE, givers = min(a.tiles1, W);
 #pragma unroll 1
-        for (int q = tid / SLICE; q < SEG_ROWS; q += W * 32 / SLICE) {
+        for (int q = tid / SLICE; q < m; q += W * 32 / SLICE) {  // places behind the last row keep what they had: products of theirs are dropped
             float v = bias;
-            if (q < m)
-                for (int o = col / COLS; o < givers; o += HALVES) v += red_of(team * W + o)[q * RED_STRIDE + col % COLS];  // float: a warp has sums of one half of the columns
-            v = v < 0.0f || q >= m || slice_ * SLICE + col >= a.h ? 0.0f : v;  // a NaN stays
+            for (int o = col / COLS; o < givers; o += HALVES) v += red_of(team * W + o)[q * RED_STRIDE + col % COLS];  // float: a warp has sums of one half of the columns
+            v = v < 0.0f || slice_ * SLICE + col >= a.h ? 0.0f : v;  // a NaN stays
             if constexpr (BF16) {
                 const bf16 hi = __float2bfloat16_rn(v);
                 const float f = __bfloat162float(hi);
@@ -719,7 +718,7 @@ template <typename T> struct Worker {
         const int32_t token = a.by_finals(number, piece), col = piece * 16 + (lane & 3) * 4, parts = a.k * a.units;
         const float *from = a.parts + (int64_t)token * parts * a.d + col;
         float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        constexpr int B = 8;
+        constexpr int B = 8;  // loads in flight (4, 16: 0.5 to 1 us more)
 #pragma unroll 1
         for (int32_t j0 = lane >> 2; j0 < parts; j0 += 8 * B) {
             float4 f[B];
