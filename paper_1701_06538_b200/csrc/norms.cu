@@ -98,76 +98,85 @@ __device__ __forceinline__ void team_sums(float (&s)[4], int warps, float *sh, i
 }
 
 // Y: the block's output goes through its norm and the gate onto x; NEXT: a norm of the result (without Y: of x). Arithmetic in pairs: element by element it was 31 instructions an element
-// and kept memory waiting, 28.2 us for 32768 x 512.
-template <typename T, int V, bool Y, bool NEXT, bool GATE>
+// and kept memory waiting, 28.2 us for 32768 x 512. AHEAD: a team has several rows and the next one on its way; else one.
+template <typename T, int V, bool Y, bool NEXT, bool GATE, bool AHEAD>
 __global__ void __launch_bounds__(512) norm_rows_kernel(const NormArgs a, int warps) {
     wait_previous_kernel();
     constexpr int N = Vec<T>::N, P = N / 2;
     __shared__ float sh[2 * 32 * MAX_SUMS];
     int side = 0;
     const int threads = warps * 32, teams = blockDim.x / threads, lane = threadIdx.x % threads;
-    const int64_t row = (int64_t)blockIdx.x * teams + threadIdx.x / threads;
-    if (row >= a.T) return;  // the whole team
+    const int64_t stride = (int64_t)gridDim.x * teams;
     const int32_t pieces = a.d / N;
     const float by = 1.0f / (float)a.d;
-    Vec<T> xv[V], yv[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int32_t q = lane + v * threads;
-        if (q >= pieces) break;
-        if constexpr (Y) yv[v] = load_vec<T>(a.y, row, a.d, q);
-        xv[v] = load_vec<T>(a.x, row, a.d, q);
-    }
-    float2 o[V][P];
-    float2 sum = both(0.0f);
-    if constexpr (Y) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (lane + v * threads < pieces)
-#pragma unroll
-                for (int i = 0; i < P; ++i) { const float2 f = yv[v].get(2 * i); sum = fma2(f, f, sum); }
-        const float r = 1.0f / sqrtf(team_sum(sum.x + sum.y, warps, sh, side) * by + a.eps);
-        if (lane == 0) a.rstd[row] = r;
-        const int64_t gate_row = GATE ? (int64_t)((uint32_t)row / (uint32_t)a.rows_per_gate) : 0;
-        sum = both(0.0f);
+    struct Row { Vec<T> x[V], y[Y ? V : 1]; };
+    auto fetch = [&](Row &f, int64_t row) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t q = lane + v * threads;
             if (q >= pieces) break;
-            float2 w[P];
-            load_floats(a.w + (int64_t)q * N, w);
-            Vec<T> g, res;
-            if constexpr (GATE) g = load_vec<T>(a.gate, gate_row, a.d, q);
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                float2 u = mul2(mul2(yv[v].get(2 * i), both(r)), w[i]);
-                if constexpr (GATE) u = mul2(u, g.get(2 * i));
-                o[v][i] = fma2(both(a.residual_scale), xv[v].get(2 * i), u);
-                sum = fma2(o[v][i], o[v][i], sum);
-                res.set(2 * i, o[v][i]);
-            }
-            store_vec<T>(a.out, row, a.d, q, res);
+            if constexpr (Y) f.y[v] = load_vec<T>(a.y, row, a.d, q);
+            f.x[v] = load_vec<T>(a.x, row, a.d, q);
         }
-    } else {
+    };
+    Row next;
+    int64_t row = (int64_t)blockIdx.x * teams + threadIdx.x / threads;
+    if (row < a.T) fetch(next, row);
+#pragma unroll 1
+    for (; row < a.T; row += AHEAD ? stride : a.T) {
+        const Row now = next;
+        if (AHEAD && row + stride < a.T) fetch(next, row + stride);
+        float2 o[V][P];
+        float2 sum = both(0.0f);
+        if constexpr (Y) {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (lane + v * threads < pieces)
+            for (int v = 0; v < V; ++v)
+                if (lane + v * threads < pieces)
 #pragma unroll
-                for (int i = 0; i < P; ++i) { o[v][i] = xv[v].get(2 * i); sum = fma2(o[v][i], o[v][i], sum); }
-    }
-    if constexpr (NEXT) {  // of what was not rounded yet
-        const float r = 1.0f / sqrtf(team_sum(sum.x + sum.y, warps, sh, side) * by + a.eps);
-        if (lane == 0 && a.rstd_next) a.rstd_next[row] = r;
+                    for (int i = 0; i < P; ++i) { const float2 f = now.y[v].get(2 * i); sum = fma2(f, f, sum); }
+            const float r = 1.0f / sqrtf(team_sum(sum.x + sum.y, warps, sh, side) * by + a.eps);
+            if (lane == 0) a.rstd[row] = r;
+            const int64_t gate_row = GATE ? (int64_t)((uint32_t)row / (uint32_t)a.rows_per_gate) : 0;
+            sum = both(0.0f);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int32_t q = lane + v * threads;
-            if (q >= pieces) break;
-            float2 w[P];
-            load_floats(a.w_next + (int64_t)q * N, w);
-            Vec<T> res;
+            for (int v = 0; v < V; ++v) {
+                const int32_t q = lane + v * threads;
+                if (q >= pieces) break;
+                float2 w[P];
+                load_floats(a.w + (int64_t)q * N, w);
+                Vec<T> g, res;
+                if constexpr (GATE) g = load_vec<T>(a.gate, gate_row, a.d, q);
 #pragma unroll
-            for (int i = 0; i < P; ++i) res.set(2 * i, mul2(mul2(o[v][i], both(r)), w[i]));
-            store_vec<T>(a.next, row, a.d, q, res);
+                for (int i = 0; i < P; ++i) {
+                    float2 u = mul2(mul2(now.y[v].get(2 * i), both(r)), w[i]);
+                    if constexpr (GATE) u = mul2(u, g.get(2 * i));
+                    o[v][i] = fma2(both(a.residual_scale), now.x[v].get(2 * i), u);
+                    sum = fma2(o[v][i], o[v][i], sum);
+                    res.set(2 * i, o[v][i]);
+                }
+                store_vec<T>(a.out, row, a.d, q, res);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (lane + v * threads < pieces)
+#pragma unroll
+                    for (int i = 0; i < P; ++i) { o[v][i] = now.x[v].get(2 * i); sum = fma2(o[v][i], o[v][i], sum); }
+        }
+        if constexpr (NEXT) {  // of what was not rounded yet
+            const float r = 1.0f / sqrtf(team_sum(sum.x + sum.y, warps, sh, side) * by + a.eps);
+            if (lane == 0 && a.rstd_next) a.rstd_next[row] = r;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int32_t q = lane + v * threads;
+                if (q >= pieces) break;
+                float2 w[P];
+                load_floats(a.w_next + (int64_t)q * N, w);
+                Vec<T> res;
+#pragma unroll
+                for (int i = 0; i < P; ++i) res.set(2 * i, mul2(mul2(o[v][i], both(r)), w[i]));
+                store_vec<T>(a.next, row, a.d, q, res);
+            }
         }
     }
 }
@@ -779,8 +788,22 @@ __global__ void __launch_bounds__(RUNS * 32) norm_sums_kernel(const NormGradArgs
 }
 
 template <typename T, int V> int32_t launch_rows(const NormArgs &a, int warps, int teams, cudaStream_t st) {
-    const dim3 grid((unsigned)cdiv(a.T, teams)), block(warps * 32 * teams);
-#define MOE_NORM_ROWS(Y, NEXT, GATE) launch_kernel(norm_rows_kernel<T, V, Y, NEXT, GATE>, grid, block, 0, st, a, warps)
+    // As many blocks as the SMs hold at once, 3 (bf16, norm and residual, two vectors a lane) or 4 an SM, for several rows each: 32768 x 512 with norm and next 23.4 us (4 an SM: 27.9),
+    // 131072 x 512, norm_in 43.3 (3: 45.5, 6: 48.6), 65536 x 256 23.7 (26.1, 27.8), float, 30000 x 320 29.4 (31.5, 32.7). Blocks of one row a team: 26.8, 55.0, 31.5 and 38.6; they stay for few
+    // rows and for rows of more than eight warps (8192 x 8192: 121, several rows each 131).
+    const int64_t at_once = 148 * (V == 2 && a.y && sizeof(T) == 2 ? 3 : 4), blocks = cdiv(a.T, teams);
+    const bool ahead = V <= 2 && warps <= 8 && blocks > at_once;
+    const dim3 grid((unsigned)(ahead ? at_once : blocks)), block(warps * 32 * teams);
+#define MOE_NORM_ROWS(Y, NEXT, GATE)                                                                                      \
+    do {                                                                                                                  \
+        if constexpr (V <= 2) {                                                                                           \
+            if (ahead) {                                                                                                  \
+                launch_kernel(norm_rows_kernel<T, V, Y, NEXT, GATE, true>, grid, block, 0, st, a, warps);                 \
+                break;                                                                                                    \
+            }                                                                                                             \
+        }                                                                                                                 \
+        launch_kernel(norm_rows_kernel<T, V, Y, NEXT, GATE, false>, grid, block, 0, st, a, warps);                        \
+    } while (0)
     if (a.y && a.next && a.gate) MOE_NORM_ROWS(true, true, true);
     else if (a.y && a.next) MOE_NORM_ROWS(true, true, false);
     else if (a.y && a.gate) MOE_NORM_ROWS(true, false, true);

@@ -218,3 +218,17 @@ def test_shares_of_many_rows(T, d, act, per):
     again = backward(cfg, t, f, per, 0.7)
     for q in want:
         assert torch.equal(o[q], again[q]), q
+
+
+@pytest.mark.parametrize("T,d,act", [(9001, 72, "bf16"), (7000, 512, "bf16"), (5003, 1024, "bf16"), (1201, 4096, "bf16"), (900, 2056, "bf16"), (9001, 320, "f32"), (1500, 2048, "f32"), (700, 8192, "bf16")])
+def test_several_rows_a_team(T, d, act):
+    cfg = config(T, d, act)
+    for per in (0, 1, 100):
+        test_norm_out(T, d, act, True, per)
+    test_norm_out(T, d, act, False, 7)
+    test_norm_in(T, d, act)
+    # rows behind the last are left
+    t = tensors(T, d, act)
+    big = torch.full((T + 3, d), 3.0, device="cuda", dtype=DT[act])
+    B.moe_norm_in(cfg, t["x"], t["w"], EPS, big[:T], None)
+    assert (big[T:] == 3.0).all()
