@@ -353,23 +353,41 @@ def _checked(name, status):
         raise MoeError(name, status)
 
 
+def _here():
+    """_p for a call whose tensors have to be where it runs: on the current device."""
+    device = torch.cuda.current_device()
+
+    def p(t):
+        if t is None:
+            return None
+        if t.get_device() != device:
+            raise ValueError("a tensor is not on the current device")
+        assert t.is_contiguous(), "device tensors must be contiguous CUDA tensors"
+        return t.data_ptr()
+    return p
+
+
 def moe_norm_in(cfg, x, w, eps, xn, rstd):
-    _checked("moe_norm_in", _bound("moe_norm_in", "cppfpp")(cfg, _p(x), _p(w), eps, _p(xn), _p(rstd), _stream()))
+    p = _here()
+    _checked("moe_norm_in", _bound("moe_norm_in", "cppfpp")(cfg, p(x), p(w), eps, p(xn), p(rstd), _stream()))
 
 
 def moe_norm_in_bwd(cfg, dxn, x, w, rstd, dres, dX, dw, ws):
-    _checked("moe_norm_in_bwd", _bound("moe_norm_in_bwd", "cpppppppp")(cfg, _p(dxn), _p(x), _p(w), _p(rstd), _p(dres), _p(dX), _p(dw), _p(ws), _stream()))
+    p = _here()
+    _checked("moe_norm_in_bwd", _bound("moe_norm_in_bwd", "cpppppppp")(cfg, p(dxn), p(x), p(w), p(rstd), p(dres), p(dX), p(dw), p(ws), _stream()))
 
 
 def moe_norm_out(cfg, x, y, w, gate, rows_per_gate, residual_scale, w_next, eps, out, next, rstd, rstd_next):
-    _checked("moe_norm_out", _bound("moe_norm_out", "cppppifpfpppp")(cfg, _p(x), _p(y), _p(w), _p(gate), rows_per_gate, residual_scale, _p(w_next), eps, _p(out),
-                                                                     _p(next), _p(rstd), _p(rstd_next), _stream()))
+    p = _here()
+    _checked("moe_norm_out", _bound("moe_norm_out", "cppppifpfpppp")(cfg, p(x), p(y), p(w), p(gate), rows_per_gate, residual_scale, p(w_next), eps, p(out),
+                                                                     p(next), p(rstd), p(rstd_next), _stream()))
 
 
 def moe_norm_out_bwd(cfg, dOut, dNext, out, y, w, gate, rows_per_gate, residual_scale, w_next, rstd, rstd_next, dX, dY, dw, dgate, dw_next,
                      ws):
-    _checked("moe_norm_out_bwd", _bound("moe_norm_out_bwd", "cppppppifppppppppp")(cfg, _p(dOut), _p(dNext), _p(out), _p(y), _p(w), _p(gate), rows_per_gate, residual_scale,
-                                                                                  _p(w_next), _p(rstd), _p(rstd_next), _p(dX), _p(dY), _p(dw), _p(dgate), _p(dw_next), _p(ws),
+    p = _here()
+    _checked("moe_norm_out_bwd", _bound("moe_norm_out_bwd", "cppppppifppppppppp")(cfg, p(dOut), p(dNext), p(out), p(y), p(w), p(gate), rows_per_gate, residual_scale,
+                                                                                  p(w_next), p(rstd), p(rstd_next), p(dX), p(dY), p(dw), p(dgate), p(dw_next), p(ws),
                                                                                   _stream()))
 
 
@@ -378,7 +396,8 @@ def moe_few_workspace_bytes(cfg) -> int:
 
 
 def moe_forward_few(cfg, x, Wg, W1, b1, W2, b2, y, topk_idx, gates, ws):
-    _checked("moe_forward_few", _bound("moe_forward_few", "cpppppppppp")(cfg, _p(x), _p(Wg), _p(W1), _p(b1), _p(W2), _p(b2), _p(y), _p(topk_idx), _p(gates), _p(ws),
+    p = _here()
+    _checked("moe_forward_few", _bound("moe_forward_few", "cpppppppppp")(cfg, p(x), p(Wg), p(W1), p(b1), p(W2), p(b2), p(y), p(topk_idx), p(gates), p(ws),
                                                                          _stream()))
 
 

@@ -236,3 +236,20 @@ def test_steps_that_train(bits):
         for q in a:
             if torch.is_tensor(a[q]):
                 assert torch.equal(a[q].view(torch.uint8), b[q].view(torch.uint8)), q
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    s, tr = Server(2, 64, 64, 4, 2, "bf16"), Trainer(8, 64, 48, 4, 2, "f32", 4)
+    t = torch.zeros(256, device="cuda")
+    opt = B.moe_adamw_list([dict(w=t, g=t.clone(), m=t.clone(), v=t.clone())])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)  # of tensors on device 0
+    w, o, c = s.blocks[0], s.o[0], s.cfg
+    g, q, tc = tr.g, tr.o, tr.cfg
+    for call in (lambda: B.moe_norm_in(c, s.x, w["w_in"], EPS, s.xn, s.r),
+                 lambda: B.moe_forward_few(c, s.xn, w["Wg"], w["W1"], w["b1"], w["W2"], w["b2"], o["y"], o["idx"], o["gates"], s.ws),
+                 lambda: B.moe_norm_out(c, s.x, o["y"], w["w"], None, 0, SCALE, None, EPS, o["out"], None, o["rstd"], None),
+                 lambda: B.moe_norm_out_bwd(tc, tr.t["dOut"], None, None, q["y"], tr.w["w"], None, 0, SCALE, None, q["rstd"], None, q["dX"], q["dY"], g["w"], None, None, tr.ws),
+                 lambda: B.moe_norm_in_bwd(tc, q["dxn"], tr.t["x"], tr.w["w_in"], q["r_in"], None, q["dX"], g["w_in"], tr.ws),
+                 lambda: B.moe_adamw(opt, 1e-3, 0.9, 0.999, 1e-8, 1)):
+        with pytest.raises(ValueError):
+            call()
