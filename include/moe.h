@@ -429,7 +429,7 @@ int32_t moe_layer_backward(const moe_config *cfg, const void *dOut, const void *
  * rstd, rstd_next [T] float: the factors rsqrt(mean + eps) for the backward pass.
  * Of cfg only T, d and act matter. d is at most MOE_NORM_MAX_D (MOE_ERR_UNSUPPORTED beyond). eps > 0, residual_scale finite.
  * y may come from any call that writes [T,d]: moe_forward, moe_forward_few, moe_combine, moe_combine_balanced.
- * xn may be x, out may be x or y, and next may be the one of them that out is not.
+ * xn may be x, out may be x or y, and next may be the one of them that out is not; next is not out, dX not dY.
  * ------------------------------------------------------------------------------------------ */
 #define MOE_NORM_MAX_D 16384
 

@@ -74,6 +74,7 @@ int32_t moe_norm_out(const moe_config *cfg, const void *x, const void *y, const 
     REQUIRE_PTRS(x, y, w, out, rstd);
     if (gate && (bad_ptr(gate) || rows_per_gate <= 0)) return MOE_ERR_INVALID_ARG;
     if (w_next) REQUIRE_PTRS(w_next, next, rstd_next);
+    if (w_next && next == out) return MOE_ERR_INVALID_ARG;
     if (!(eps > 0.0f) || bad_float(eps) || bad_float(residual_scale)) return MOE_ERR_INVALID_ARG;
     NormArgs a = {};
     a.T = cfg->T; a.d = cfg->d; a.act = cfg->act; a.x = x; a.y = y; a.gate = gate; a.w = w; a.w_next = w_next; a.rows_per_gate = rows_per_gate;
@@ -89,7 +90,7 @@ int32_t moe_norm_out_bwd(const moe_config *cfg, const void *dOut, const void *dN
     REQUIRE_PTRS(dOut, y, w, rstd, dX, dY, dw, ws);
     if (gate && (bad_ptr(gate) || bad_ptr(dgate) || rows_per_gate <= 0)) return MOE_ERR_INVALID_ARG;
     if (w_next) REQUIRE_PTRS(w_next, dNext, out, rstd_next, dw_next);
-    if (bad_float(residual_scale)) return MOE_ERR_INVALID_ARG;
+    if (bad_float(residual_scale) || dX == dY) return MOE_ERR_INVALID_ARG;
     NormGradArgs a = {};
     a.T = cfg->T; a.d = cfg->d; a.act = cfg->act; a.dOut = dOut; a.y = y; a.w = w; a.rstd = rstd; a.residual_scale = residual_scale;
     a.dX = dX; a.dY = dY; a.dw = dw;
@@ -110,7 +111,7 @@ int32_t moe_forward_few(const moe_config *cfg, const void *x, const float *Wg, c
                         const void *b2, void *y, int32_t *topk_idx, float *gates, void *ws, void *stream) {
     MOE_TRY(check_few(cfg));
     REQUIRE_PTRS(x, Wg, W1, b1, W2, b2, y, ws);
-    if ((topk_idx && bad_ptr(topk_idx)) || (gates && bad_ptr(gates))) return MOE_ERR_INVALID_ARG;
+    if ((topk_idx && bad_ptr(topk_idx)) || (gates && bad_ptr(gates)) || y == x) return MOE_ERR_INVALID_ARG;  // rows of x are read until the last of y are written
     return launch_few_tokens(*cfg, x, Wg, W1, b1, W2, b2, y, topk_idx, gates, ws, static_cast<cudaStream_t>(stream));
 }
 

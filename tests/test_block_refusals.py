@@ -110,3 +110,14 @@ def test_adamw_list_checks_its_tensors():
                dict(m=torch.zeros(8, dtype=torch.uint8), v=torch.zeros(8, dtype=torch.uint8))):
         with pytest.raises((ValueError, AssertionError)):
             B.moe_adamw_list([dict(t, **kw)])
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="made-up addresses")
+def test_outputs_in_one_place(lib):
+    """Distinct addresses but for two that may not be one."""
+    at = lambda i: ctypes.c_void_p(4096 * (i + 1))
+    c = ctypes.byref(cfg())
+    p = [at(i) for i in range(20)]
+    assert lib.moe_forward_few(c, p[0], *p[1:6], p[0], NULL, NULL, p[7], NULL) == INVALID                                      # y in the place of x
+    assert lib.moe_norm_out(c, p[0], p[1], p[2], NULL, 0, F(1.0), p[3], F(1e-6), p[4], p[4], p[5], p[6], NULL) == INVALID      # next in the place of out
+    assert lib.moe_norm_out_bwd(c, p[0], NULL, NULL, p[1], p[2], NULL, 0, F(1.0), NULL, p[3], NULL, p[4], p[4], p[5], NULL, NULL, p[6], NULL) == INVALID  # dX and dY
