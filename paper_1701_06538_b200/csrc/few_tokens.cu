@@ -182,6 +182,8 @@ __global__ void __launch_bounds__(256) few_logits_kernel(const T *__restrict__ x
     // The experts' blocks may come as soon as there is room for them: they set up barriers and tables meanwhile and wait for this launch's end before they read of it
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     wait_previous_kernel();
+    // The first block's shared memory may be written once it is known to run: all blocks say here that they do, and wait for the others behind the chain, where nobody waits any more
+    if constexpr (ROUTE) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     __shared__ float all[ROUTE ? LOGIT_TOKENS : 1][ROUTE ? LOGIT_BLOCKS * 32 : 1];
     __shared__ __align__(16) float xf[2][LOGIT_TOKENS][LOGIT_STEP];
     extern __shared__ __align__(16) char few_shared[];
@@ -255,6 +257,8 @@ __global__ void __launch_bounds__(256) few_logits_kernel(const T *__restrict__ x
         }
     }
     if constexpr (ROUTE) {
+        __syncwarp();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (warp < LOGIT_TOKENS) {
             const uint32_t to = peer_smem_addr(smem_u32(&all[warp][col0 + lane]), 0);
             asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(acc) : "memory");
