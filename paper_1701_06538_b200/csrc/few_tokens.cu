@@ -35,6 +35,8 @@ constexpr int SEG_ROWS = 16, NT = SEG_ROWS / 8;  // rows of a task: an expert wi
 
 // bf16 rows that the matrix instruction takes (x, hid) stand as it wants them (turned()), x in a copy whose width is rounded up to tiles with zeros behind the last column.
 // hid is kept in two bf16 terms (float layers: float): in one its rounding would cost as much accuracy as that of y.
+// Read by ordinary loads throughout: this launch begins before the one that writes x, idx and gates has ended (and before what wrote the weights has), so nothing of it is read-only for
+// as long as the launch runs, which is what non-coherent loads are for.
 struct Few {
     const void *x, *b1, *b2;     // x: [T][d], of bf16 layers the turned copy [T][dw]
     void *y;
@@ -108,7 +110,7 @@ __device__ __forceinline__ void put_routing(const Routing &r, int32_t t, int32_t
 }
 
 // A block per token: a warp takes an eighth of the columns, 256 at a time beside the best of those before, then one warp the eight warps' best
-__global__ void __launch_bounds__(256) few_select_kernel(const float *__restrict__ logits, int32_t n, int32_t k, const Routing r) {
+__global__ void __launch_bounds__(256) few_select_kernel(const float *logits, int32_t n, int32_t k, const Routing r) {
     wait_previous_kernel();
     constexpr int V = 8;
     __shared__ uint32_t sh_key[64];
@@ -328,8 +330,8 @@ __device__ __forceinline__ void make_segments(const Few &a, FewShared &S, FewTab
         token[i] = a.by_k(p, none);
         e[i] = -1;
         if (p >= R) continue;
-        e[i] = __ldg(a.idx + p);
-        const float g = __ldg(a.gates + p);
+        e[i] = a.idx[p];
+        const float g = a.gates[p];
         const bool known = (uint32_t)e[i] < (uint32_t)a.n;  // always, but for a gate of a launch that gave up
         MOE_BOUNDS_NOTE(known);
         e[i] = known ? e[i] : 0;
@@ -536,7 +538,7 @@ template <typename T> struct Worker {
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int u = 0; u < NT; ++u)
-                    if (i < a.tiles1 && (u == 0 || more)) next[j][0][u] = __ldg(reinterpret_cast<const uint4 *>(row[u] + i * TILE_K + 32 * j));
+                    if (i < a.tiles1 && (u == 0 || more)) next[j][0][u] = *reinterpret_cast<const uint4 *>(row[u] + i * TILE_K + 32 * j);
         };
         fetch(w);
 #pragma unroll 1
@@ -693,7 +695,7 @@ template <typename T> struct Worker {
                 float4 *part = reinterpret_cast<float4 *>(a.parts + ((int64_t)rows[q] * a.units + t.unit) * a.d + col);
                 float4 old = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (slice > t.slice) old = *part;
-                else if (slice == 0) old = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(a.b2) + (int64_t)t.expert * a.d + col));
+                else if (slice == 0) old = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.b2) + (int64_t)t.expert * a.d + col);
                 *part = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
             });
         }
