@@ -769,6 +769,7 @@ template <typename T> struct Worker {
             }
         }
         __threadfence();
+        __syncwarp();  // the other lanes' loads come behind lane 0's look at the counter: a vote orders no memory
         return __all_sync(0xffffffffu, ok);
     }
 };

@@ -16,3 +16,11 @@ def test_no_non_coherent_loads():
     text = source()
     assert "__ldg(" not in text and "ld.global.nc" not in text
     assert not re.search(r"__global__[^;{]*few_select_kernel\([^)]*__restrict__", text)
+
+
+def test_the_lanes_loads_come_behind_the_look_at_the_counter():
+    """One lane waits for a token's parts, all lanes load them: between the two stand a fence and a warp barrier. A vote makes the lanes meet but orders no memory."""
+    text = source()
+    body = text[text.index("bool complete("):]
+    body = body[:body.index("return __all_sync")]
+    assert 0 < body.index("load_relaxed") < body.index("__threadfence()") < body.index("__syncwarp()")
