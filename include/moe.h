@@ -461,6 +461,7 @@ int32_t moe_norm_workspace_bytes(const moe_config *cfg, size_t *host_bytes);
  * backward pass), in two launches (three with more than 256 experts): what moe_forward with noise 0 computes,
  *     logits = x.W_g by the fixed chain of moe_gate, topk_idx / gates as moe_gate chooses them,
  *     hid = relu(x.W1 + b1) (float; bf16 layers: two bf16 terms), y = sum_s gates_s * (hid_s.W2 + b2) in float, one rounding.
+ *     (bf16 layers: a product with W2 of 64 hidden units that is no finite number is that of the first term alone, as in moe_forward.)
  * The routing is moe_gate's without its screen bit for bit. T larger or a hierarchical layer: MOE_ERR_UNSUPPORTED. y may not overlap an input.
  * in : x [T,d] act, Wg [d,n], W1, b1, W2, b2 as in moe_forward
  * out: y [T,d] act; topk_idx [T,k], gates [T,k] (each may be NULL).   ws: moe_few_workspace_bytes, its own in every call that may

@@ -585,6 +585,27 @@ template <typename T> struct Worker {
             if (!arrived()) return;
 #pragma unroll
             for (int j = 0; j < 2; ++j) multiply<2>(acc, at_hand() + j * (32 * 128), x[j], more);
+            // hid's second term has either sign, or is 0: it makes a NaN of the infinity that the first gives beside an infinite weight or beyond float's range. What is no finite number is
+            // therefore the first term's alone, as if hid were one bf16 number. Rare: a sum of zero times every element that is used, and a vote
+            float odd = 0.0f;
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    if (u * 8 + 2 * c + r < m)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) odd = fmaf(acc[e >> 1][u][2 * (e & 1) + r], 0.0f, odd);
+            if (__any_sync(0xffffffffu, odd != 0.0f)) {
+                float first[4][NT][4];
+                clear(first);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) multiply<1>(first, at_hand() + j * (32 * 128), reinterpret_cast<const uint4 (&)[1][NT]>(x[j][0]), more);
+#pragma unroll
+                for (int i = 0; i < 16 * NT; ++i) {
+                    float &v = acc[i / (4 * NT)][i / 4 % NT][i % 4];
+                    v = fabsf(v) <= FLT_MAX ? v : first[i / (4 * NT)][i / 4 % NT][i % 4];
+                }
+            }
             release();
 #pragma unroll
             for (int u = 0; u < NT; ++u)
