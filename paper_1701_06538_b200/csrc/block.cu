@@ -111,7 +111,11 @@ int32_t moe_forward_few(const moe_config *cfg, const void *x, const float *Wg, c
                         const void *b2, void *y, int32_t *topk_idx, float *gates, void *ws, void *stream) {
     MOE_TRY(check_few(cfg));
     REQUIRE_PTRS(x, Wg, W1, b1, W2, b2, y, ws);
-    if ((topk_idx && bad_ptr(topk_idx)) || (gates && bad_ptr(gates)) || y == x) return MOE_ERR_INVALID_ARG;  // rows of x are read until the last of y are written
+    if ((topk_idx && bad_ptr(topk_idx)) || (gates && bad_ptr(gates))) return MOE_ERR_INVALID_ARG;
+    const int64_t T = cfg->T, d = cfg->d, h = cfg->h, n = cfg->n, act = (int64_t)act_bytes(cfg->act);
+    const struct { const void *at; int64_t bytes; } inputs[] = {{x, T * d * act}, {Wg, d * n * 4}, {W1, n * d * h * act}, {b1, n * h * act}, {W2, n * h * d * act}, {b2, n * d * act}};
+    for (const auto &in : inputs)  // which are read until the last of y is written
+        if (overlap(y, T * d * act, in.at, in.bytes)) return MOE_ERR_INVALID_ARG;
     return launch_few_tokens(*cfg, x, Wg, W1, b1, W2, b2, y, topk_idx, gates, ws, static_cast<cudaStream_t>(stream));
 }
 
