@@ -440,8 +440,11 @@ def moe_adamw(tensors, lr, beta1, beta2, eps, step, seed=0, grad_scale=1.0, rate
     are read when the kernels run."""
     if tensors.device is not None and tensors.device != torch.cuda.current_device():
         raise ValueError("moe_adamw: the tensors are not on the current device")
-    if rates is not None and rates.get_device() != torch.cuda.current_device():
-        raise ValueError("moe_adamw: rates are not on the current device")
+    if rates is not None:
+        if rates.dtype not in (torch.float32, torch.int32, torch.uint32) or rates.numel() < 5 or not rates.is_contiguous():
+            raise ValueError(f"moe_adamw: rates are {rates.numel()} elements of {rates.dtype}, wanted 5 contiguous 4-byte words")
+        if rates.get_device() != torch.cuda.current_device():
+            raise ValueError("moe_adamw: rates are not on the current device")
     p = moe_adamw_params(lr, beta1, beta2, eps, grad_scale, step, seed & 0xffffffff)
     status = lib().moe_adamw(tensors.array, ctypes.c_int32(len(tensors.tensors)), ctypes.byref(p), ctypes.c_void_p(_p(rates)), ctypes.c_void_p(_stream()))
     if status:
