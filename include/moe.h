@@ -162,7 +162,11 @@ int64_t moe_debug_bounds_violations(void);
 
 /* Synchronises `stream`, then reads the status word the kernels of the last call that used
  * `ws` left there. MOE_OK, or MOE_ERR_TIMEOUT if a bounded wait inside a tensor-core kernel
- * gave up (its outputs are then undefined; the context stays usable). */
+ * gave up (its outputs are then undefined; the context stays usable).
+ * Calls without such waits leave the word as they find it: moe_dispatch, moe_losses, moe_losses_bwd, moe_gate_balanced,
+ * moe_expert_adam_factored, moe_norm_in_bwd, moe_norm_out_bwd, and moe_gate_balanced_bwd where its contractions are not on
+ * the tensor cores. A report of an earlier call in the same workspace stays there; in a workspace that no other call has
+ * used the word is whatever the memory held, and says nothing. */
 int32_t moe_check_status(const void *ws, void *stream);
 
 /* ------------------------------------------------------------------------------------------
