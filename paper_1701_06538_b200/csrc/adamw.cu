@@ -247,7 +247,7 @@ __device__ __forceinline__ void update(const Entry &t, int64_t chunk, const Cons
 template <typename WT, typename GT, bool MASTER, bool FULL>
 __device__ __forceinline__ void update_eight(const Entry &t, int64_t begin, int32_t steps, const Constants &k, const moe_adamw_rates &r) {
     using MT = typename std::conditional<MASTER, float, WT>::type;  // of what the step is taken on
-    const float down = -r.lr / r.bias1, root_by = 1.0f / sqrtf(r.bias2), decay = -r.lr * t.decay;
+    const float down = -r.lr / r.bias1, root_by = 1.0f / sqrtf(r.bias2), decay = t.decay * r.bias1;
     const float by_g = k.one_beta1 * r.grad_scale, minus_by_gg = -k.one_beta2 * r.grad_scale * r.grad_scale;
     const int64_t at = begin + threadIdx.x * EACH;
     WT *w_at = static_cast<WT *>(t.w) + at;
@@ -307,8 +307,10 @@ __device__ __forceinline__ void update_eight(const Entry &t, int64_t begin, int3
             const float2 mm = fma2(both(k.one), mul2(both(k.beta1), mul2(make_float2(m[e], m[e + 1]), both(ms))), mul2(both(by_g), gg));
             const float2 old = mul2(make_float2(root[e], root[e + 1]), both(vs));
             const float2 rt = minus_roots(fma2(both(k.one), mul2(both(-k.beta2), mul2(old, old)), mul2(both(minus_by_gg), mul2(gg, gg)))), den = fma2(rt, both(-root_by), both(k.eps));
-            // The step as one number before the weight: 1 - lr weight_decay as a factor of the weight is rounded to 2^-24, which is all of a small rate
-            const float2 old_w = make_float2(w[e], w[e + 1]), ww = add2(old_w, fma2(mul2(mm, both(down)), make_float2(reciprocal(den.x), reciprocal(den.y)), mul2(old_w, both(decay))));
+            // w - lr / bias1 (m / den + weight_decay bias1 w): the step is one number before it meets the weight. (1 - lr weight_decay as a factor of the weight is rounded to 2^-24, which is
+            // all of a small rate)
+            const float2 old_w = make_float2(w[e], w[e + 1]), part = mul2(mm, make_float2(reciprocal(den.x), reciprocal(den.y)));
+            const float2 ww = fma2(fma2(old_w, both(decay), part), both(down), old_w);
             m[e] = mm.x; m[e + 1] = mm.y;
             root[e] = rt.x; root[e + 1] = rt.y;
             w[e] = ww.x; w[e + 1] = ww.y;
