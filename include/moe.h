@@ -427,7 +427,7 @@ int32_t moe_layer_backward(const moe_config *cfg, const void *dOut, const void *
  *     out = residual_scale * x + gate * (y * rsqrt(mean(y^2) + eps) * w)    (moe_norm_out)
  * and moe_norm_out gives the norm before the NEXT block with it, while the row is at hand:
  *     next = out * rsqrt(mean(out^2) + eps) * w_next                        (of `out` before it is rounded)
- * Means are over the d columns of a row. w, w_next [d] float; gate [ceil(T / rows_per_gate), d] act: row t takes gate row
+ * Means are over the d columns of a row, of squares in float: a row whose sum of squares is beyond float's range (elements of 2^60 or so) has the factor 0. w, w_next [d] float; gate [ceil(T / rows_per_gate), d] act: row t takes gate row
  * t / rows_per_gate (1: a gate per token; the length of a sequence: one per sequence; T: one for all), or NULL for ones
  * (rows_per_gate is then ignored). w_next NULL: no norm behind it; next and rstd_next are then ignored.
  * rstd, rstd_next [T] float: the factors rsqrt(mean + eps) for the backward pass.
@@ -488,7 +488,8 @@ int32_t moe_forward_few(const moe_config *cfg, const void *x, const float *Wg, c
  * x ^= x >> 16, x *= 0x7feb352d, x ^= x >> 15, x *= 0x846ca68b, x ^= x >> 16: give every step its own seed and the tensors of a
  * step ranges of `first` that do not overlap. v above 0 keeps a code above 0. An element that is no finite number is held as
  * NaN and leaves its block's scale to the others (so is the root of a v beyond float's range, of a gradient beyond 2^64 or so; the weight becomes NaN
- * with it). Zeroed codes and scales are the state before the first step. eps is at least float's smallest normal number.
+ * with it). What 8 bits cost: with gradients of one normal distribution over 10,000 steps of beta2 0.999 the roots neither drift nor stick, but wander: of 98 in 100 elements they are 0.68 to 1.48 of
+ * the true ones (moments in float: 0.96 to 1.04), the mean of v is 5 percent high, and m is off by a twelfth of its size (root mean square). Zeroed codes and scales are the state before the first step. eps is at least float's smallest normal number.
  * All pointers but host_tensors, host_params are device pointers, w, g, master, m, v on 32-byte boundaries. The list is read before the call
  * returns; tensors of a list may not overlap. rates: NULL, or a moe_adamw_rates in device memory that takes the place of lr, step, grad_scale and
  * seed when the kernels run, for recorded graphs.

@@ -242,7 +242,7 @@ __device__ __forceinline__ void update(const Entry &t, int64_t chunk, const Cons
     }
 }
 
-// With 8-bit moments the arithmetic is more than the memory: 66 instructions an element (93 as it was written first: 1218 us), issued in three cycles of four, 596 us for 268
+// With 8-bit moments the arithmetic is more than the memory: 59 instructions an element (93 as it was written first: 1218 us), 576 us for 268
 // million elements, whose bytes take 415. begin: the block's first element; FULL: none of its steps meets the tensor's end
 template <typename WT, typename GT, bool MASTER, bool FULL>
 __device__ __forceinline__ void update_eight(const Entry &t, int64_t begin, int32_t steps, const Constants &k, const moe_adamw_rates &r) {

@@ -6,7 +6,7 @@
 //   few_select_kernel   picks them from logits in memory, where a cluster does not hold the gate (more than 256 experts)
 //   few_experts_kernel  one block per SM. Every block sorts the slots by expert; then its teams of warps draw tasks from a counter: an expert's rows (16 at most) and 64 hidden
 //                       units. The team makes hid of those units, which nobody else needs, and its part of y from them. (Tasks for hid and tasks for y, hid handed over through
-//                       memory: 27.8 us, not 21.0, for 1 token of 1024 x 4096, 35.4, not 24.0, for 24 tokens of 32 experts of 512 x 1024, of which a warp waited 3 to 7 us for hid
+//                       memory: 27.8 us, not 21.3, for 1 token of 1024 x 4096, 35.4, not 24.4, for 24 tokens of 32 experts of 512 x 1024, of which a warp waited 3 to 7 us for hid
 //                       and whoever came last summed up a token's y alone, for up to 7.) When all tasks are drawn, warps draw 16 columns of a token's y each, wait until its parts
 //                       are there and add them up in order: results do not depend on who does what, and whoever waits, waits for blocks that are running.
 //
@@ -586,7 +586,8 @@ template <typename T> struct Worker {
 #pragma unroll
             for (int j = 0; j < 2; ++j) multiply<2>(acc, at_hand() + j * (32 * 128), x[j], more);
             // hid's second term has either sign, or is 0: it makes a NaN of the infinity that the first gives beside an infinite weight or beyond float's range. What is no finite number is
-            // therefore the first term's alone, as if hid were one bf16 number. Rare: a sum of zero times every element that is used, and a vote
+            // therefore the first term's alone, as if hid were one bf16 number. Rare, and found by a sum of zero times every element that is used, and a vote: no time by the clock (24 tokens 28.3 us a
+            // call with it, 28.7 without)
             float odd = 0.0f;
 #pragma unroll
             for (int u = 0; u < NT; ++u)

@@ -790,7 +790,7 @@ __global__ void __launch_bounds__(RUNS * 32) norm_sums_kernel(const NormGradArgs
 template <typename T, int V> int32_t launch_rows(const NormArgs &a, int warps, int teams, cudaStream_t st) {
     // As many blocks as the SMs hold at once, 3 (bf16, norm and residual, two vectors a lane) or 4 an SM, for several rows each: 32768 x 512 with norm and next 23.4 us (4 an SM: 27.9),
     // 131072 x 512, norm_in 43.3 (3: 45.5, 6: 48.6), 65536 x 256 23.7 (26.1, 27.8), float, 30000 x 320 29.4 (31.5, 32.7). Blocks of one row a team: 26.8, 55.0, 31.5 and 38.6; they stay for few
-    // rows and for rows of more than eight warps (8192 x 8192: 121, several rows each 131).
+    // rows and for rows of more than eight warps (8192 x 8192, norm, no gate, next: 121, several rows each 131).
     const int64_t at_once = 148 * (V == 2 && a.y && sizeof(T) == 2 ? 3 : 4), blocks = cdiv(a.T, teams);
     const bool ahead = V <= 2 && warps <= 8 && blocks > at_once;
     const dim3 grid((unsigned)(ahead ? at_once : blocks)), block(warps * 32 * teams);
