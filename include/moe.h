@@ -427,7 +427,8 @@ int32_t moe_layer_backward(const moe_config *cfg, const void *dOut, const void *
  *     out = residual_scale * x + gate * (y * rsqrt(mean(y^2) + eps) * w)    (moe_norm_out)
  * and moe_norm_out gives the norm before the NEXT block with it, while the row is at hand:
  *     next = out * rsqrt(mean(out^2) + eps) * w_next                        (of `out` before it is rounded)
- * Means are over the d columns of a row, of squares in float: a row whose sum of squares is beyond float's range (elements of 2^60 or so) has the factor 0. w, w_next [d] float; gate [ceil(T / rows_per_gate), d] act: row t takes gate row
+ * Means are over the d columns of a row, of squares in float: a row whose sum of squares is beyond float's range (elements of
+ * 2^60 or so) has the factor 0. w, w_next [d] float; gate [ceil(T / rows_per_gate), d] act: row t takes gate row
  * t / rows_per_gate (1: a gate per token; the length of a sequence: one per sequence; T: one for all), or NULL for ones
  * (rows_per_gate is then ignored). w_next NULL: no norm behind it; next and rstd_next are then ignored.
  * rstd, rstd_next [T] float: the factors rsqrt(mean + eps) for the backward pass.

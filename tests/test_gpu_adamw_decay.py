@@ -41,5 +41,4 @@ def test_decay_adds_up(bits, w, master, lr):
         size = float(before.square().sum())
         off += float(((at.double() - (before - part - decay).float().double()) * before).sum()) / size
         decayed += float((decay * before).sum()) / size
-    print(bits, w, lr, off, decayed)
     assert abs(off) <= 8e-9 and decayed >= 1.2e-6
