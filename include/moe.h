@@ -144,7 +144,8 @@ typedef enum {
     MOE_BUF_CONTEXT = 3,     /* ctx of the fused calls                        */
     MOE_BUF_WS_ADAM = 4,     /* ws of moe_expert_adam_factored                */
     MOE_BUF_WS_NORM = 5,     /* ws of moe_norm_in_bwd / moe_norm_out_bwd      */
-    MOE_BUF_WS_FEW = 6       /* ws of moe_forward_few                         */
+    MOE_BUF_WS_FEW = 6,      /* ws of moe_forward_few                         */
+    MOE_BUF_WS_LAYER_NORM = 7 /* ws of moe_layer_norm_bwd                     */
 } moe_buffer_role;
 int32_t moe_check_buffer_sizes(const moe_config *cfg, int32_t which, size_t bytes);
 
@@ -164,7 +165,7 @@ int64_t moe_debug_bounds_violations(void);
  * `ws` left there. MOE_OK, or MOE_ERR_TIMEOUT if a bounded wait inside a tensor-core kernel
  * gave up (its outputs are then undefined; the context stays usable).
  * Calls without such waits leave the word as they find it: moe_dispatch, moe_losses, moe_losses_bwd, moe_gate_balanced,
- * moe_expert_adam_factored, moe_norm_in_bwd, moe_norm_out_bwd, and moe_gate_balanced_bwd where its contractions are not on
+ * moe_expert_adam_factored, moe_norm_in_bwd, moe_norm_out_bwd, moe_layer_norm_bwd, moe_router_losses, and moe_gate_balanced_bwd where its contractions are not on
  * the tensor cores. A report of an earlier call in the same workspace stays there; in a workspace that no other call has
  * used the word is whatever the memory held, and says nothing. */
 int32_t moe_check_status(const void *ws, void *stream);
@@ -518,6 +519,96 @@ typedef struct moe_adamw_rates {
 } moe_adamw_rates;
 int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe_adamw_params *host_params, const moe_adamw_rates *rates,
                   void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The Muon step over a list of batches of matrices (experts' weights, gates): momentum, the update orthogonalised by Newton-Schulz products, weights.
+ * For every matrix of [count, rows, cols]
+ *     m = momentum m + g                        (g times grad_scale; rounded to m's type)
+ *     u = g + momentum m  (nesterov)  or  m
+ *     X = u / (|u| + eps)                       (over the Frobenius norm)
+ *     `steps` times:  X = a X + b (X X') X + c (X X') (X X') X,   a = 3.4445, b = -4.7750, c = 2.0315
+ *     w = w - lr * (scale X + weight_decay w)   (in float, one rounding to w's type)
+ * After five steps X's singular values lie between 0.7 and 1.2, wherever those of u were between 1 and 1/1000 or so of its norm. scale: 0.2 sqrt(max(rows, cols)) makes the update's elements as
+ * large as those of an Adam step. With `master` (float, only beside bf16 weights) the step is taken on the master and w is its rounding.
+ * The products' operands are X, X X' and the polynomial in fp16, scaled so that nothing overflows, with sums in float: X is off by 5e-4 of itself (root mean square) for u of any size; what u holds
+ * in directions below 2^-12 of its largest is lost in that. g and m may be as large as 2^60 or so: a matrix with a larger or no finite element in u becomes NaN as a whole. A matrix whose u is zero
+ * keeps its weights but for the decay.
+ * All pointers but host_tensors, host_params are device pointers; w, g, m, master on 32-byte boundaries. The list is read before the call returns; tensors of a list may not overlap.
+ * Matrices of one shape are taken together, from whatever tensors of the list: a list of a model's layers is three launches for each shape (and for each 1 GiB of X of it).
+ * rates: NULL, or a moe_muon_rates in device memory that takes the place of lr and grad_scale when the kernels run, for recorded graphs.
+ * ws: moe_muon_workspace_bytes, its own in every call that may run at the same time; 256-byte aligned. MOE_ERR_TIMEOUT in its status word: see moe_check_status.
+ * ------------------------------------------------------------------------------------------ */
+#define MOE_MUON_MAX_SIDE 32768
+#define MOE_MUON_MAX_STEPS 16
+typedef struct moe_muon_tensor {
+    void *w;                   /* [count, rows, cols], in-out */
+    const void *g;             /* [count, rows, cols] */
+    float *master;             /* [count, rows, cols], in-out, or NULL */
+    void *m;                   /* [count, rows, cols], in-out; zeros before the first step */
+    int64_t count;             /* matrices */
+    int32_t rows, cols;        /* each at most MOE_MUON_MAX_SIDE */
+    int32_t w_type, g_type, m_type; /* moe_dtype */
+    float weight_decay, scale;
+} moe_muon_tensor;
+typedef struct moe_muon_params {
+    double lr, momentum, eps, grad_scale;
+    int32_t steps;             /* 1 to MOE_MUON_MAX_STEPS */
+    int32_t nesterov;          /* 1 or 0 */
+} moe_muon_params;
+typedef struct moe_muon_rates {
+    float lr, grad_scale;
+} moe_muon_rates;
+int32_t moe_muon_workspace_bytes(const moe_muon_tensor *host_tensors, int32_t count, size_t *host_bytes);
+int32_t moe_muon(const moe_muon_tensor *host_tensors, int32_t count, const moe_muon_params *host_params, const moe_muon_rates *rates, void *ws, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Losses of the router over all experts' probabilities (moe_losses are those over the kept gates), with their gradient, for flat layers. A token is live if it lies in a
+ * sequence and keep does not say 0; T_s: live tokens of sequence s, L: of all. With p = softmax(logits) and lse = log(sum(exp(logits))) of a token
+ *     counts[s, j]    = choices of expert j by the live tokens of sequence s     (ids outside [0, n) count nowhere)
+ *     prob_sums[s, j] = sum of p_tj over them
+ *     losses[0] = w_balance * n / (k L) * sum_s (1 / T_s) sum_j counts[s, j] prob_sums[s, j]      (w_balance where everything is even)
+ *     losses[1] = w_z / L * sum_t lse_t^2
+ *     dlogits   = gradient of losses[0] + losses[1], counts being constants; rows of tokens that are not live are 0
+ * logits may hold -inf (an expert that is shut: p = 0); a live row of nothing else has p = 0, lse = 0 and no gradient, and counts as a token. NaN and +inf make their row's gradient and the
+ * losses NaN. Rows that are not live are not read.
+ * in : logits [T,n] float (moe_gate's `clean`), topk_idx [T,k]; keep [T] uint8 or NULL (all); seq_offsets [sequences + 1] int32, ascending, inside [0, T], or NULL: the whole batch is one
+ *      sequence (sequences is 1 then). Tokens before the first offset and from the last one on are padding, whatever the offsets between
+ *      say; sequences may be empty.
+ * out: losses [2], counts [sequences, n] int32, prob_sums [sequences, n] (may be NULL), dlogits [T,n] float (NULL: losses alone). No output may overlap an input or another one.
+ * Of cfg only T, n and k matter. dlogits goes into moe_gate_bwd_added / moe_backward_added / moe_layer_backward_added.
+ * ws: moe_router_losses_workspace_bytes, its own in every call that may run at the same time.
+ * ------------------------------------------------------------------------------------------ */
+#define MOE_MAX_SEQUENCES 4096
+int32_t moe_router_losses_workspace_bytes(const moe_config *cfg, int32_t sequences, size_t *host_bytes);
+int32_t moe_router_losses(const moe_config *cfg, const float *logits, const int32_t *topk_idx, const uint8_t *keep, const int32_t *seq_offsets, int32_t sequences,
+                          float w_balance, float w_z, float *losses, int32_t *counts, float *prob_sums, float *dlogits, void *ws, void *stream);
+
+/* moe_gate_bwd, moe_backward and moe_layer_backward with a gradient that reaches the clean logits from elsewhere added: dlogits [T,n] float (moe_router_losses'), or NULL for the plain call.
+ * Flat layers (MOE_ERR_UNSUPPORTED otherwise). Same workspaces. */
+int32_t moe_gate_bwd_added(const moe_config *cfg, const void *x, const float *Wg, const float *Wnoise, const float *noise, const float *clean, const float *raw_noise,
+                           const int32_t *topk_idx, const float *gates, const float *kth_vals, const int32_t *kth_idx, float *dgates, const float *dload, const float *dlogits,
+                           float *dWg, float *dWnoise, float *dX_gate, void *ws, void *stream);
+int32_t moe_backward_added(const moe_config *cfg, const void *dY, const void *x, const float *Wg, const float *Wnoise, const float *noise, const void *W1, const void *b1,
+                           const void *W2, const void *b2, const void *ctx, const float *dlogits, void *dX, float *dWg, float *dWnoise, void *dW1, void *db1, void *dW2,
+                           void *db2, void *ws, void *stream);
+int32_t moe_layer_backward_added(const moe_config *cfg, const void *dOut, const void *x, const float *Wg, const float *Wnoise, const float *noise, const void *W1, const void *b1,
+                                 const void *W2, const void *b2, const uint8_t *keep_bits, float drop_prob, const void *ctx, const float *dlogits, void *dX, float *dWg,
+                                 float *dWnoise, void *dW1, void *db1, void *dW2, void *db2, void *ws, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Layer norm, for blocks that have it in the place of moe_norm_in:
+ *     xn = (x - mean) * rstd * w + b,   rstd = (variance + eps)^-1/2,   mean and variance over the d columns of a row
+ * w, b [d] float; b NULL: no bias (db is then ignored). mean, rstd [T] float for the backward pass. Squares are float: a row whose differences from the mean are beyond 2^60 or so has the factor 0.
+ * Of cfg only T, d and act matter. d is at most MOE_NORM_MAX_D (MOE_ERR_UNSUPPORTED beyond). eps > 0. xn may be x.
+ * ------------------------------------------------------------------------------------------ */
+/* in : x [T,d] act, w, b   out: xn [T,d] act, mean, rstd (each may be NULL) */
+int32_t moe_layer_norm(const moe_config *cfg, const void *x, const float *w, const float *b, float eps, void *xn, float *mean, float *rstd, void *stream);
+
+/* dX = dres + the adjoint of moe_layer_norm: dres [T,d] act is the gradient that reaches x beside the norm, or NULL.
+ * in: dxn [T,d] act, x, w, mean, rstd   out: dX [T,d] act, dw, db [d] float (db may be NULL). dX may be dxn, dres or x.   ws: moe_layer_norm_workspace_bytes */
+int32_t moe_layer_norm_bwd(const moe_config *cfg, const void *dxn, const void *x, const float *w, const float *mean, const float *rstd, const void *dres, void *dX, float *dw,
+                           float *db, void *ws, void *stream);
+int32_t moe_layer_norm_workspace_bytes(const moe_config *cfg, size_t *host_bytes);
 
 #ifdef __cplusplus
 }

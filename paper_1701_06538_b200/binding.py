@@ -28,7 +28,8 @@ EXPORTS = ["moe_debug_launch_count", "moe_validate", "moe_query_sizes", "moe_wor
            "moe_expert_ffn_bits", "moe_expert_ffn_bwd_bits", "moe_query_balanced_sizes", "moe_gate_balanced", "moe_dispatch_balanced", "moe_combine_balanced",
            "moe_combine_balanced_bwd", "moe_gate_balanced_bwd", "moe_dispatch_balanced_bwd",
            "moe_norm_in", "moe_norm_in_bwd", "moe_norm_out", "moe_norm_out_bwd", "moe_norm_workspace_bytes", "moe_few_workspace_bytes",
-           "moe_forward_few", "moe_adamw"]
+           "moe_forward_few", "moe_adamw", "moe_muon_workspace_bytes", "moe_muon", "moe_router_losses_workspace_bytes", "moe_router_losses", "moe_gate_bwd_added",
+           "moe_backward_added", "moe_layer_backward_added", "moe_layer_norm", "moe_layer_norm_bwd", "moe_layer_norm_workspace_bytes"]
 
 
 class MoeError(RuntimeError):
@@ -67,6 +68,15 @@ class moe_adamw_tensor(ctypes.Structure):
 
 class moe_adamw_params(ctypes.Structure):
     _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [("step", ctypes.c_int32), ("seed", ctypes.c_uint32)]
+
+
+class moe_muon_tensor(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("w", "g", "master", "m")] + [("count", ctypes.c_int64)] + \
+               [(name, ctypes.c_int32) for name in ("rows", "cols", "w_type", "g_type", "m_type")] + [(name, ctypes.c_float) for name in ("weight_decay", "scale")]
+
+
+class moe_muon_params(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "momentum", "eps", "grad_scale")] + [("steps", ctypes.c_int32), ("nesterov", ctypes.c_int32)]
 
 
 _lib = None
@@ -449,6 +459,99 @@ def moe_adamw(tensors, lr, beta1, beta2, eps, step, seed=0, grad_scale=1.0, rate
     status = lib().moe_adamw(tensors.array, ctypes.c_int32(len(tensors.tensors)), ctypes.byref(p), ctypes.c_void_p(_p(rates)), ctypes.c_void_p(_stream()))
     if status:
         raise MoeError("moe_adamw", status)
+
+
+class moe_muon_list:
+    """The matrices of a Muon step, made once for a model. `tensors`: dicts with w, g, m of [rows, cols] or [count, rows, cols] and, where they apply, master, weight_decay (0),
+    scale (1). Keeps references to the tensors: their addresses are what the call gets."""
+
+    def __init__(self, tensors):
+        self.tensors = [dict(t) for t in tensors]
+        self.array = (moe_muon_tensor * max(len(self.tensors), 1))()
+        types, self.device = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}, None
+        for t, r in zip(self.tensors, self.array):
+            shape = tuple(t["w"].shape)
+            if len(shape) not in (2, 3):
+                raise ValueError(f"moe_muon_list: w is {shape}, wanted [rows, cols] or [count, rows, cols]")
+            for q, dtypes in (("w", tuple(types)), ("g", tuple(types)), ("m", tuple(types)), ("master", (torch.float32,))):
+                x = t.get(q)
+                if x is None:
+                    if q != "master":
+                        raise ValueError(f"moe_muon_list: {q} is missing")
+                    continue
+                if x.dtype not in dtypes or tuple(x.shape) != shape:
+                    raise ValueError(f"moe_muon_list: {q} is {tuple(x.shape)} of {x.dtype}, wanted {shape} of {dtypes}")
+                if self.device is None:
+                    self.device = x.get_device()
+                if x.get_device() != self.device:
+                    raise ValueError("moe_muon_list: the tensors are on different devices")
+                setattr(r, q, _p(x))
+            r.count, (r.rows, r.cols) = shape[0] if len(shape) == 3 else 1, shape[-2:]
+            r.w_type, r.g_type, r.m_type = types[t["w"].dtype], types[t["g"].dtype], types[t["m"].dtype]
+            r.weight_decay, r.scale = t.get("weight_decay", 0.0), t.get("scale", 1.0)
+
+
+def moe_muon_workspace_bytes(tensors) -> int:
+    out = ctypes.c_size_t(0)
+    _checked("moe_muon_workspace_bytes", lib().moe_muon_workspace_bytes(tensors.array, ctypes.c_int32(len(tensors.tensors)), ctypes.byref(out)))
+    return out.value
+
+
+def moe_muon(tensors, lr, momentum, eps, steps, nesterov, ws, grad_scale=1.0, rates=None):
+    """`tensors`: a moe_muon_list. `rates`: two floats of device memory (lr, grad_scale) that are read when the kernels run."""
+    here = torch.cuda.current_device()
+    if tensors.device is not None and tensors.device != here:
+        raise ValueError("moe_muon: the tensors are not on the current device")
+    if ws.get_device() != here:
+        raise ValueError("moe_muon: the workspace is not on the current device")
+    if rates is not None:
+        if rates.dtype != torch.float32 or rates.numel() < 2 or not rates.is_contiguous():
+            raise ValueError(f"moe_muon: rates are {rates.numel()} elements of {rates.dtype}, wanted 2 contiguous floats")
+        if rates.get_device() != here:
+            raise ValueError("moe_muon: rates are not on the current device")
+    if ws.numel() * ws.element_size() < moe_muon_workspace_bytes(tensors):
+        raise ValueError("moe_muon: the workspace is too small")
+    p = moe_muon_params(lr, momentum, eps, grad_scale, steps, int(nesterov))
+    _checked("moe_muon", lib().moe_muon(tensors.array, ctypes.c_int32(len(tensors.tensors)), ctypes.byref(p), ctypes.c_void_p(_p(rates)), ctypes.c_void_p(_p(ws)),
+                                        ctypes.c_void_p(_stream())))
+
+
+def moe_router_losses_workspace_bytes(cfg, sequences=1) -> int:
+    out = ctypes.c_size_t(0)
+    _checked("moe_router_losses_workspace_bytes", lib().moe_router_losses_workspace_bytes(ctypes.byref(cfg), ctypes.c_int32(sequences), ctypes.byref(out)))
+    return out.value
+
+
+def moe_router_losses(cfg, logits, topk_idx, keep, seq_offsets, sequences, w_balance, w_z, losses, counts, prob_sums, dlogits, ws):
+    p = _here()
+    _checked("moe_router_losses", _bound("moe_router_losses", "cppppiffppppp")(cfg, p(logits), p(topk_idx), p(keep), p(seq_offsets), sequences, w_balance, w_z, p(losses), p(counts),
+                                                                               p(prob_sums), p(dlogits), p(ws), _stream()))
+
+
+def moe_gate_bwd_added(cfg, x, Wg, Wnoise, noise, clean, raw_noise, topk_idx, gates, kth_vals, kth_idx, dgates, dload, dlogits, dWg, dWnoise, dX_gate, ws):
+    _call("moe_gate_bwd_added", cfg, x, Wg, Wnoise, noise, clean, raw_noise, topk_idx, gates, kth_vals, kth_idx, dgates, dload, dlogits, dWg, dWnoise, dX_gate, ws)
+
+
+def moe_backward_added(cfg, dY, x, Wg, Wnoise, noise, W1, b1, W2, b2, ctx, dlogits, dX, dWg, dWnoise, dW1, db1, dW2, db2, ws):
+    _call("moe_backward_added", cfg, dY, x, Wg, Wnoise, noise, W1, b1, W2, b2, ctx, dlogits, dX, dWg, dWnoise, dW1, db1, dW2, db2, ws)
+
+
+def moe_layer_backward_added(cfg, dOut, x, Wg, Wnoise, noise, W1, b1, W2, b2, keep_bits, drop_prob, ctx, dlogits, dX, dWg, dWnoise, dW1, db1, dW2, db2, ws):
+    _call("moe_layer_backward_added", cfg, dOut, x, Wg, Wnoise, noise, W1, b1, W2, b2, keep_bits, float(drop_prob), ctx, dlogits, dX, dWg, dWnoise, dW1, db1, dW2, db2, ws)
+
+
+def moe_layer_norm_workspace_bytes(cfg) -> int:
+    return _one_size("moe_layer_norm_workspace_bytes", cfg)
+
+
+def moe_layer_norm(cfg, x, w, b, eps, xn, mean, rstd):
+    p = _here()
+    _checked("moe_layer_norm", _bound("moe_layer_norm", "cpppfppp")(cfg, p(x), p(w), p(b), eps, p(xn), p(mean), p(rstd), _stream()))
+
+
+def moe_layer_norm_bwd(cfg, dxn, x, w, mean, rstd, dres, dX, dw, db, ws):
+    p = _here()
+    _checked("moe_layer_norm_bwd", _bound("moe_layer_norm_bwd", "cpppppppppp")(cfg, p(dxn), p(x), p(w), p(mean), p(rstd), p(dres), p(dX), p(dw), p(db), p(ws), _stream()))
 
 
 # ----------------------------------------------------------------------------------------------

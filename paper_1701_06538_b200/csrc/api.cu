@@ -706,9 +706,10 @@ int32_t do_gate_bwd(const moe_config *c, const Dims &D, const void *x, const flo
                     const float *gates, const float *kth_vals, const int32_t *kth_idx, float *dgates,
                     const float *dload, float *dWg, float *dWnoise, float *dX_gate, void *ws_base, GateBwdWs &w,
                     cudaStream_t st, const HierIdx *ready = nullptr, SecondaryRows *sec = nullptr, const ColumnSums *beside = nullptr,
-                    BackwardTail *tail = nullptr) {
+                    BackwardTail *tail = nullptr, const float *added = nullptr) {
     // sec: the caller adds the secondary gates' rows to dX_gate itself (they stay in the scratch); beside: tile sums to be formed along
-    // with the logit gradients; tail: the last pass over the (first) gate's weight gradient may be left to the caller
+    // with the logit gradients; tail: the last pass over the (first) gate's weight gradient may be left to the caller; added (flat layers): a
+    // gradient of the clean logits from elsewhere
     GateParts left = {};
     GateParts *parts = tail ? &left : nullptr;
     auto leave_parts = [&]() {
@@ -787,7 +788,7 @@ int32_t do_gate_bwd(const moe_config *c, const Dims &D, const void *x, const flo
         return launch_add_slot_rows(w.dX_sec, D.T, (int32_t)D.k1, (int32_t)D.d, dX_gate, st);
     }
     MOE_TRY(launch_gate_logit_grads(noise, clean, raw_noise, topk_idx, gates, kth_vals, kth_idx, dgates, dload,
-                                    nullptr, D.T, (int32_t)D.n, (int32_t)D.k, w.dlogit, w.dsplit, nullptr, st, beside));
+                                    nullptr, D.T, (int32_t)D.n, (int32_t)D.k, w.dlogit, w.dsplit, nullptr, st, beside, added));
     if (w.tc)
         MOE_TRY(launch_tc_gate_bwd(x, D.T, (int32_t)D.d, (int32_t)D.n, Wg, Wnoise, w.dsplit, w.wsplit, w.partials, dWg,
                                    dWnoise, dX_gate, status_word(ws_base), st, D.flags, 0, parts));
@@ -896,9 +897,10 @@ int32_t moe_check_buffer_sizes(const moe_config *cfg, int32_t which, size_t byte
         case MOE_BUF_CONTEXT: need = s.ctx_bytes; break;
         case MOE_BUF_WS_ADAM: need = s.ws_adam_bytes; break;
         case MOE_BUF_WS_NORM:
-        case MOE_BUF_WS_FEW: {
+        case MOE_BUF_WS_FEW:
+        case MOE_BUF_WS_LAYER_NORM: {
             size_t own;
-            MOE_TRY(which == MOE_BUF_WS_NORM ? moe_norm_workspace_bytes(cfg, &own) : moe_few_workspace_bytes(cfg, &own));
+            MOE_TRY(which == MOE_BUF_WS_NORM ? moe_norm_workspace_bytes(cfg, &own) : which == MOE_BUF_WS_FEW ? moe_few_workspace_bytes(cfg, &own) : moe_layer_norm_workspace_bytes(cfg, &own));
             need = (int64_t)own;
             break;
         }
@@ -1030,11 +1032,24 @@ int32_t moe_losses_bwd(const moe_config *cfg, const float *importance, const flo
     return do_losses_bwd(cfg, D, importance, load, topk_idx, dgates, dload, cv, as_stream(stream));
 }
 
+// a gradient of the clean logits from elsewhere: of flat layers
+static int32_t check_added(const moe_config *cfg, const float *dlogits) {
+    MOE_TRY(check_config(cfg));
+    if (dlogits && bad_ptr(dlogits)) return MOE_ERR_INVALID_ARG;
+    return dlogits && cfg->a > 0 ? MOE_ERR_UNSUPPORTED : MOE_OK;
+}
+
 int32_t moe_gate_bwd(const moe_config *cfg, const void *x, const float *Wg, const float *Wnoise,
                      const float *noise, const float *clean, const float *raw_noise, const int32_t *topk_idx,
                      const float *gates, const float *kth_vals, const int32_t *kth_idx, float *dgates,
                      const float *dload, float *dWg, float *dWnoise, float *dX_gate, void *ws, void *stream) {
-    MOE_TRY(check_config(cfg));
+    return moe_gate_bwd_added(cfg, x, Wg, Wnoise, noise, clean, raw_noise, topk_idx, gates, kth_vals, kth_idx, dgates, dload, nullptr, dWg, dWnoise, dX_gate, ws, stream);
+}
+
+int32_t moe_gate_bwd_added(const moe_config *cfg, const void *x, const float *Wg, const float *Wnoise, const float *noise, const float *clean, const float *raw_noise,
+                           const int32_t *topk_idx, const float *gates, const float *kth_vals, const int32_t *kth_idx, float *dgates, const float *dload, const float *dlogits,
+                           float *dWg, float *dWnoise, float *dX_gate, void *ws, void *stream) {
+    MOE_TRY(check_added(cfg, dlogits));
     REQUIRE_PTRS(x, Wg, Wnoise, noise, clean, raw_noise, topk_idx, gates, kth_vals, kth_idx, dgates, dload, dWg,
                  dWnoise, dX_gate, ws);
     const Dims D = dims_of(cfg);
@@ -1043,7 +1058,7 @@ int32_t moe_gate_bwd(const moe_config *cfg, const void *x, const float *Wg, cons
     MOE_TRY(reset_status(ws, as_stream(stream)));
     GateBwdWs w(cv, D);
     return do_gate_bwd(cfg, D, x, Wg, Wnoise, noise, clean, raw_noise, topk_idx, gates, kth_vals, kth_idx, dgates,
-                       dload, dWg, dWnoise, dX_gate, ws, w, as_stream(stream));
+                       dload, dWg, dWnoise, dX_gate, ws, w, as_stream(stream), nullptr, nullptr, nullptr, nullptr, dlogits);
 }
 
 // keep_bits != nullptr: the output is that of the layer epilogue (sigmoid, dropout, residual) instead of Eq. 1 alone
@@ -1114,8 +1129,8 @@ static int32_t backward_impl(const moe_config *cfg, const void *dY, const void *
                              const float *Wnoise, const float *noise, const void *W1, const void *b1, const void *W2,
                              const void *b2, const uint8_t *keep_bits, float drop_prob, const void *ctx, void *dX,
                              float *dWg, float *dWnoise, void *dW1, void *db1, void *dW2, void *db2, void *ws,
-                             void *stream) {
-    MOE_TRY(check_config(cfg));
+                             void *stream, const float *dlogits = nullptr) {
+    MOE_TRY(check_added(cfg, dlogits));
     REQUIRE_PTRS(dY, x, Wg, Wnoise, noise, W1, b1, W2, b2, ctx, dX, dWg, dWnoise, dW1, db1, dW2, db2, ws);
     if (keep_bits) MOE_TRY(check_layer(cfg, keep_bits, drop_prob));
     const Dims D = dims_of(cfg);
@@ -1147,7 +1162,7 @@ static int32_t backward_impl(const moe_config *cfg, const void *dY, const void *
     SecondaryRows sec = {};
     const ColumnSums db2s = db2_sums(D, B.dys, db2, C.offsets, B.ffn, plan);
     MOE_TRY(do_gate_bwd(cfg, D, x, Wg, Wnoise, noise, C.clean, C.raw_noise, C.topk_idx, C.gates, C.kth_vals,
-                        C.kth_idx, B.dgates, B.dload, dWg, dWnoise, B.dX_gate, ws, B.gate, st, &C.hier, keeps_secondary_rows(D) ? &sec : nullptr, left ? &db2s : nullptr, left));
+                        C.kth_idx, B.dgates, B.dload, dWg, dWnoise, B.dX_gate, ws, B.gate, st, &C.hier, keeps_secondary_rows(D) ? &sec : nullptr, left ? &db2s : nullptr, left, dlogits));
     const void *hid = C.hid;
     uint32_t *bits = C.relu_bits;
     if (!hid) {  // MOE_FLAG_RECOMPUTE_HID: the forward kept no hidden activations; the first GEMM is run again
@@ -1179,6 +1194,19 @@ int32_t moe_layer_backward(const moe_config *cfg, const void *dOut, const void *
     if (!keep_bits) return MOE_ERR_INVALID_ARG;
     return backward_impl(cfg, dOut, x, Wg, Wnoise, noise, W1, b1, W2, b2, keep_bits, drop_prob, ctx, dX, dWg, dWnoise,
                          dW1, db1, dW2, db2, ws, stream);
+}
+
+int32_t moe_backward_added(const moe_config *cfg, const void *dY, const void *x, const float *Wg, const float *Wnoise, const float *noise, const void *W1, const void *b1,
+                           const void *W2, const void *b2, const void *ctx, const float *dlogits, void *dX, float *dWg, float *dWnoise, void *dW1, void *db1, void *dW2,
+                           void *db2, void *ws, void *stream) {
+    return backward_impl(cfg, dY, x, Wg, Wnoise, noise, W1, b1, W2, b2, nullptr, 0.0f, ctx, dX, dWg, dWnoise, dW1, db1, dW2, db2, ws, stream, dlogits);
+}
+
+int32_t moe_layer_backward_added(const moe_config *cfg, const void *dOut, const void *x, const float *Wg, const float *Wnoise, const float *noise, const void *W1, const void *b1,
+                                 const void *W2, const void *b2, const uint8_t *keep_bits, float drop_prob, const void *ctx, const float *dlogits, void *dX, float *dWg,
+                                 float *dWnoise, void *dW1, void *db1, void *dW2, void *db2, void *ws, void *stream) {
+    if (!keep_bits) return MOE_ERR_INVALID_ARG;
+    return backward_impl(cfg, dOut, x, Wg, Wnoise, noise, W1, b1, W2, b2, keep_bits, drop_prob, ctx, dX, dWg, dWnoise, dW1, db1, dW2, db2, ws, stream, dlogits);
 }
 
 int32_t moe_expert_adam_factored(const moe_config *cfg, void *W1, void *b1, void *W2, void *b2, const void *dW1,

@@ -35,6 +35,19 @@ int64_t norm_bytes(const moe_config &c, float **floats, void *ws) {
     return (int64_t)cv.off;
 }
 
+int64_t layer_norm_bytes(const moe_config &c, float **floats, void *ws) {
+    Carver cv(ws);
+    cv.take_bytes(kWsHeader);
+    float *f = cv.take<float>(layer_norm_grad_floats(c.T, c.d, c.act));
+    if (floats) *floats = f;
+    return (int64_t)cv.off;
+}
+int32_t check_router(const moe_config *c, int32_t sequences) {
+    MOE_TRY(moe_validate(c));
+    if (sequences < 1 || sequences > MOE_MAX_SEQUENCES) return MOE_ERR_INVALID_ARG;
+    return c->a > 0 ? MOE_ERR_UNSUPPORTED : MOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -126,6 +139,75 @@ int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe
     if (!(p.beta1 >= 0.0 && p.beta1 < 1.0 && p.beta2 >= 0.0 && p.beta2 < 1.0) || !((float)p.eps >= FLT_MIN) || bad_float((float)p.eps)) return MOE_ERR_INVALID_ARG;
     if (rates ? ((uintptr_t)rates & 3) != 0 : (p.step < 1 || bad_float((float)p.lr) || bad_float((float)p.grad_scale))) return MOE_ERR_INVALID_ARG;
     return launch_adamw(host_tensors, count, p, rates, static_cast<cudaStream_t>(stream));
+}
+
+int32_t moe_muon_workspace_bytes(const moe_muon_tensor *host_tensors, int32_t count, size_t *host_bytes) {
+    if (count < 0 || (count > 0 && !host_tensors) || !host_bytes) return MOE_ERR_INVALID_ARG;
+    MOE_TRY(muon_check(host_tensors, count));
+    int64_t bytes = 0;
+    MOE_TRY(muon_bytes(host_tensors, count, &bytes));
+    *host_bytes = (size_t)bytes;
+    return MOE_OK;
+}
+
+int32_t moe_muon(const moe_muon_tensor *host_tensors, int32_t count, const moe_muon_params *host_params, const moe_muon_rates *rates, void *ws, void *stream) {
+    if (count < 0 || (count > 0 && !host_tensors) || !host_params) return MOE_ERR_INVALID_ARG;
+    const moe_muon_params &p = *host_params;
+    if (!(p.momentum >= 0.0 && p.momentum < 1.0) || !(p.eps > 0.0) || !((float)p.eps >= FLT_MIN) || bad_float((float)p.eps)) return MOE_ERR_INVALID_ARG;
+    if (p.steps < 1 || p.steps > MOE_MUON_MAX_STEPS || (p.nesterov != 0 && p.nesterov != 1)) return MOE_ERR_INVALID_ARG;
+    if (rates ? ((uintptr_t)rates & 3) != 0 : (bad_float((float)p.lr) || bad_float((float)p.grad_scale))) return MOE_ERR_INVALID_ARG;
+    MOE_TRY(muon_check(host_tensors, count));
+    if (!ws || ((uintptr_t)ws & 255) != 0) return MOE_ERR_INVALID_ARG;
+    return launch_muon(host_tensors, count, p, rates, ws, static_cast<cudaStream_t>(stream));
+}
+
+int32_t moe_router_losses_workspace_bytes(const moe_config *cfg, int32_t sequences, size_t *host_bytes) {
+    MOE_TRY(check_router(cfg, sequences));
+    if (!host_bytes) return MOE_ERR_INVALID_ARG;
+    *host_bytes = (size_t)(kWsHeader + router_losses_bytes(cfg->T, cfg->n, sequences));
+    return MOE_OK;
+}
+
+int32_t moe_router_losses(const moe_config *cfg, const float *logits, const int32_t *topk_idx, const uint8_t *keep, const int32_t *seq_offsets, int32_t sequences,
+                          float w_balance, float w_z, float *losses, int32_t *counts, float *prob_sums, float *dlogits, void *ws, void *stream) {
+    MOE_TRY(check_router(cfg, sequences));
+    REQUIRE_PTRS(logits, topk_idx, losses, counts, ws);
+    if ((keep && bad_ptr(keep)) || (seq_offsets && bad_ptr(seq_offsets)) || (prob_sums && bad_ptr(prob_sums)) || (dlogits && bad_ptr(dlogits))) return MOE_ERR_INVALID_ARG;
+    if (!seq_offsets && sequences != 1) return MOE_ERR_INVALID_ARG;
+    if (bad_float(w_balance) || bad_float(w_z)) return MOE_ERR_INVALID_ARG;
+    const int64_t T = cfg->T, n = cfg->n, k = cfg->k, S = sequences;
+    const struct { const void *at; int64_t bytes; } all[] = {{losses, 8}, {counts, S * n * 4}, {prob_sums, S * n * 4}, {dlogits, T * n * 4}, {logits, T * n * 4}, {topk_idx, T * k * 4},
+                                                             {keep, T}, {seq_offsets, (S + 1) * 4}};
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 8; ++j)
+            if (all[i].at && all[j].at && overlap(all[i].at, all[i].bytes, all[j].at, all[j].bytes)) return MOE_ERR_INVALID_ARG;
+    const RouterLossArgs a = {T, cfg->n, cfg->k, sequences, logits, topk_idx, keep, seq_offsets, w_balance, w_z, losses, counts, prob_sums, dlogits};
+    return launch_router_losses(a, static_cast<char *>(ws) + kWsHeader, static_cast<cudaStream_t>(stream));
+}
+
+int32_t moe_layer_norm_workspace_bytes(const moe_config *cfg, size_t *host_bytes) {
+    MOE_TRY(check_norm(cfg));
+    if (!host_bytes) return MOE_ERR_INVALID_ARG;
+    *host_bytes = (size_t)layer_norm_bytes(*cfg, nullptr, nullptr);
+    return MOE_OK;
+}
+
+int32_t moe_layer_norm(const moe_config *cfg, const void *x, const float *w, const float *b, float eps, void *xn, float *mean, float *rstd, void *stream) {
+    MOE_TRY(check_norm(cfg));
+    REQUIRE_PTRS(x, w, xn);
+    if ((b && bad_ptr(b)) || (mean && bad_ptr(mean)) || (rstd && bad_ptr(rstd)) || !(eps > 0.0f) || bad_float(eps)) return MOE_ERR_INVALID_ARG;
+    const LayerNormArgs a = {cfg->T, cfg->d, cfg->act, x, w, b, eps, xn, mean, rstd};
+    return launch_layer_norm(a, static_cast<cudaStream_t>(stream));
+}
+
+int32_t moe_layer_norm_bwd(const moe_config *cfg, const void *dxn, const void *x, const float *w, const float *mean, const float *rstd, const void *dres, void *dX, float *dw,
+                           float *db, void *ws, void *stream) {
+    MOE_TRY(check_norm(cfg));
+    REQUIRE_PTRS(dxn, x, w, mean, rstd, dX, dw, ws);
+    if ((dres && bad_ptr(dres)) || (db && bad_ptr(db))) return MOE_ERR_INVALID_ARG;
+    LayerNormGradArgs a = {cfg->T, cfg->d, cfg->act, dxn, x, dres, w, mean, rstd, dX, dw, db, nullptr};
+    layer_norm_bytes(*cfg, &a.part, ws);
+    return launch_layer_norm_grads(a, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

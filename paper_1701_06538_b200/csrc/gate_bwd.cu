@@ -17,6 +17,12 @@ struct Beside {
     }
 };
 
+// What goes along with a launch: such sums, a gradient of the clean logits from elsewhere [rows, n] to be added, or both
+struct Added { const float *added; };
+struct BesideAdded : Beside { const float *added; };
+template <typename Ride> constexpr bool has_sums() { return std::is_base_of<Beside, Ride>::value; }
+template <typename Ride> constexpr bool has_added() { return std::is_same<Ride, Added>::value || std::is_same<Ride, BesideAdded>::value; }
+
 // One warp per row. With sigma = softplus(r), z = (c - thr)/sigma, q_j = dLoad_j * phi(z_j)/sigma_j:
 //   softmax over the kept slots:  dH[idx_s] += g_s (dg_s - sum_s' g_s' dg_s')
 //   load estimator:               dc_j += q_j ; dsigma_j += -z_j q_j ;
@@ -32,7 +38,7 @@ __global__ void __launch_bounds__(256) gate_logit_grads_kernel(
     bf16 *__restrict__ dsplit, const int32_t *__restrict__ split_row_index, const __grid_constant__ Ride beside) {
     wait_previous_kernel();
     int32_t block = blockIdx.x;
-    if constexpr (rides<Ride>()) {
+    if constexpr (has_sums<Ride>()) {
         if (block < beside.blocks) return beside.run(block);
         block -= beside.blocks;
     }
@@ -76,7 +82,9 @@ __global__ void __launch_bounds__(256) gate_logit_grads_kernel(
         if (j == j_k1) dh -= q_sel;
         if (j == j_k && k < n) dh -= q_uns;
         const float dsigma = fmaf(ej, dh, -zq);
-        const float dc = q + dh, dr = dsigma / (1.0f + expf(-rj));
+        float dc = q + dh;
+        const float dr = dsigma / (1.0f + expf(-rj));
+        if constexpr (has_added<Ride>()) dc += beside.added[row * n + j];
         if (dsplit) {
             // three-term bf16 split (hi | mid | lo), row layout [3][clean n | raw n], for the tensor-core products
             const int64_t orow = split_row_index ? split_row_index[row] : row;  // e.g. sorted by primary group
@@ -165,7 +173,7 @@ __global__ void __launch_bounds__(256) gate_logit_grads_pairs_kernel(
     const int32_t *__restrict__ split_row_index, const __grid_constant__ Ride beside) {
     wait_previous_kernel();
     int32_t block = blockIdx.x;
-    if constexpr (rides<Ride>()) {
+    if constexpr (has_sums<Ride>()) {
         if (block < beside.blocks) return beside.run(block);
         block -= beside.blocks;
     }
@@ -247,6 +255,7 @@ __global__ void __launch_bounds__(256) gate_logit_grads_pairs_kernel(
             if (j + h == j_k && k < n) dh -= q_uns;
             const float dsigma = fmaf(ej, dh, -zqv[2 * u + h]);
             dc[h] = qv[2 * u + h] + dh;
+            if constexpr (has_added<Ride>()) dc[h] += beside.added[row * n + j + h];
             dr[h] = __fdividef(dsigma, 1.0f + __expf(-rj));
         }
         // three-term bf16 split (hi | mid | lo), row layout [3][clean n | raw n], for the tensor-core products
@@ -265,7 +274,7 @@ int32_t launch_gate_logit_grads(const float *noise, const float *clean, const fl
                                 const float *gates, const float *kth_vals, const int32_t *kth_idx,
                                 const float *dgates, const float *dload, const int32_t *dload_row_group,
                                 int64_t rows, int32_t n, int32_t k, float *dlogit, void *dsplit,
-                                const int32_t *split_row_index, cudaStream_t st, const ColumnSums *sums) {
+                                const int32_t *split_row_index, cudaStream_t st, const ColumnSums *sums, const float *added) {
     if (rows == 0) return sums ? launch_segment_colsum(*sums, st) : MOE_OK;
     const int64_t more = sums ? column_tiles(*sums) * column_slabs(*sums) : 0;
     const unsigned grid = (unsigned)(cdiv(rows, 8) + more);
@@ -311,7 +320,9 @@ int32_t launch_gate_logit_grads(const float *noise, const float *clean, const fl
         MOE_LAUNCHED();
         return MOE_OK;
     };
-    return sums ? run(Beside{*sums, (int32_t)more, (int32_t)column_slabs(*sums)}) : run(Nothing{});
+    if (!sums) return added ? run(Added{added}) : run(Nothing{});
+    const Beside beside = {*sums, (int32_t)more, (int32_t)column_slabs(*sums)};
+    return added ? run(BesideAdded{beside, added}) : run(beside);
 }
 
 MOE_BOUNDS_READER(bounds_violations_gate_bwd)

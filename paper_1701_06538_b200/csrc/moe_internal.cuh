@@ -334,8 +334,8 @@ int32_t launch_gate_logit_grads(const float *noise, const float *clean, const fl
                                 const float *gates, const float *kth_vals, const int32_t *kth_idx,
                                 const float *dgates, const float *dload, const int32_t *dload_row_group,
                                 int64_t rows, int32_t n, int32_t k, float *dlogit, void *dsplit,
-                                const int32_t *split_row_index, cudaStream_t st, const struct ColumnSums *beside = nullptr);
-// beside: tile sums of a bias gradient, by blocks of their own in the same launch
+                                const int32_t *split_row_index, cudaStream_t st, const struct ColumnSums *beside = nullptr, const float *added = nullptr);
+// beside: tile sums of a bias gradient, by blocks of their own in the same launch; added [rows, n]: to dclean
 
 // ----------------------------------------------------------------------------- SIMT grouped GEMM (gemm_simt.cu)
 enum GemmType { G_F32 = 0, G_BF16 = 1 };

@@ -1,0 +1,601 @@
+// Newton-Schulz products of the Muon step (Jordan et al., 2024) on the 5th-generation tensor cores, for a batch of matrices X [rows, cols]. `steps` times
+//   A = X X'  (of the shorter side: X' X where there are more rows than columns),   B = a I + b A + c A A,   X <- B X  (X B)
+// and the last X goes straight from the accumulators into the weights: w = w - lr (scale X + decay w). M is the shorter side, N the longer one.
+//
+// Bound by the tensor cores: M^2 N + M^3 + 2 M^2 N operations a step and matrix, of A and B the lower half by tiles. A and B are symmetric, and what reads a tile of the upper half
+// reads the stored one in its place, transposed by the operand's major-ness, which an instruction has of its own.
+//
+// Operands are fp16, not bf16: a step multiplies small singular values by 3.4 and what rounding has put beside them too. X over its Frobenius norm and everything made of it stay
+// below 8 whatever the input, so that the range is known and fp16's three bits more are free: held times 2^10, elements down to 2^-24 are normal numbers. The diagonals of A and B are not
+// among the operands: they are kept in float, d and r, and enter the products' results beside the accumulators,
+//   A A = A' A' + A' (d_i + d_j) + d_i^2 [i = j],   B X = B' X + r X      (A', B' without their diagonals)
+// An element's rounding error off the diagonal is one of many in a singular value and averages out; on the diagonal it scales a whole row, and near the singular value 1.2 a step
+// multiplies such an error by 5 (a gate of 512 x 32, whose A is nearly diagonal, was off by 3e-3 with rounded diagonals). Accumulators are float, and the last X is not rounded at all.
+//
+// All products of all matrices are one launch: tiles are drawn one after the other in an order in which what a tile reads is always drawn before it (group of matrices, step, product,
+// matrix, tile), and a count of stored tiles for every matrix tells when it is there. With a group of matrices that fills the SMs more than once, what a tile waits for was stored long
+// ago. (A launch for every product leaves its last wave of tiles half empty: 3 tiles of A and B and 8 of X for each of 512 x 1024.) Whoever waits does so for tiles of blocks that run
+// already, so that no number of resident blocks is presumed.
+//
+// PAIR: two CTAs (an SM pair) have a tile of 256 x 256 by cta_group::2, each stages 128 rows of A's operand and half of B's columns. Otherwise, for M up to 128, a CTA has 128 x 128.
+// Warp 0 copies operands, warp 1 issues the products, warps 2 to 9 store results, warp 10 draws tiles. Every wait is bounded (2 s); on expiry the CTA records MOE_ERR_TIMEOUT
+// in the workspace's status word and drains.
+#include <string.h>
+
+#include "muon.cuh"
+#include "tc.cuh"
+
+namespace moe {
+
+namespace {
+
+constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
+constexpr int RING = 2;                       // tiles drawn ahead
+constexpr int NS_THREADS = 352;
+constexpr int NS_STAGES = 5;
+constexpr uint32_t BOX = 4096;                // a warp's 32 rows of 64 columns: what a result needs of the operand it is added to, then the result
+constexpr int NS_DATA = NS_STAGES * STAGE2_BYTES + 2 * 8 * BOX, NS_SMEM = NS_DATA + 1024 + 512;
+
+enum { FIRST = 0, SECOND = 1, THIRD = 2 };    // A, B, X
+struct NsMaps { CUtensorMap x_k[2], x_mn[2], x_box[2], a_k, a_mn, a_box, b_k, b_mn, b_box; };  // x[0]: all matrices, the others: a ring of slots
+struct NsArgs {
+    int32_t rows, cols, ld, M, Mld, matrices, steps, left;
+    int32_t square, cols3, tiles3;            // tiles of A and B (lower half), tiles of X beside each other, of X
+    int32_t group, slots, total;
+    int32_t *done, *next, *status;
+    float *d, *r;                             // [slots][M] diagonals of A and B
+    float lr;
+    const moe_muon_rates *rates;
+};
+struct NsTile { int32_t matrix, step, product, row, col; };
+
+template <bool PAIR> constexpr int tile_side() { return PAIR ? 256 : 128; }
+template <bool PAIR> constexpr int arrivals() { return PAIR ? 16 : 8; }  // of a stored tile: warps
+
+// Tile number `id`: {matrix or -1, step * 4 + product, row, column}
+template <bool PAIR> __device__ __forceinline__ int4 find_ns_tile(const NsArgs &p, int32_t id) {
+    if (id >= p.total) return make_int4(-1, 0, 0, 0);
+    const int32_t each = 2 * p.square + p.tiles3, per_group = p.group * p.steps * each;
+    const int32_t g = id / per_group, here = min(p.group, p.matrices - g * p.group);
+    int32_t r = id - g * per_group;
+    const int32_t step = r / (here * each);
+    r -= step * here * each;
+    int32_t product = FIRST, tiles = p.square;
+    if (r >= 2 * here * p.square) { product = THIRD; r -= 2 * here * p.square; tiles = p.tiles3; }
+    else if (r >= here * p.square) { product = SECOND; r -= here * p.square; }
+    const int32_t m = r / tiles;
+    int32_t t = r - m * tiles, row, col;
+    if (product == THIRD) {
+        row = t / p.cols3;
+        col = t - row * p.cols3;
+    } else {
+        for (row = 0; t > row; ++row) t -= row + 1;
+        col = t;
+    }
+    return make_int4(g * p.group + m, step * 4 + product, row * tile_side<PAIR>(), col * tile_side<PAIR>());
+}
+__device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
+    int32_t v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+// Arrivals that a matrix has when everything before this product is stored
+template <bool PAIR> __device__ __forceinline__ int32_t wanted(const NsArgs &p, const NsTile &t) {
+    return arrivals<PAIR>() * (t.step * (2 * p.square + p.tiles3) + t.product * p.square);
+}
+__device__ __forceinline__ bool wait_count(const int32_t *count, int32_t at_least, volatile int *abort_flag, int32_t *status) {
+    if (load_acquire(count) >= at_least) return true;
+    const unsigned long long t0 = global_ns();
+    while (load_acquire(count) < at_least) {
+        if (*abort_flag) return false;
+        if (global_ns() - t0 > WAIT_LIMIT_NS) {
+            *abort_flag = 1;
+            atomicExch(status, (int32_t)MOE_ERR_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+__device__ __forceinline__ void store_box_3d(const CUtensorMap *tm, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(tm), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+// As make_idesc, of fp16 operands
+__device__ __forceinline__ uint32_t idesc_of(bool pair, bool a_mn, bool b_mn, int n) {
+    return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)((pair ? 256 : 128) >> 4) << 24);
+}
+
+// Records of drawn tiles, read by every role. The reader's copy is in its registers before its report leaves: see the loads
+template <bool PAIR> struct NsRing {
+    const NsArgs &p;
+    const uint32_t ring, full0, empty0;
+    volatile int *abort_flag;
+    const bool warp_wide, arrives;
+    int i;
+    __device__ __forceinline__ bool next(NsTile &t) {
+        const uint32_t slot = (uint32_t)i % RING, par = ((uint32_t)i / RING) & 1u, full = full0 + 8u * slot;
+        bool ok = mbar_wait(full, par, abort_flag, p.status);
+        if (warp_wide) ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return false;
+        if (PAIR) mbar_try_wait_cluster(full, par);  // acquire at cluster scope: the record came from the other CTA's thread
+        int4 a;
+        asm volatile("ld.volatile.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w) : "r"(ring + 16u * slot) : "memory");
+        uint32_t seen = (uint32_t)a.w;  // (its sign bit is always 0: the report's address depends on the load)
+        if (warp_wide) seen = __reduce_or_sync(0xffffffffu, seen);
+        if (arrives) {
+            const uint32_t empty = empty0 + 8u * slot + ((seen >> 31) << 3);
+            if (PAIR) mbar_arrive_leader_relaxed(empty);
+            else mbar_arrive(empty);
+        }
+        ++i;
+        t.matrix = a.x; t.step = a.y >> 2; t.product = a.y & 3; t.row = a.z; t.col = a.w;
+        return a.x >= 0;
+    }
+};
+
+// 32 rows of 32 columns of the last X, which lie in `box` as floats, onto the weights: eight lanes a row, so that a row's 32 columns are read and written together
+template <bool BF16, bool MASTER, bool VECTORS>
+__device__ __forceinline__ void step_box(const NsArgs &p, const MuonEntry &e, int64_t first, int32_t rows_left, int32_t cols_left, const float *box, int lane, float lr) {
+    const int32_t c = (lane & 7) * 4;
+    float4 w[8];
+    auto at = [&](int i) { return first + (int64_t)(4 * i + (lane >> 3)) * p.cols + c; };
+    auto in = [&](int i) { return 4 * i + (lane >> 3) < rows_left && c < cols_left; };
+    const float *floats = MASTER ? e.master : static_cast<const float *>(e.w);
+    bf16 *halves = static_cast<bf16 *>(e.w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        w[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (!in(i)) continue;
+        if constexpr (VECTORS) {
+            if constexpr (!BF16 || MASTER) w[i] = *reinterpret_cast<const float4 *>(floats + at(i));
+            else {
+                const uint2 u = *reinterpret_cast<const uint2 *>(halves + at(i));
+                w[i] = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+            }
+        } else {
+            float *to = reinterpret_cast<float *>(&w[i]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (c + q < cols_left) to[q] = !BF16 || MASTER ? floats[at(i) + q] : to_f32(halves[at(i) + q]);
+        }
+    }
+    const float by = e.scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int32_t r = 4 * i + (lane >> 3);
+        const float4 x = *reinterpret_cast<const float4 *>(box + r * 32 + (((lane & 7) ^ (r & 7)) << 2));
+        w[i].x -= lr * fmaf(x.x, by, e.decay * w[i].x);
+        w[i].y -= lr * fmaf(x.y, by, e.decay * w[i].y);
+        w[i].z -= lr * fmaf(x.z, by, e.decay * w[i].z);
+        w[i].w -= lr * fmaf(x.w, by, e.decay * w[i].w);
+        if (!in(i)) continue;
+        float *to = MASTER ? e.master : static_cast<float *>(e.w);
+        if constexpr (VECTORS) {
+            if constexpr (!BF16 || MASTER) *reinterpret_cast<float4 *>(to + at(i)) = w[i];
+            if constexpr (BF16) {
+                const __nv_bfloat162 a = __floats2bfloat162_rn(w[i].x, w[i].y), b = __floats2bfloat162_rn(w[i].z, w[i].w);
+                *reinterpret_cast<uint2 *>(halves + at(i)) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+            }
+        } else {
+            const float *v = reinterpret_cast<const float *>(&w[i]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (c + q >= cols_left) break;
+                if constexpr (!BF16 || MASTER) to[at(i) + q] = v[q];
+                if constexpr (BF16) halves[at(i) + q] = __float2bfloat16_rn(v[q]);
+            }
+        }
+    }
+}
+
+template <bool PAIR>
+__global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsArgs p, const __grid_constant__ MuonBatch batch) {
+    constexpr int SIDE = tile_side<PAIR>(), NST = NS_STAGES, STAGE = STAGE2_BYTES, ACC = SIDE;  // ACC: columns of an accumulator
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t bars = base + NS_DATA;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (NST + s); };
+    auto tfull_bar = [&](int a) { return bars + 8u * (2 * NST + a); };
+    auto tempty_bar = [&](int a) { return bars + 8u * (2 * NST + 2 + a); };
+    const uint32_t ring_full0 = bars + 128, ring_empty0 = bars + 160, ring = bars + 256, box_bar0 = bars + 320;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + NS_DATA + 192);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + NS_DATA + 200);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < NST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), arrivals<PAIR>()); }
+        // readers of a record: producer and 8 epilogue warps in each CTA, the MMA warp of the even one
+        for (int q = 0; q < RING; ++q) { mbar_init(ring_full0 + 8u * q, 1); mbar_init(ring_empty0 + 8u * q, PAIR ? 19 : 10); }
+        for (int q = 0; q < 16; ++q) mbar_init(box_bar0 + 8u * q, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)), "r"((uint32_t)TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)), "r"((uint32_t)TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();  // both CTAs' barriers exist before anything is signalled across the pair
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    wait_previous_kernel();
+
+    const int kblocks1 = ((p.left ? p.cols : p.rows) + BK - 1) / BK, kblocks2 = (p.M + BK - 1) / BK;
+    auto kblocks_of = [&](const NsTile &t) { return t.product == FIRST ? kblocks1 : kblocks2; };
+    // columns that exist of a tile's output, and of the product (both CTAs' halves of B's operand begin at multiples of 64)
+    auto cols_out = [&](const NsTile &t) { return t.product == THIRD ? p.ld : p.Mld; };
+    auto width_of = [&](const NsTile &t) { return PAIR && cols_out(t) - t.col > 128 ? 256 : 128; };
+    // Where an operand lies in a product whose contraction runs along the shorter side: block kb of it is in the lower half for rows from `at` on, or has to be transposed
+    auto upper = [&](int kb, int32_t at) { return kb * BK / SIDE > at / SIDE; };
+    auto a_is_mn = [&](const NsTile &t, int kb) { return t.product == FIRST ? !p.left : t.product == THIRD && !p.left ? false : upper(kb, t.row); };
+    auto b_is_mn = [&](const NsTile &t, int kb) { return t.product == FIRST ? !p.left : t.product == THIRD && p.left ? true : upper(kb, t.col); };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ bulk tensor copies (both CTAs)
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, false, true, 0};
+            NsTile t;
+            while (ok && tiles.next(t)) {
+                ok = wait_count(p.done + t.matrix, wanted<PAIR>(p, t), abort_flag, p.status);
+                if (ok && t.step == 0 && t.product == FIRST && t.matrix >= p.slots)  // the slot's last user has read what is overwritten now
+                    ok = wait_count(p.done + t.matrix - p.slots, arrivals<PAIR>() * p.steps * (2 * p.square + p.tiles3), abort_flag, p.status);
+                if (!ok) break;
+                fence_async();  // what other SMs' copies have stored, before this thread's copies read it
+                const int slot = t.matrix % p.slots, x = t.step & 1, xm = x ? slot : t.matrix;
+                const bool a_x = t.product == FIRST || (t.product == THIRD && !p.left), b_x = t.product == FIRST || (t.product == THIRD && p.left);
+                const CUtensorMap *sym_k = t.product == SECOND ? &maps.a_k : &maps.b_k, *sym_mn = t.product == SECOND ? &maps.a_mn : &maps.b_mn;
+                const CUtensorMap *ak = a_x ? &maps.x_k[x] : sym_k, *an = a_x ? &maps.x_mn[x] : sym_mn, *bk = b_x ? &maps.x_k[x] : sym_k, *bn = b_x ? &maps.x_mn[x] : sym_mn;
+                const int am = a_x ? xm : slot, bm = b_x ? xm : slot;
+                const int a0 = t.row + 128 * (int)rank, b0 = t.col + (PAIR ? width_of(t) / 2 * (int)rank : 0);
+                const int kblocks = kblocks_of(t);
+                for (int kb = 0; kb < kblocks; ++kb) {
+                    ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.status);
+                    if (!ok) break;
+                    if (rank == 0) mbar_expect_tx(full_bar(s), PAIR ? 2 * STAGE : STAGE);
+                    auto load = [&](uint32_t dst, bool mn, const CUtensorMap *k_map, const CUtensorMap *mn_map, int at, int matrix) {
+                        if (mn) {
+                            if (PAIR) tma2_load_4d(dst, mn_map, full_bar(s), 0, kb * BK, at / 64, matrix);
+                            else tma_load_4d(dst, mn_map, full_bar(s), 0, kb * BK, at / 64, matrix);
+                        } else {
+                            if (PAIR) tma2_load_3d(dst, k_map, full_bar(s), kb * BK, at, matrix);
+                            else tma_load_3d(dst, k_map, full_bar(s), kb * BK, at, matrix);
+                        }
+                    };
+                    load(base + s * STAGE, a_is_mn(t, kb), ak, an, a0, am);
+                    load(base + s * STAGE + A2_BYTES, b_is_mn(t, kb), bk, bn, b0, bm);
+                    if (++s == NST) { s = 0; ph ^= 1u; }
+                }
+            }
+            // gave up: copies in flight have landed long before a millisecond is over, and only then may the CTA exit
+            if (!ok)
+                for (const unsigned long long t0 = global_ns(); global_ns() - t0 < 1000000ull;) {}
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer (one thread, even CTA only)
+        if (rank == 0 && lane == 0) {
+            int s = 0, acc = 0;
+            uint32_t ph = 0, acc_ph = 0;
+            bool ok = true;
+            NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, false, true, 0};
+            NsTile t;
+            while (ok && tiles.next(t)) {
+                ok = mbar_wait(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.status);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + acc * ACC;
+                const int kblocks = kblocks_of(t), width = width_of(t);
+                for (int kb = 0; kb < kblocks; ++kb) {
+                    ok = mbar_wait(full_bar(s), ph, abort_flag, p.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const bool a_mn = a_is_mn(t, kb), b_mn = b_is_mn(t, kb);
+                    const uint32_t a_src = base + s * STAGE, b_src = a_src + A2_BYTES, idesc = idesc_of(PAIR, a_mn, b_mn, width);
+                    const uint64_t ad = a_mn ? desc_mnmajor(a_src) : desc_kmajor(a_src), bd = b_mn ? desc_mnmajor(b_src) : desc_kmajor(b_src);
+                    const uint64_t a_step = a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = b_mn ? (16 * 128) >> 4 : 32 >> 4;
+#pragma unroll
+                    for (int k = 0; k < BK / 16; ++k) {
+                        if (PAIR) tc_mma2_bf16(d_tmem, ad + k * a_step, bd + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                        else tc_mma_bf16(d_tmem, ad + k * a_step, bd + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                    }
+                    if (PAIR) tc_commit2(empty_bar(s));
+                    else tc_commit(empty_bar(s));
+                    if (++s == NST) { s = 0; ph ^= 1u; }
+                }
+                if (!ok) break;
+                if (PAIR) tc_commit2(tfull_bar(acc));
+                else tc_commit(tfull_bar(acc));
+                if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+            }
+        }
+    } else if (warp == 10) {
+        // ------------------------------------------------------------------ drawing tiles (even CTA, one thread)
+        if (rank == 0 && lane == 0) {
+            const uint32_t peer_ring = PAIR ? peer_smem_addr(ring, 1) : 0u, peer_full0 = PAIR ? peer_smem_addr(ring_full0, 1) : 0u;
+            for (int i = 0;; ++i) {
+                const uint32_t slot = (uint32_t)i % RING;
+                if (i >= RING) {  // every reader of the record this slot held has its copy
+                    const uint32_t par = ((uint32_t)i / RING - 1) & 1u;
+                    if (!mbar_wait(ring_empty0 + 8u * slot, par, abort_flag, p.status)) break;
+                    if (PAIR) mbar_try_wait_cluster(ring_empty0 + 8u * slot, par);
+                }
+                const int4 a = find_ns_tile<PAIR>(p, atomicAdd(p.next, 1));
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ring + 16u * slot), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
+                if (PAIR) st_cluster_v4(peer_ring + 16u * slot, a);
+                mbar_arrive(ring_full0 + 8u * slot);
+                if (PAIR) mbar_arrive_cluster_addr(peer_full0 + 8u * slot);
+                if (a.x < 0) break;
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue (warps 2..9, both CTAs)
+        // Two warps share each quarter of the accumulator's rows and take half of its columns each, in boxes of 64.
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        uint8_t *boxes_at = smem + NST * STAGE + (warp - 2) * 2 * BOX;
+        const uint32_t box_bar = box_bar0 + 16u * (warp - 2);
+        const float lr = p.rates ? p.rates->lr : p.lr;
+        int acc = 0;
+        uint32_t acc_ph = 0, box_ph[2] = {0, 0};
+        NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, true, lane == 0, 0};
+        NsTile t;
+        bool ok = true;
+        while (ok && tiles.next(t)) {
+            const int32_t row0 = t.row + 128 * (int)rank + 32 * quarter, first = t.col + half * (width_of(t) / 2), row = row0 + lane;
+            const int32_t rows_out = t.product == THIRD ? p.rows : p.M;
+            const bool last = t.product == THIRD && t.step + 1 == p.steps;
+            const int boxes = row0 < rows_out ? max(0, min(width_of(t) / 128, (cols_out(t) - first) / 64)) : 0;
+            const int slot = t.matrix % p.slots, x = t.step & 1;
+            // What the result is added to, box by box, is on its way while the products run: A' or X as it was
+            if (t.product != FIRST) {
+                ok = wait_count(p.done + t.matrix, wanted<PAIR>(p, t), abort_flag, p.status);  // (the copying thread has seen it, and this one has to)
+                if (ok && lane == 0) {
+                    fence_async();
+                    for (int u = 0; u < boxes; ++u) {
+                        mbar_expect_tx(box_bar + 8u * u, BOX);
+                        tma_load_3d(smem_u32(boxes_at + u * BOX), t.product == SECOND ? &maps.a_box : &maps.x_box[x], box_bar + 8u * u, first + 64 * u, row0,
+                                    t.product == THIRD && !x ? t.matrix : slot);
+                    }
+                }
+            }
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.status));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t mine = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * ACC + half * (width_of(t) / 2);
+            auto release = [&]() {  // the warp's part of the accumulator is in registers: the buffer goes back
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) mbar_arrive_leader_relaxed(tempty_bar(acc));
+                    else mbar_arrive(tempty_bar(acc));
+                }
+            };
+            float *d = p.d + (int64_t)slot * p.M, *r = p.r + (int64_t)slot * p.M;
+            // of this lane's row: SECOND d_i, THIRD r_i (X has rows of B)
+            const float of_row = t.product == FIRST || row >= p.M || (t.product == THIRD && !p.left) ? 0.0f : __ldcg((t.product == SECOND ? d : r) + row);
+            const float *of_cols = t.product == SECOND ? d : t.product == THIRD && !p.left ? r : nullptr;
+#pragma unroll 1
+            for (int u = 0; u < boxes; ++u) {
+                const int32_t col = first + 64 * u;
+                uint8_t *box = boxes_at + u * BOX;
+                uint32_t v[2][32];
+                tc_ld_32x32(mine + 64 * u, v[0]);
+                tc_ld_32x32(mine + 64 * u + 32, v[1]);
+                if (t.product != FIRST) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(box_bar + 8u * u, box_ph[u], abort_flag, p.status));
+                    box_ph[u] ^= 1u;
+                }
+                tc_ld_wait();
+                if (u + 1 == boxes) release();
+                if (!ok) break;
+                const bool diagonal = t.product != THIRD && row >= col && row < col + 64 && row < p.M;
+                const float by = last ? 1.0f / (MUON_UNIT * MUON_UNIT) : 1.0f / MUON_UNIT;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    uint4 *place = reinterpret_cast<uint4 *>(box + lane * 128 + ((q ^ (lane & 7)) << 4));
+                    uint4 old = make_uint4(0u, 0u, 0u, 0u);
+                    if (t.product != FIRST) old = *place;
+                    float cs[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) cs[j] = of_row;
+                    if (of_cols)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) cs[j] += col + 8 * q + j < p.M ? __ldcg(of_cols + col + 8 * q + j) : 0.0f;
+                    if (t.product == SECOND)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) cs[j] = fmaf(NS_C, cs[j], NS_B);
+                    const uint32_t *raw = reinterpret_cast<const uint32_t *>(&old);
+                    uint32_t packed[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = 8 * q + 2 * j;
+                        float2 y = make_float2(__uint_as_float(v[at >> 5][at & 31]), __uint_as_float(v[at >> 5][(at & 31) + 1]));
+                        if (diagonal && (at == row - col || at + 1 == row - col)) {  // kept in float; no part of the operand
+                            float &own = at == row - col ? y.x : y.y;
+                            const float sum = own * (1.0f / (MUON_UNIT * MUON_UNIT));
+                            if (t.product == FIRST) d[row] = sum;
+                            else r[row] = fmaf(NS_C, fmaf(of_row, of_row, sum), fmaf(NS_B, of_row, NS_A));
+                            own = 0.0f;  // (and A' has a zero here)
+                        }
+                        const float2 o = __half22float2(*reinterpret_cast<const __half2 *>(&raw[j]));
+                        const float unit = t.product == SECOND ? NS_C / MUON_UNIT : by, scale = last ? 1.0f / MUON_UNIT : 1.0f;
+                        y.x = fmaf(y.x, unit, o.x * (cs[2 * j] * scale));
+                        y.y = fmaf(y.y, unit, o.y * (cs[2 * j + 1] * scale));
+                        if (last) {
+                            v[at >> 5][at & 31] = __float_as_uint(y.x);
+                            v[at >> 5][(at & 31) + 1] = __float_as_uint(y.y);
+                        } else {
+                            const __half2 h = __floats2half2_rn(y.x, y.y);
+                            packed[j] = *reinterpret_cast<const uint32_t *>(&h);
+                        }
+                    }
+                    if (!last) *place = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+                }
+                if (last) {
+                    const int32_t i = batch.entry_of(t.matrix);
+                    const MuonEntry &e = batch.t[i];
+                    const int64_t in_entry = (int64_t)(t.matrix - batch.first[i]) * p.rows * p.cols;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (col + 32 * j >= p.cols) break;
+                        __syncwarp();
+                        float *floats = reinterpret_cast<float *>(box);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            *reinterpret_cast<uint4 *>(floats + lane * 32 + ((q ^ (lane & 7)) << 2)) = make_uint4(v[j][4 * q], v[j][4 * q + 1], v[j][4 * q + 2], v[j][4 * q + 3]);
+                        __syncwarp();
+                        const int64_t at = in_entry + (int64_t)row0 * p.cols + col + 32 * j;
+                        const int32_t rl = p.rows - row0, cl = p.cols - col - 32 * j;
+                        const bool vectors = p.cols % 4 == 0;
+                        if (e.kind & 8) vectors ? step_box<true, true, true>(p, e, at, rl, cl, floats, lane, lr) : step_box<true, true, false>(p, e, at, rl, cl, floats, lane, lr);
+                        else if (e.kind & 1) vectors ? step_box<true, false, true>(p, e, at, rl, cl, floats, lane, lr) : step_box<true, false, false>(p, e, at, rl, cl, floats, lane, lr);
+                        else vectors ? step_box<false, false, true>(p, e, at, rl, cl, floats, lane, lr) : step_box<false, false, false>(p, e, at, rl, cl, floats, lane, lr);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the box is copied into again
+                    continue;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    const CUtensorMap *out = t.product == FIRST ? &maps.a_box : t.product == SECOND ? &maps.b_box : &maps.x_box[x ^ 1];
+                    store_box_3d(out, smem_u32(box), col, row0, t.product == THIRD && x ? t.matrix : slot);
+                    tma_store_commit();
+                }
+            }
+            if (boxes == 0) release();
+            if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_wait_all();
+                fence_async();
+                asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + t.matrix) : "memory");
+            }
+            __syncwarp();
+        }
+        if (!ok)  // gave up, see above
+            for (const unsigned long long t0 = global_ns(); global_ns() - t0 < 1000000ull;) {}
+        if (lane == 0) tma_store_wait_all();  // no bulk store may outlive the CTA's shared memory
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();  // the pair's MMAs read both CTAs' shared memory: leave together
+    if (warp == 1) {
+        tc_fence_after();
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------------------------------ host
+struct NsPlan {
+    bool pair;
+    int32_t square, rows3, cols3;
+    int64_t M, Mld, ld, group, slots;
+};
+NsPlan plan_of(int32_t rows, int32_t cols, int64_t matrices) {
+    NsPlan q;
+    q.M = imin(rows, cols);
+    q.Mld = muon_ld(q.M);
+    q.ld = muon_ld(cols);
+    q.pair = q.M > 128;
+    const int side = q.pair ? 256 : 128;
+    const int64_t s = cdiv(q.M, side);
+    q.square = (int32_t)(s * (s + 1) / 2);
+    q.rows3 = (int32_t)cdiv(rows, side);
+    q.cols3 = (int32_t)cdiv(cols, side);
+    // as many matrices as give every SM pair (SM) more than one tile of A
+    q.group = imin(matrices, cdiv(5 * (q.pair ? 74 : 148), 4 * (int64_t)q.square));
+    q.slots = imin(matrices, 2 * q.group);
+    return q;
+}
+struct NsScratch { __half *x, *a, *b; float *d, *r; };
+NsScratch ns_scratch(Carver &cv, const NsPlan &q, int64_t rows) {
+    NsScratch s;
+    s.x = cv.take<__half>(q.slots * rows * q.ld);
+    s.a = cv.take<__half>(q.slots * q.M * q.Mld);
+    s.b = cv.take<__half>(q.slots * q.M * q.Mld);
+    s.d = cv.take<float>(q.slots * q.M);
+    s.r = cv.take<float>(q.slots * q.M);
+    return s;
+}
+// [count][rows][ld] halves: boxes of 64 columns x 128 rows, of 64 rows x two pieces of 64 columns, and the epilogue's of 64 columns x 32 rows
+int32_t maps_of(const __half *at, int64_t count, int64_t rows, int64_t ld, CUtensorMap *k, CUtensorMap *mn, CUtensorMap *box32) {
+    const uint64_t dims[3] = {(uint64_t)ld, (uint64_t)rows, (uint64_t)count}, str[2] = {(uint64_t)ld * 2, (uint64_t)(rows * ld) * 2};
+    const uint32_t box[3] = {64, 128, 1}, box_out[3] = {64, 32, 1};
+    MOE_TRY(tc_make_map(k, at, 3, dims, str, box));
+    MOE_TRY(tc_make_map(box32, at, 3, dims, str, box_out));
+    const uint64_t dims4[4] = {64, (uint64_t)rows, (uint64_t)(ld / 64), (uint64_t)count}, str4[3] = {(uint64_t)ld * 2, 128, (uint64_t)(rows * ld) * 2};
+    const uint32_t box4[4] = {64, BK, 2, 1};
+    return tc_make_map(mn, at, 4, dims4, str4, box4);
+}
+
+template <bool PAIR> int32_t launch_ns(const NsMaps &maps, const NsArgs &p, const MuonBatch &batch, cudaStream_t st) {
+    static PerDevice most;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // as launch_kernel
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = 2; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
+    cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM; cfg.stream = st;
+    cfg.attrs = attrs; cfg.numAttrs = PAIR ? 2 : 1;
+    const auto kernel = newton_schulz_kernel<PAIR>;
+    const int workers = most.get([&]() {
+        if (cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess) return 0;
+        if (!PAIR) return tc_sm_count();
+        int n = 0;
+        cfg.gridDim = dim3(2 * (tc_sm_count() / 2));
+        return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
+    });
+    if (workers <= 0) return MOE_ERR_CUDA;
+    cfg.gridDim = dim3((PAIR ? 2 : 1) * (unsigned)imin(p.total, workers));
+    MOE_CUDA(cudaLaunchKernelEx(&cfg, kernel, maps, p, batch));
+    MOE_LAUNCHED();
+    return MOE_OK;
+}
+
+}  // namespace
+
+int64_t ns_scratch_bytes(int32_t rows, int32_t cols, int64_t matrices) {
+    Carver cv(nullptr);
+    ns_scratch(cv, plan_of(rows, cols, matrices), rows);
+    return (int64_t)cv.off;
+}
+
+int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st) {
+    const int32_t rows = w.batch->rows, cols = w.batch->cols;
+    const NsPlan q = plan_of(rows, cols, w.matrices);
+    Carver cv(w.scratch);
+    const NsScratch s = ns_scratch(cv, q, rows);
+    NsMaps maps;
+    MOE_TRY(maps_of(w.x, w.matrices, rows, q.ld, &maps.x_k[0], &maps.x_mn[0], &maps.x_box[0]));
+    MOE_TRY(maps_of(s.x, q.slots, rows, q.ld, &maps.x_k[1], &maps.x_mn[1], &maps.x_box[1]));
+    MOE_TRY(maps_of(s.a, q.slots, q.M, q.Mld, &maps.a_k, &maps.a_mn, &maps.a_box));
+    MOE_TRY(maps_of(s.b, q.slots, q.M, q.Mld, &maps.b_k, &maps.b_mn, &maps.b_box));
+    NsArgs p = {};
+    p.rows = rows; p.cols = cols; p.ld = (int32_t)q.ld; p.M = (int32_t)q.M; p.Mld = (int32_t)q.Mld;
+    p.matrices = w.matrices; p.steps = w.steps; p.left = rows <= cols;
+    p.square = q.square; p.cols3 = q.cols3; p.tiles3 = q.rows3 * q.cols3;
+    p.group = (int32_t)q.group; p.slots = (int32_t)q.slots;
+    const int64_t total = (int64_t)w.matrices * w.steps * (2 * (int64_t)p.square + p.tiles3);
+    if (total > (int64_t)1 << 30) return MOE_ERR_UNSUPPORTED;
+    p.total = (int32_t)total;
+    p.done = w.done; p.next = w.next; p.status = w.status; p.d = s.d; p.r = s.r; p.lr = w.lr; p.rates = w.rates;
+    return q.pair ? launch_ns<true>(maps, p, *w.batch, st) : launch_ns<false>(maps, p, *w.batch, st);
+}
+
+}  // namespace moe
