@@ -15,29 +15,43 @@ namespace moe {
 
 namespace {
 
-constexpr int FORWARD_STAGES = 3;  // rows of a team on their way or in work
+// Rows of a team on their way or in work (131072 x 1024 forward with 2, 3, 4 of them: 94.2, 95.9, 97.1 us; backward of 65536 x 1024 with 2, 3, 4: 85.8, 86.2, 87.0)
+constexpr int STAGES = 2;
 
-// N sums over the threads of a team at once: in the first steps lanes give away half of their sums, so that eight sums take nine exchanges and not forty. Lane l is left with
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return fma2(a, both(1.0f), b); }
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    return v;
+}
+// N sums over the threads of a team at once: in the first steps lanes give away half of their sums, so that four sums take seven exchanges and not twenty. Lane l is left with
 // sum l / (32 / N). `sh` has a place per warp and sum, twice: who writes the next sums does so on the other side, and the barrier of those keeps it from coming round.
-template <int N> __device__ __forceinline__ void sums_of_team(float (&s)[N], int warps, float *sh, int &side) {
+template <int N, bool ONE> __device__ __forceinline__ void sums_of_team(float (&s)[N], int warps, float *sh, int &side) {
     const int lane = threadIdx.x & 31;
-    int off = 16;
+    float t;
+    if constexpr (N == 1) {
+        t = warp_sum(s[0]);
+    } else {
+        int off = 16;
 #pragma unroll
-    for (int m = N / 2; m >= 1; m >>= 1, off >>= 1) {
-        const bool up = lane & off;
+        for (int m = N / 2; m >= 1; m >>= 1, off >>= 1) {
+            const bool up = lane & off;
 #pragma unroll
-        for (int i = 0; i < m; ++i) {
-            const float keep = up ? s[i + m] : s[i], send = up ? s[i] : s[i + m];
-            s[i] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+            for (int i = 0; i < m; ++i) {
+                const float keep = up ? s[i + m] : s[i], send = up ? s[i] : s[i + m];
+                s[i] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+            }
         }
+        t = s[0];
+#pragma unroll
+        for (; off >= 1; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
     }
-    float t = s[0];
-#pragma unroll
-    for (; off >= 1; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
     constexpr int EACH = 32 / N;  // lanes of a sum
-    if (warps == 1) {
+    if constexpr (ONE) {
+        if constexpr (N == 1) s[0] = t;
+        else
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = __shfl_sync(0xffffffffu, t, i * EACH);
+            for (int i = 0; i < N; ++i) s[i] = __shfl_sync(0xffffffffu, t, i * EACH);
         return;
     }
     const int warp = threadIdx.x >> 5, team = warp / warps;
@@ -47,101 +61,125 @@ template <int N> __device__ __forceinline__ void sums_of_team(float (&s)[N], int
     asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = 0.0f;
-    for (int q = team * warps; q < (team + 1) * warps; ++q)
+    const float *q = mine + team * warps * N;
+    for (int w = 0; w < warps; ++w, q += N) {
+        if constexpr (N % 4 == 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] += mine[q * N + i];
-}
-
-// The weights of a thread's columns: in registers, or where a thread has more than two vectors of each row read when they are wanted
-template <typename T, int V> struct Weights {
-    static constexpr int P = Vec<T>::N / 2;
-    static constexpr bool HELD = V <= 2;
-    const float *at;
-    float2 held[HELD ? V : 1][P];
-    __device__ __forceinline__ Weights(const float *p, int first, int step, int pieces) : at(p) {
-        if constexpr (HELD)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-#pragma unroll
-                for (int i = 0; i < P; ++i) held[v][i] = both(0.0f);
-                if (p && first + v * step < pieces) load_floats<P>(p + (int64_t)(first + v * step) * Vec<T>::N, held[v]);
+            for (int i = 0; i < N; i += 4) {
+                const float4 f = *reinterpret_cast<const float4 *>(q + i);
+                s[i] += f.x; s[i + 1] += f.y; s[i + 2] += f.z; s[i + 3] += f.w;
             }
-    }
-    __device__ __forceinline__ void get(int v, int q, float2 (&w)[P]) const {  // of vector q, the thread's v-th
-        if constexpr (HELD) {
-#pragma unroll
-            for (int i = 0; i < P; ++i) w[i] = held[v][i];
+        } else if constexpr (N == 2) {
+            const float2 f = *reinterpret_cast<const float2 *>(q);
+            s[0] += f.x; s[1] += f.y;
         } else {
-#pragma unroll
-            for (int i = 0; i < P; ++i) w[i] = both(0.0f);
-            if (at) load_floats<P>(at + (int64_t)q * Vec<T>::N, w);
+            s[0] += *q;
         }
     }
-};
+}
 
-template <typename T, int V, int K, int THREADS, int BLOCKS>
+// Where a thread's vectors lie. Everything that a row or a stage further on needs is an addition.
+template <typename T, int V> struct Places {
+    int64_t first;        // bytes: row 0 of the team, the thread's first vector
+    int64_t row_bytes;
+    int32_t v_bytes;      // between the thread's vectors of a row
+    bool in[V];           // which of them there are
+    __device__ __forceinline__ Places(int32_t d, int lane, int threads) {
+        const int32_t pieces = d / Vec<T>::N;
+        first = 16 * (int64_t)lane;
+        row_bytes = (int64_t)d * sizeof(T);
+        v_bytes = 16 * threads;
+#pragma unroll
+        for (int v = 0; v < V; ++v) in[v] = lane + v * threads < pieces;
+    }
+};
+template <typename T, int V> __device__ __forceinline__ void load_weights(const float *p, int lane, int threads, const Places<T, V> &at, float2 (&w)[V][Vec<T>::N / 2]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+        for (int i = 0; i < Vec<T>::N / 2; ++i) w[v][i] = both(0.0f);
+        if (p && at.in[v]) load_floats(p + (int64_t)(lane + v * threads) * Vec<T>::N, w[v]);
+    }
+}
+
+// ONE: a row is one warp's
+template <typename T, int V, int K, int THREADS, int BLOCKS, bool ONE>
 __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_kernel(const LayerNormArgs a, int warps) {
     constexpr int N = Vec<T>::N, P = N / 2;
-    extern __shared__ uint4 ring[];  // [stage][row of K][vector of V][thread]
-    __shared__ float sh[2 * 16 * K];
+    extern __shared__ uint4 ring[];  // [stage][row of K][vector of V][thread of THREADS]
+    __shared__ __align__(16) float sh[2 * 16 * K];
     int side = 0;
-    const int threads = warps * 32, teams = blockDim.x / threads, lane = threadIdx.x % threads, wide = blockDim.x;
-    const int32_t pieces = a.d / N;
+    const int threads = ONE ? 32 : warps * 32, teams = blockDim.x / threads, lane = threadIdx.x % threads;
     const float by = 1.0f / (float)a.d;
     const int64_t step = (int64_t)gridDim.x * teams * K;
     int64_t row = ((int64_t)blockIdx.x * teams + threadIdx.x / threads) * K;
-    const Weights<T, V> w(a.w, lane, threads, pieces), b(a.b, lane, threads, pieces);
+    const Places<T, V> at(a.d, lane, threads);
+    float2 w[V][P], b[V][P];
+    load_weights<T, V>(a.w, lane, threads, at, w);
+    load_weights<T, V>(a.b, lane, threads, at, b);
     wait_previous_kernel();
-    auto place = [&](int stage, int k, int v) { return ring + ((stage * K + k) * V + v) * wide + threadIdx.x; };
-    auto fetch = [&](int stage, int64_t first) {
+    const char *from = static_cast<const char *>(a.x) + at.first + row * at.row_bytes;
+    char *to = static_cast<char *>(a.xn) + at.first + row * at.row_bytes;
+    const int64_t step_bytes = step * at.row_bytes;
+    int64_t ahead = row;  // the rows that are fetched next
+    auto fetch = [&](int stage) {
+        if (ahead < a.T) {
+            const char *p = from;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k, p += at.row_bytes)
+                if (k == 0 || ahead + k < a.T)
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (first + k < a.T && lane + v * threads < pieces)
-                    copy16(place(stage, k, v), static_cast<const T *>(a.x) + (first + k) * a.d + (int64_t)(lane + v * threads) * N);
+                    for (int v = 0; v < V; ++v)
+                        if (at.in[v]) copy16(ring + ((stage * K + k) * V + v) * THREADS + threadIdx.x, p + v * at.v_bytes);
+        }
         copies_commit();
+        from += step_bytes;
+        ahead += step;
     };
 #pragma unroll
-    for (int s = 0; s < FORWARD_STAGES - 1; ++s) fetch(s, row + s * step);
+    for (int s = 0; s < STAGES - 1; ++s) fetch(s);
     int stage = 0;
-    for (; row < a.T; row += step) {
-        fetch(stage == 0 ? FORWARD_STAGES - 1 : stage - 1, row + (FORWARD_STAGES - 1) * step);
-        copies_wait<FORWARD_STAGES - 1>();
-        Vec<T> x[K][V];
-        float s[K];
+    for (; row < a.T; row += step, to += step_bytes) {
+        fetch(stage == 0 ? STAGES - 1 : stage - 1);
+        copies_wait<STAGES - 1>();
+        float2 x[K][V][P];
+        float s[K], mean[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             float2 sum = both(0.0f);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                x[k][v].raw = make_uint4(0u, 0u, 0u, 0u);
-                if (lane + v * threads < pieces && row + k < a.T) x[k][v].raw = *place(stage, k, v);
+                Vec<T> raw;
+                raw.raw = make_uint4(0u, 0u, 0u, 0u);
+                if (at.in[v] && (k == 0 || row + k < a.T)) raw.raw = ring[((stage * K + k) * V + v) * THREADS + threadIdx.x];
 #pragma unroll
-                for (int i = 0; i < P; ++i) sum = fma2(x[k][v].get(2 * i), both(1.0f), sum);
+                for (int i = 0; i < P; ++i) {
+                    x[k][v][i] = raw.get(2 * i);
+                    sum = add2(x[k][v][i], sum);
+                }
             }
             s[k] = sum.x + sum.y;
         }
-        sums_of_team<K>(s, warps, sh, side);
-        float mean[K];
+        sums_of_team<K, ONE>(s, warps, sh, side);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             mean[k] = s[k] * by;
             float2 sum = both(0.0f);
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                if (lane + v * threads < pieces)
 #pragma unroll
-                    for (int i = 0; i < P; ++i) {
-                        const float2 off = fma2(x[k][v].get(2 * i), both(1.0f), both(-mean[k]));
-                        sum = fma2(off, off, sum);
-                    }
+                for (int i = 0; i < P; ++i) {
+                    x[k][v][i] = add2(x[k][v][i], both(-mean[k]));
+                    if (!at.in[v]) x[k][v][i] = both(0.0f);
+                    sum = fma2(x[k][v][i], x[k][v][i], sum);
+                }
             s[k] = sum.x + sum.y;
         }
-        sums_of_team<K>(s, warps, sh, side);
+        sums_of_team<K, ONE>(s, warps, sh, side);
+        char *out = to;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (row + k >= a.T) break;
+        for (int k = 0; k < K; ++k, out += at.row_bytes) {
+            if (k > 0 && row + k >= a.T) break;
             const float r = 1.0f / sqrtf(s[k] * by + a.eps);
             if (lane == 0) {
                 if (a.mean) a.mean[row + k] = mean[k];
@@ -149,52 +187,73 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_kernel(const Layer
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int q = lane + v * threads;
-                if (q >= pieces) break;
-                float2 wv[P], bv[P];
-                w.get(v, q, wv);
-                b.get(v, q, bv);
+                if (!at.in[v]) break;
                 Vec<T> o;
 #pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const float2 off = fma2(x[k][v].get(2 * i), both(1.0f), both(-mean[k]));
-                    o.set(2 * i, fma2(mul2(off, both(r)), wv[i], bv[i]));
-                }
-                store_vec<T>(a.xn, row + k, a.d, q, o);
+                for (int i = 0; i < P; ++i) o.set(2 * i, fma2(mul2(x[k][v][i], both(r)), w[v][i], b[v][i]));
+                *reinterpret_cast<uint4 *>(out + v * at.v_bytes) = o.raw;
             }
         }
-        stage = stage + 1 == FORWARD_STAGES ? 0 : stage + 1;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
 }
 
-// Backward. Every thread adds up dxn n and dxn of its columns; at the end the block's teams are added up and its sums written.
-template <typename T, int V, int K, int THREADS, int BLOCKS, int STAGES>
+// Backward. Every thread adds up dxn n and dxn of its columns; at the end the block's teams are added up and its sums written. HELD: weights in registers; else, in the widest rows, read
+// when they are wanted.
+template <typename T, int V, int K, int THREADS, int BLOCKS, int S, bool ONE, bool RES, bool HELD>
 __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const LayerNormGradArgs a, int warps) {
-    constexpr int N = Vec<T>::N, P = N / 2;
-    extern __shared__ uint4 ring[];  // [stage][tensor: x, dxn, dres][row of K][vector of V][thread]
-    __shared__ float sh[2 * 16 * 2 * K];
+    constexpr int N = Vec<T>::N, P = N / 2, TENSORS = RES ? 3 : 2;
+    extern __shared__ uint4 ring[];  // [stage][tensor: x, dxn, dres][row of K][vector of V][thread of THREADS]
+    __shared__ __align__(16) float sh[2 * 16 * 2 * K];
     int side = 0;
-    const int threads = warps * 32, teams = blockDim.x / threads, lane = threadIdx.x % threads, wide = blockDim.x, team = threadIdx.x / threads;
-    const int32_t pieces = a.d / N;
-    const float by = 1.0f / (float)a.d;
+    const int threads = ONE ? 32 : warps * 32, teams = blockDim.x / threads, lane = threadIdx.x % threads, team = threadIdx.x / threads;
+    const float by = -1.0f / (float)a.d;
     const int64_t step = (int64_t)gridDim.x * teams * K;
     int64_t row = ((int64_t)blockIdx.x * teams + team) * K;
-    const int tensors = a.dres ? 3 : 2;
-    const Weights<T, V> w(a.w, lane, threads, pieces);
+    const Places<T, V> at(a.d, lane, threads);
+    float2 held[HELD ? V : 1][P];
+    if constexpr (HELD) load_weights<T, V>(a.w, lane, threads, at, held);
+    auto weights = [&](int v, float2 (&w)[P]) {
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) w[i] = held[v][i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) w[i] = both(0.0f);
+            if (at.in[v]) load_floats(a.w + (int64_t)(lane + v * threads) * N, w);
+        }
+    };
     wait_previous_kernel();
-    auto place = [&](int stage, int tensor, int k, int v) { return ring + (((stage * tensors + tensor) * K + k) * V + v) * wide + threadIdx.x; };
-    auto fetch = [&](int stage, int64_t first) {
+    const int64_t offset = at.first + row * at.row_bytes, step_bytes = step * at.row_bytes;
+    const char *x_from = static_cast<const char *>(a.x) + offset, *g_from = static_cast<const char *>(a.dxn) + offset, *res_from = static_cast<const char *>(a.dres) + offset;
+    char *to = static_cast<char *>(a.dX) + offset;
+    int64_t ahead = row;
+    auto place = [&](int stage, int tensor, int k, int v) { return ring + (((stage * TENSORS + tensor) * K + k) * V + v) * THREADS + threadIdx.x; };
+    auto fetch = [&](int stage) {
+        if (ahead < a.T) {
+            int64_t p = 0;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k, p += at.row_bytes)
+                if (k == 0 || ahead + k < a.T)
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (first + k < a.T && lane + v * threads < pieces) {
-                    const int64_t at = (first + k) * a.d + (int64_t)(lane + v * threads) * N;
-                    copy16(place(stage, 0, k, v), static_cast<const T *>(a.x) + at);
-                    copy16(place(stage, 1, k, v), static_cast<const T *>(a.dxn) + at);
-                    if (tensors == 3) copy16(place(stage, 2, k, v), static_cast<const T *>(a.dres) + at);
-                }
+                    for (int v = 0; v < V; ++v)
+                        if (at.in[v]) {
+                            copy16(place(stage, 0, k, v), x_from + p + v * at.v_bytes);
+                            copy16(place(stage, 1, k, v), g_from + p + v * at.v_bytes);
+                            if constexpr (RES) copy16(place(stage, 2, k, v), res_from + p + v * at.v_bytes);
+                        }
+        }
         copies_commit();
+        x_from += step_bytes; g_from += step_bytes; res_from += step_bytes;
+        ahead += step;
+    };
+    float next_mean[K], next_r[K];  // of the rows to come: loaded a turn ahead
+    auto statistics = [&](int64_t first) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            next_mean[k] = first + k < a.T ? a.mean[first + k] : 0.0f;
+            next_r[k] = first + k < a.T ? a.rstd[first + k] : 0.0f;
+        }
     };
     float2 dw[V][P], db[V][P];
 #pragma unroll
@@ -202,71 +261,72 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
 #pragma unroll
         for (int i = 0; i < P; ++i) dw[v][i] = db[v][i] = both(0.0f);
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s) fetch(s, row + s * step);
+    for (int i = 0; i < S; ++i) fetch(i);
+    statistics(row);
     int stage = 0;
-    for (; row < a.T; row += step) {
-        float off[K], r[K], s[2 * K];
+    for (; row < a.T; row += step, to += step_bytes) {
+        float r[K], s[2 * K], off[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            r[k] = row + k < a.T ? a.rstd[row + k] : 0.0f;
-            off[k] = row + k < a.T ? -a.mean[row + k] * r[k] : 0.0f;
+            r[k] = next_r[k];
+            off[k] = -next_mean[k] * r[k];
         }
-        copies_wait<STAGES - 1>();
-        Vec<T> x[K][V], g[K][V];
+        statistics(row + step);
+        copies_wait<S - 1>();
+        Vec<T> g[K][V];
+        float2 n[K][V][P];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             float2 first = both(0.0f), second = both(0.0f);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                x[k][v].raw = g[k][v].raw = make_uint4(0u, 0u, 0u, 0u);
-                const int q = lane + v * threads;
-                if (q < pieces && row + k < a.T) {
-                    x[k][v].raw = *place(stage, 0, k, v);
+                Vec<T> x;
+                x.raw = g[k][v].raw = make_uint4(0u, 0u, 0u, 0u);
+                if (at.in[v] && (k == 0 || row + k < a.T)) {
+                    x.raw = *place(stage, 0, k, v);
                     g[k][v].raw = *place(stage, 1, k, v);
                 }
-                float2 wv[P];
-                if (Weights<T, V>::HELD || q < pieces) w.get(v, q, wv);
-                else
-#pragma unroll
-                    for (int i = 0; i < P; ++i) wv[i] = both(0.0f);
+                float2 w[P];
+                weights(v, w);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const float2 n = fma2(x[k][v].get(2 * i), both(r[k]), both(off[k])), d = g[k][v].get(2 * i), u = mul2(d, wv[i]);
-                    first = fma2(u, both(1.0f), first);
-                    second = fma2(u, n, second);
-                    dw[v][i] = fma2(d, n, dw[v][i]);
-                    db[v][i] = fma2(d, both(1.0f), db[v][i]);
+                    n[k][v][i] = fma2(x.get(2 * i), both(r[k]), both(off[k]));
+                    const float2 d = g[k][v].get(2 * i), u = mul2(d, w[i]);
+                    first = add2(u, first);
+                    second = fma2(u, n[k][v][i], second);
+                    dw[v][i] = fma2(d, n[k][v][i], dw[v][i]);
+                    db[v][i] = add2(d, db[v][i]);
                 }
             }
             s[2 * k] = first.x + first.y;
             s[2 * k + 1] = second.x + second.y;
         }
-        sums_of_team<2 * K>(s, warps, sh, side);
+        sums_of_team<2 * K, ONE>(s, warps, sh, side);
+        char *out = to;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (row + k >= a.T) break;
-            const float m1 = -s[2 * k] * by, m2 = -s[2 * k + 1] * by;
+        for (int k = 0; k < K; ++k, out += at.row_bytes) {
+            if (k > 0 && row + k >= a.T) break;
+            const float m1 = s[2 * k] * by, m2 = s[2 * k + 1] * by;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int q = lane + v * threads;
-                if (q >= pieces) break;
-                float2 wv[P];
-                w.get(v, q, wv);
+                if (!at.in[v]) break;
+                float2 w[P];
+                weights(v, w);
                 Vec<T> res, o;
-                if (tensors == 3) res.raw = *place(stage, 2, k, v);
+                if constexpr (RES) res.raw = *place(stage, 2, k, v);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const float2 n = fma2(x[k][v].get(2 * i), both(r[k]), both(off[k]));
-                    const float2 t = fma2(n, both(m2), fma2(g[k][v].get(2 * i), wv[i], both(m1)));
-                    o.set(2 * i, tensors == 3 ? fma2(t, both(r[k]), res.get(2 * i)) : mul2(t, both(r[k])));
+                    const float2 t = fma2(n[k][v][i], both(m2), fma2(g[k][v].get(2 * i), w[i], both(m1)));
+                    if constexpr (RES) o.set(2 * i, fma2(t, both(r[k]), res.get(2 * i)));
+                    else o.set(2 * i, mul2(t, both(r[k])));
                 }
-                store_vec<T>(a.dX, row + k, a.d, q, o);
+                *reinterpret_cast<uint4 *>(out + v * at.v_bytes) = o.raw;
             }
         }
-        fetch(stage, row + STAGES * step);  // each thread has read its own places
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        fetch(stage);  // each thread has read its own places
+        stage = stage + 1 == S ? 0 : stage + 1;
     }
-    // Sums of the block: team behind team through the ring, which takes 2 d floats (4 bytes a column for every 32 of a row's 2-byte elements in it)
+    // Sums of the block, team behind team through the ring, which has room for 2 d floats
     copies_wait<0>();
     float *all = reinterpret_cast<float *>(ring);
     for (int turn = 0; turn < teams; ++turn) {
@@ -274,13 +334,12 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
         if (team != turn) continue;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int q = lane + v * threads;
-            if (q >= pieces) break;
-            float2 *to = reinterpret_cast<float2 *>(all + (int64_t)q * N), *to_b = reinterpret_cast<float2 *>(all + a.d + (int64_t)q * N);
+            if (!at.in[v]) break;
+            float2 *to_w = reinterpret_cast<float2 *>(all + (int64_t)(lane + v * threads) * N), *to_b = reinterpret_cast<float2 *>(all + a.d + (int64_t)(lane + v * threads) * N);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                to[i] = turn ? fma2(to[i], both(1.0f), dw[v][i]) : dw[v][i];
-                to_b[i] = turn ? fma2(to_b[i], both(1.0f), db[v][i]) : db[v][i];
+                to_w[i] = turn ? add2(to_w[i], dw[v][i]) : dw[v][i];
+                to_b[i] = turn ? add2(to_b[i], db[v][i]) : db[v][i];
             }
         }
     }
@@ -289,8 +348,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
     for (int i = threadIdx.x; i < a.d / 2; i += blockDim.x) reinterpret_cast<float4 *>(part)[i] = reinterpret_cast<const float4 *>(all)[i];
 }
 
-// dw and db from the blocks' sums: 32 columns a block, a warp every sixteenth part
-constexpr int COLUMN_WARPS = 16;
+// dw and db from the blocks' sums: 32 columns a block, a warp every 32nd part, its loads (ten at most) together
+constexpr int COLUMN_WARPS = 32;
 __global__ void __launch_bounds__(COLUMN_WARPS * 32) layer_norm_columns_kernel(const float *part, int32_t parts, int32_t d, float *dw, float *db) {
     wait_previous_kernel();
     __shared__ double sh[COLUMN_WARPS][32];
@@ -298,7 +357,7 @@ __global__ void __launch_bounds__(COLUMN_WARPS * 32) layer_norm_columns_kernel(c
     const int32_t col = blockIdx.x * 32 + lane;
     double s = 0.0;
     if (col < 2 * d)
-#pragma unroll 8
+#pragma unroll 10
         for (int32_t p = warp; p < parts; p += COLUMN_WARPS) s += (double)part[(int64_t)p * 2 * d + col];
     sh[warp][lane] = s;
     __syncthreads();
@@ -309,28 +368,42 @@ __global__ void __launch_bounds__(COLUMN_WARPS * 32) layer_norm_columns_kernel(c
     else if (db) db[col - d] = (float)s;
 }
 
-// Vectors of a row in each thread of a team of up to 16 warps
-struct Team { int V, K, warps, threads; };
-Team team_of(int32_t d, int32_t act) {
+// A row's vectors: V of them in each thread of a team of up to 16 warps. As many a thread as there are registers for (no sums between warps for rows of up to 128 vectors), fewer
+// where that leaves more than a fifth of a team's threads without work.
+struct Team { int V, warps, threads; };
+Team team_of(int32_t d, int32_t act, int most) {
     const int64_t pieces = (int64_t)d * (int64_t)act_bytes(act) / 16;
-    Team t;
-    t.V = pieces <= 256 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8;
-    t.K = t.V == 1 ? 4 : t.V == 2 ? 2 : 1;
-    t.warps = (int)cdiv(pieces, 32 * t.V);
-    t.threads = 32 * t.warps * (t.warps <= 8 ? 8 / t.warps : 1);
-    return t;
+    Team best = {0, 0, 0};
+    double share = 0.0;
+    for (int V = most; V >= 1; V /= 2) {
+        const int64_t warps = cdiv(pieces, 32 * V);
+        const double s = (double)pieces / (double)(32 * V * warps);
+        if (warps > 16 || s <= share) continue;
+        best = {V, (int)warps, (int)(32 * warps * (warps <= 8 ? 8 / warps : 1))};
+        share = s;
+        if (s >= 0.8) break;
+    }
+    return best;
 }
-// Blocks that an SM holds: of 256 threads four, or two with the backward pass's sums; of 512 threads one
-int per_sm(const Team &t, bool backward) { return t.threads > 256 ? 1 : backward ? 2 : 4; }
+Team forward_team(int32_t d, int32_t act) { return team_of(d, act, (int64_t)d * (int64_t)act_bytes(act) / 16 > 2048 ? 8 : 4); }
+Team backward_team(int32_t d, int32_t act) {  // 16 elements of a row a thread, whose sums of columns take 32 registers; the widest rows have 32
+    const int64_t pieces = (int64_t)d * (int64_t)act_bytes(act) / 16;
+    const int most = act == MOE_BF16 ? 2 : 4;
+    return team_of(d, act, pieces > 512 * most ? 2 * most : most);
+}
+// Rows of a team at a time: two vectors of a row and its gradient are what fits beside the sums of columns (bf16 backward of 65536 x 1024 with two rows of two: 121 us, with one 86)
+constexpr int rows_at_once(int V, bool backward) { return backward ? (V == 1 ? 2 : 1) : V >= 4 ? 1 : 4 / V; }
+// 512 threads an SM, in two blocks or, of teams of more than eight warps, in one
 int64_t blocks_of(int64_t T, const Team &t, bool backward) {
-    return imin(cdiv(T, (int64_t)t.K * (t.threads / (32 * t.warps))), (int64_t)per_sm(t, backward) * 148);
+    return imin(cdiv(T, (int64_t)rows_at_once(t.V, backward) * (t.threads / (32 * t.warps))), t.threads > 256 ? 148 : 2 * 148);
 }
 
-template <typename T, int V, int K, int THREADS, int BLOCKS> int32_t forward(const LayerNormArgs &a, const Team &t, cudaStream_t st) {
+template <typename T, int V, int THREADS, bool ONE> int32_t forward(const LayerNormArgs &a, const Team &t, cudaStream_t st) {
+    constexpr int K = rows_at_once(V, false), BYTES = STAGES * K * V * THREADS * 16;
+    constexpr auto kernel = layer_norm_kernel<T, V, K, THREADS, 512 / THREADS, ONE>;
     static PerDevice allowed;
-    const int bytes = FORWARD_STAGES * K * V * t.threads * 16;
-    if (!allow_shared(allowed, layer_norm_kernel<T, V, K, THREADS, BLOCKS>, FORWARD_STAGES * K * V * THREADS * 16)) return MOE_ERR_CUDA;
-    launch_kernel(layer_norm_kernel<T, V, K, THREADS, BLOCKS>, dim3((unsigned)blocks_of(a.T, t, false)), dim3(t.threads), bytes, st, a, t.warps);
+    if (!allow_shared(allowed, kernel, BYTES)) return MOE_ERR_CUDA;
+    launch_kernel(kernel, dim3((unsigned)blocks_of(a.T, t, false)), dim3(t.threads), BYTES, st, a, t.warps);
     MOE_LAUNCHED();
     return MOE_OK;
 }
@@ -339,46 +412,57 @@ int32_t columns(const LayerNormGradArgs &a, int32_t blocks, cudaStream_t st) {
     MOE_LAUNCHED();
     return MOE_OK;
 }
-template <typename T, int V, int K, int THREADS, int BLOCKS, int STAGES> int32_t backward(const LayerNormGradArgs &a, const Team &t, cudaStream_t st) {
+template <typename T, int V, int THREADS, bool ONE, bool RES> int32_t backward(const LayerNormGradArgs &a, const Team &t, cudaStream_t st) {
+    constexpr int K = rows_at_once(V, true), S = V == 8 ? 1 : STAGES, BYTES = S * (RES ? 3 : 2) * K * V * THREADS * 16;
+    constexpr auto kernel = layer_norm_grads_kernel<T, V, K, THREADS, 512 / THREADS, S, ONE, RES, V * Vec<T>::N <= 16>;
     static PerDevice allowed;
-    const int bytes = STAGES * 3 * K * V * 16;  // a thread
-    if (!allow_shared(allowed, layer_norm_grads_kernel<T, V, K, THREADS, BLOCKS, STAGES>, bytes * THREADS)) return MOE_ERR_CUDA;
+    if (!allow_shared(allowed, kernel, BYTES)) return MOE_ERR_CUDA;
     const int64_t blocks = blocks_of(a.T, t, true);
-    launch_kernel(layer_norm_grads_kernel<T, V, K, THREADS, BLOCKS, STAGES>, dim3((unsigned)blocks), dim3(t.threads), (size_t)bytes * t.threads, st, a, t.warps);
+    launch_kernel(kernel, dim3((unsigned)blocks), dim3(t.threads), BYTES, st, a, t.warps);
     MOE_LAUNCHED();
     return columns(a, (int32_t)blocks, st);
 }
-template <typename T> int32_t forward_of(const LayerNormArgs &a, const Team &t, cudaStream_t st) {
-    if (t.V == 1) return forward<T, 1, 4, 256, 4>(a, t, st);
-    if (t.V == 2) return t.threads <= 256 ? forward<T, 2, 2, 256, 4>(a, t, st) : forward<T, 2, 2, 512, 1>(a, t, st);
-    if (t.V == 4) return forward<T, 4, 1, 512, 1>(a, t, st);
-    if constexpr (sizeof(T) == 4) return forward<T, 8, 1, 512, 1>(a, t, st);
+template <typename T, int V> int32_t forward_of(const LayerNormArgs &a, const Team &t, cudaStream_t st) {
+    if (t.warps == 1) return forward<T, V, 256, true>(a, t, st);
+    return t.threads <= 256 ? forward<T, V, 256, false>(a, t, st) : forward<T, V, 512, false>(a, t, st);
+}
+template <typename T, int V, bool RES> int32_t backward_of(const LayerNormGradArgs &a, const Team &t, cudaStream_t st) {
+    if (t.warps == 1) return backward<T, V, 256, true, RES>(a, t, st);
+    return t.threads <= 256 ? backward<T, V, 256, false, RES>(a, t, st) : backward<T, V, 512, false, RES>(a, t, st);
+}
+template <typename T> int32_t forward_any(const LayerNormArgs &a, const Team &t, cudaStream_t st) {
+    if (t.V == 1) return forward_of<T, 1>(a, t, st);
+    if (t.V == 2) return forward_of<T, 2>(a, t, st);
+    if (t.V == 4) return forward_of<T, 4>(a, t, st);
+    if constexpr (sizeof(T) == 4) return forward<T, 8, 512, false>(a, t, st);
     return MOE_ERR_UNSUPPORTED;  // (no such row: MOE_NORM_MAX_D)
 }
-template <typename T> int32_t backward_of(const LayerNormGradArgs &a, const Team &t, cudaStream_t st) {
-    if (t.V == 1) return backward<T, 1, 4, 256, 2, 2>(a, t, st);
-    if (t.V == 2) return t.threads <= 256 ? backward<T, 2, 2, 256, 2, 2>(a, t, st) : backward<T, 2, 2, 512, 1, 2>(a, t, st);
-    if (t.V == 4) return backward<T, 4, 1, 512, 1, 2>(a, t, st);
-    if constexpr (sizeof(T) == 4) return backward<T, 8, 1, 512, 1, 1>(a, t, st);
+template <typename T, bool RES> int32_t backward_any(const LayerNormGradArgs &a, const Team &t, cudaStream_t st) {
+    if (t.V == 1) return backward_of<T, 1, RES>(a, t, st);
+    if (t.V == 2) return backward_of<T, 2, RES>(a, t, st);
+    if (t.V == 4) {
+        if constexpr (sizeof(T) == 4) return backward_of<T, 4, RES>(a, t, st);
+        return backward<T, 4, 512, false, RES>(a, t, st);
+    }
+    if constexpr (sizeof(T) == 4) return backward<T, 8, 512, false, RES>(a, t, st);
     return MOE_ERR_UNSUPPORTED;
 }
 
 }  // namespace
 
-int64_t layer_norm_grad_floats(int64_t T, int32_t d, int32_t act) {
-    return 2 * (int64_t)d * imax(1, blocks_of(T, team_of(d, act), true));
-}
+int64_t layer_norm_grad_floats(int64_t T, int32_t d, int32_t act) { return 2 * (int64_t)d * imax(1, blocks_of(T, backward_team(d, act), true)); }
 
 int32_t launch_layer_norm(const LayerNormArgs &a, cudaStream_t st) {
     if (a.T == 0) return MOE_OK;
-    const Team t = team_of(a.d, a.act);
-    return a.act == MOE_BF16 ? forward_of<bf16>(a, t, st) : forward_of<float>(a, t, st);
+    const Team t = forward_team(a.d, a.act);
+    return a.act == MOE_BF16 ? forward_any<bf16>(a, t, st) : forward_any<float>(a, t, st);
 }
 
 int32_t launch_layer_norm_grads(const LayerNormGradArgs &a, cudaStream_t st) {
-    const Team t = team_of(a.d, a.act);
     if (a.T == 0) return columns(a, 0, st);  // sums of nothing
-    return a.act == MOE_BF16 ? backward_of<bf16>(a, t, st) : backward_of<float>(a, t, st);
+    const Team t = backward_team(a.d, a.act);
+    if (a.act == MOE_BF16) return a.dres ? backward_any<bf16, true>(a, t, st) : backward_any<bf16, false>(a, t, st);
+    return a.dres ? backward_any<float, true>(a, t, st) : backward_any<float, false>(a, t, st);
 }
 
 }  // namespace moe
