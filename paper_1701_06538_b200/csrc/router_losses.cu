@@ -11,14 +11,17 @@
 #include <math_constants.h>
 
 #include "block.cuh"
+#include "pairs.cuh"
+#include "tc.cuh"
 
 namespace moe {
 
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
-constexpr int COUNT_CLUSTER = 8;  // blocks that count one sequence's choices together, where there are few sequences
-constexpr int SUM_BLOCKS = 4 * 148;
+constexpr int COUNT_THREADS = 1024, COUNT_EACH = 8;  // choices a thread has on their way
+constexpr int SUM_WARPS = 32, SUM_BLOCKS = 2 * 148;
+constexpr int ROW_BLOCKS = 2 * 148;                  // two an SM (131072 x 128 with 4, 3 and 2, four rows at a time: 47.3, 41.0, 40.9 us; 20000 x 512: 35.0, 35.1, 31.3)
 
 struct Scratch {
     int32_t *live;     // [S] live tokens
@@ -27,7 +30,7 @@ struct Scratch {
     double *z;         // [chunks] sums of lse^2
     double *balance;   // [SUM_BLOCKS]
 };
-int64_t rows_of_chunk(int64_t T) { return imax(8, cdiv(T, 4 * 148)); }
+int64_t rows_of_chunk(int64_t T) { return imax(32, cdiv(cdiv(T, ROW_BLOCKS), 32) * 32); }
 int64_t chunks_of(int64_t T) { return cdiv(imax(T, 1), rows_of_chunk(T)); }
 Scratch scratch_at(Carver &cv, int64_t T, int32_t n, int32_t S) {
     Scratch s;
@@ -45,48 +48,63 @@ __device__ __forceinline__ int2 tokens_of(const RouterLossArgs &a, int32_t s) {
     const int32_t end = min(max(a.offsets[a.S], 0), (int32_t)a.T), from = min(max(a.offsets[s], 0), end), to = min(max(a.offsets[s + 1], 0), end);
     return make_int2(from, max(from, to));
 }
-__device__ __forceinline__ double sum_of_block(double v, double *sh) {  // of all threads, by all of them in the same order
+__device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    return v;
+}
+// Of N warps, for all of them, always in the same order. (By exchanges: a chain of additions in double is 30 of its latencies.) sh: a place per warp
+template <int N> __device__ __forceinline__ double sum_of_block(double v, double *sh) {
+    v = warp_sum(v);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
     __syncthreads();
-    double s = 0.0;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) s += sh[w];
-    return s;
+    return warp_sum((threadIdx.x & 31) < N ? sh[threadIdx.x & 31] : 0.0);
 }
 
-// Choices and live tokens of a sequence, by a cluster of blocks through each other's shared memory, or by one block
-template <bool CLUSTER>
-__global__ void __launch_bounds__(THREADS) router_counts_kernel(const RouterLossArgs a, const Scratch w) {
-    extern __shared__ int32_t hist[];  // [n], and the live tokens
-    const int32_t parts = CLUSTER ? COUNT_CLUSTER : 1, rank = CLUSTER ? blockIdx.x % COUNT_CLUSTER : 0, s = CLUSTER ? blockIdx.x / COUNT_CLUSTER : blockIdx.x;
-    for (int32_t j = threadIdx.x; j <= a.n; j += THREADS) hist[j] = 0;
-    __syncthreads();
-    wait_previous_kernel();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *w.ticket = 0;
+// Choices and live tokens of a sequence into hist [n + 1], by `parts` blocks together. (The loads of COUNT_EACH choices go before what depends on them.)
+__device__ __forceinline__ void count_choices(const RouterLossArgs &a, const Divisor &by_k, int32_t s, int32_t rank, int32_t parts, int32_t *hist) {
     const int2 t = tokens_of(a, s);
-    const uint32_t k = (uint32_t)a.k;
-    const int64_t end = (int64_t)t.y * k;
+    const int32_t end = t.y * a.k, stride = parts * (int32_t)blockDim.x;  // T k is below 2^31
     int32_t live = 0;
-#pragma unroll 4
-    for (int64_t i = (int64_t)t.x * k + rank * THREADS + threadIdx.x; i < end; i += parts * THREADS) {
-        const uint32_t token = (uint32_t)i / k;  // T k is below 2^31
-        if (a.keep && !a.keep[token]) continue;
-        live += (uint32_t)i == token * k;
-        const int32_t e = a.topk_idx[i];
-        if ((uint32_t)e < (uint32_t)a.n) atomicAdd(hist + e, 1);
+    for (int64_t i = (int64_t)t.x * a.k + rank * blockDim.x + threadIdx.x; i < end; i += (int64_t)COUNT_EACH * stride) {
+        int32_t e[COUNT_EACH], in_token[COUNT_EACH];
+        bool in[COUNT_EACH];
+#pragma unroll
+        for (int q = 0; q < COUNT_EACH; ++q) {
+            const int64_t at = i + (int64_t)q * stride;
+            in[q] = at < end;
+            e[q] = in[q] ? a.topk_idx[at] : -1;
+            const int32_t token = by_k((int32_t)(in[q] ? at : 0), in_token[q]);
+            if (a.keep && in[q]) in[q] = a.keep[token] != 0;
+        }
+#pragma unroll
+        for (int q = 0; q < COUNT_EACH; ++q) {
+            if (!in[q]) continue;
+            live += in_token[q] == 0;
+            if ((uint32_t)e[q] < (uint32_t)a.n) atomicAdd(hist + e[q], 1);
+        }
     }
     live = __reduce_add_sync(0xffffffffu, live);
     if ((threadIdx.x & 31) == 0 && live) atomicAdd(hist + a.n, live);
+}
+// By a cluster of blocks through each other's shared memory, or by one block
+template <bool CLUSTER>
+__global__ void __launch_bounds__(COUNT_THREADS) router_counts_kernel(const RouterLossArgs a, const Scratch w, const Divisor by_k, int32_t parts) {
+    extern __shared__ int32_t hist[];  // [n], and the live tokens
+    const int32_t rank = CLUSTER ? blockIdx.x % parts : 0, s = CLUSTER ? blockIdx.x / parts : blockIdx.x;
+    for (int32_t j = threadIdx.x; j <= a.n; j += COUNT_THREADS) hist[j] = 0;
+    __syncthreads();
+    wait_previous_kernel();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *w.ticket = 0;
+    count_choices(a, by_k, s, rank, parts, hist);
     if constexpr (CLUSTER) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        for (int32_t j = rank * THREADS + threadIdx.x; j <= a.n; j += COUNT_CLUSTER * THREADS) {
+        for (int32_t j = rank * COUNT_THREADS + threadIdx.x; j <= a.n; j += parts * COUNT_THREADS) {
             int32_t sum = 0;
             const uint32_t at = (uint32_t)__cvta_generic_to_shared(hist + j);
-#pragma unroll
-            for (int32_t q = 0; q < COUNT_CLUSTER; ++q) {
+#pragma unroll 8
+            for (int32_t q = 0; q < parts; ++q) {
                 uint32_t there;
                 int32_t v;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(q));
@@ -99,75 +117,111 @@ __global__ void __launch_bounds__(THREADS) router_counts_kernel(const RouterLoss
         asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");  // nobody leaves while it is read
     } else {
         __syncthreads();
-        for (int32_t j = threadIdx.x; j <= a.n; j += THREADS) {
+        for (int32_t j = threadIdx.x; j <= a.n; j += COUNT_THREADS) {
             if (j < a.n) a.counts[(int64_t)s * a.n + j] = hist[j];
             else w.live[s] = hist[j];
         }
     }
 }
 
-// Sums over the lanes of a row: a part of a warp, or the whole block (sh: a place per warp, twice)
-template <int LANES> __device__ __forceinline__ float row_max(float v, float *sh) {
+__device__ __forceinline__ float larger(float a, float b) {  // a NaN stays
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
+    return a;
+}
+// N values over the lanes of a row at once, put together by `op`: in the first steps lanes give away half of their values, so that eight take seventeen exchanges with what tells
+// all lanes, not forty. LANES is a part of a warp; or the whole block (N values of one row; sh: a place per warp and value)
+template <int N, int LANES, typename Op> __device__ __forceinline__ void over_lanes(float (&s)[N], float *sh, Op op) {
+    constexpr int L = LANES > 32 ? 32 : LANES;
+    const int lane = threadIdx.x & 31;
+    int off = L / 2, m = N / 2;
 #pragma unroll
-    for (int off = (LANES > 32 ? 32 : LANES) / 2; off > 0; off >>= 1) {
-        const float o = __shfl_xor_sync(0xffffffffu, v, off);
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(o));
+    for (; m >= 1; m >>= 1, off >>= 1) {
+        const bool up = lane & off;
+#pragma unroll
+        for (int i = 0; i < m; ++i) {
+            const float keep = up ? s[i + m] : s[i], send = up ? s[i] : s[i + m];
+            s[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, off));
+        }
     }
+    float t = s[0];
+#pragma unroll
+    for (; off >= 1; off >>= 1) t = op(t, __shfl_xor_sync(0xffffffffu, t, off));
+    constexpr int EACH = L / N;
     if constexpr (LANES > 32) {
         __syncthreads();
-        if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+        if (lane % EACH == 0) sh[(threadIdx.x >> 5) * N + lane / EACH] = t;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(sh[w]));
-    }
-    return v;
-}
-template <int LANES> __device__ __forceinline__ float2 row_sums(float2 v, float *sh) {
+        for (int i = 0; i < N; ++i) {
+            s[i] = sh[i];
 #pragma unroll
-    for (int off = (LANES > 32 ? 32 : LANES) / 2; off > 0; off >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, off);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
-    }
-    if constexpr (LANES > 32) {
-        if ((threadIdx.x & 31) == 0) { sh[WARPS + (threadIdx.x >> 5)] = v.x; sh[2 * WARPS + (threadIdx.x >> 5)] = v.y; }
-        __syncthreads();
-        v = make_float2(0.0f, 0.0f);
+            for (int w = 1; w < WARPS; ++w) s[i] = op(s[i], sh[w * N + i]);
+        }
+    } else if constexpr (N > 1) {
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) { v.x += sh[WARPS + w]; v.y += sh[2 * WARPS + w]; }
+        for (int i = 0; i < N; ++i) s[i] = __shfl_sync(0xffffffffu, t, i * EACH, L);
+    } else {
+        s[0] = t;
     }
-    return v;
 }
 
-template <int VEC> struct Columns;
-template <> struct Columns<4> {
-    float4 q;
-    __device__ __forceinline__ void load(const float *p) { q = *reinterpret_cast<const float4 *>(p); }
-    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = q; }
-    __device__ __forceinline__ float &operator[](int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
-};
-template <> struct Columns<1> {
-    float q;
-    __device__ __forceinline__ void load(const float *p) { q = *p; }
-    __device__ __forceinline__ void store(float *p) const { *p = q; }
-    __device__ __forceinline__ float &operator[](int) { return q; }
+__device__ __forceinline__ float power_of_two(float x) {  // the hardware's, to two units of the last place; 0 below float's smallest normal number
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// A thread's columns of a row as pairs: U vectors of VEC columns, LANES vectors apart
+template <int LANES, int U, int VEC> struct Columns {
+    static constexpr int H = U * VEC / 2;
+    static_assert(U * VEC % 2 == 0, "pairs");
+    int32_t n;
+    int lane;
+    bool in[U];
+    __device__ __forceinline__ Columns(int32_t n_, int lane_) : n(n_), lane(lane_) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) in[u] = (lane + u * LANES) * VEC < n;
+    }
+    __device__ __forceinline__ int32_t column(int e) const { return (lane + e / VEC * LANES) * VEC + e % VEC; }
+    // row: of the thread's first column
+    __device__ __forceinline__ void load(const float *row, float2 (&v)[H]) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!in[u]) continue;
+            if constexpr (VEC == 4) {
+                const float4 q = *reinterpret_cast<const float4 *>(row + u * (LANES * 4));
+                v[2 * u] = make_float2(q.x, q.y);
+                v[2 * u + 1] = make_float2(q.z, q.w);
+            } else {
+                (u & 1 ? v[u / 2].y : v[u / 2].x) = row[u * LANES];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float *row, const float2 (&v)[H]) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!in[u]) continue;
+            if constexpr (VEC == 4) *reinterpret_cast<float4 *>(row + u * (LANES * 4)) = make_float4(v[2 * u].x, v[2 * u].y, v[2 * u + 1].x, v[2 * u + 1].y);
+            else row[u * LANES] = u & 1 ? v[u / 2].y : v[u / 2].x;
+        }
+    }
 };
 
-// LANES threads have a row, U vectors of VEC columns each
-template <int LANES, int U, int VEC, bool GRAD>
-__global__ void __launch_bounds__(THREADS) router_rows_kernel(const RouterLossArgs a, const Scratch w, int32_t chunk_rows) {
-    constexpr int ROWS = THREADS / LANES;  // at a time
-    extern __shared__ float sums[];        // [min(ROWS, WARPS)][n]
-    __shared__ float sh[3 * WARPS];
-    __shared__ double wide[WARPS];
-    const int lane = threadIdx.x % LANES, place = threadIdx.x / LANES;
+// Rows first .. last - 1 by a block. LANES threads have R rows at a time, some pairs of columns of each, and the next R rows on their way.
+template <int LANES, int U, int VEC, int R, bool GRAD>
+__device__ __forceinline__ void router_rows(const RouterLossArgs &a, const Scratch &w, int32_t block, int32_t first, int32_t last, float *sums, double *wide, float *sh) {
+    constexpr int ROWS = THREADS / LANES * R, H = U * VEC / 2;  // at a time
+    constexpr float LOG2_E = 1.44269504088896340736f;
+    const int place = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     const int32_t n = a.n;
-    const int32_t first = (int32_t)blockIdx.x * chunk_rows, last = min(first + chunk_rows, (int32_t)a.T);
-    wait_previous_kernel();
-    auto column = [&](int u) { return (lane + u * LANES) * VEC; };
+    const Columns<LANES, U, VEC> mine(n, lane);
     // tokens that count, of all sequences
     double all = 0.0;
-    for (int32_t s = threadIdx.x; s < a.S; s += THREADS) all += (double)w.live[s];
-    all = sum_of_block(all, wide);
+    if (a.S == 1) {
+        all = (double)w.live[0];
+    } else {
+        for (int32_t s = threadIdx.x; s < a.S; s += THREADS) all += (double)w.live[s];
+        all = sum_of_block<WARPS>(all, wide);
+    }
     const float by_z = all > 0.0 ? (float)(2.0 * (double)a.w_z / all) : 0.0f;
     // the sequence of the first token: the last one that begins at it or before
     int32_t s = 0;
@@ -198,76 +252,92 @@ __global__ void __launch_bounds__(THREADS) router_rows_kernel(const RouterLossAr
         if (end <= at) { ++s; continue; }
         const int32_t live = w.live[s];
         const float by = live > 0 ? (float)((double)a.w_balance * n / ((double)a.k * all * live)) : 0.0f;
-        Columns<VEC> c[U], p[U];
+        float2 next[R][H];
+        int32_t row = at + place * R;  // the first of the rows to be fetched
+        const int64_t from = (int64_t)row * n + mine.lane * VEC;
+        const float *x_at = a.logits + from;
+        float *d_at = GRAD ? a.dlogits + from : nullptr;
+        auto fetch = [&]() {
+            const float *x = x_at;
+#pragma unroll
+            for (int r = 0; r < R; ++r, x += n) {
+#pragma unroll
+                for (int h = 0; h < H; ++h) next[r][h] = both(-CUDART_INF_F);
+                if (row + r < end && (!a.keep || a.keep[row + r])) mine.load(x, next[r]);
+            }
+            row += ROWS;
+            x_at += (int64_t)ROWS * n;
+        };
+        fetch();
+        float2 c[H], p[H];
         float lse2 = 0.0f;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                c[u][i] = column(u) + i < n ? (float)a.counts[(int64_t)s * n + column(u) + i] * by : 0.0f;
-                p[u][i] = 0.0f;
-            }
-        for (int32_t base = at; base < end; base += ROWS) {
-            const int32_t row = base + place;
-            const bool in = row < end, live_row = in && (!a.keep || a.keep[row]);
-            const float *x = a.logits + (int64_t)row * n;
-            Columns<VEC> v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[u][i] = -CUDART_INF_F;
-                if (live_row && column(u) < n) v[u].load(x + column(u));
-            }
-            float top = -CUDART_INF_F;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(v[u][i]));
-            top = row_max<LANES>(top, sh);
-            const bool empty = top == -CUDART_INF_F;  // no expert left, or no row
-            float2 two = make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    v[u][i] = empty ? 0.0f : exp2f((v[u][i] - top) * 1.44269504088896340736f);
-                    two.x += v[u][i];
-                    two.y = fmaf(c[u][i], v[u][i], two.y);
-                }
-            two = row_sums<LANES>(two, sh);
-            const float r = empty ? 0.0f : 1.0f / two.x, lse = empty ? 0.0f : top + logf(two.x);
-            const float pull = fmaf(two.y, -r, by_z * lse);
-            if (lane == 0) lse2 = fmaf(lse, lse, lse2);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    v[u][i] *= r;
-                    p[u][i] += v[u][i];
-                    v[u][i] *= c[u][i] + pull;
-                }
-                if (GRAD && in && column(u) < n) v[u].store(a.dlogits + (int64_t)row * n + column(u));
-            }
+        for (int h = 0; h < H; ++h) {
+            const int32_t j = mine.column(2 * h), i = mine.column(2 * h + 1);
+            c[h] = make_float2(j < n ? (float)a.counts[(int64_t)s * n + j] * by : 0.0f, i < n ? (float)a.counts[(int64_t)s * n + i] * by : 0.0f);
+            p[h] = both(0.0f);
         }
-        z += (double)lse2;
+#pragma unroll 1
+        for (int32_t left = end - at - place * R, base = at; base < end; base += ROWS, left -= ROWS) {  // left: rows from the first one of this turn on
+            float2 v[R][H];
+            float top[R], two[2 * R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                top[r] = larger(next[r][0].x, next[r][0].y);
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    v[r][h] = next[r][h];
+                    if (h > 0) top[r] = larger(larger(v[r][h].x, v[r][h].y), top[r]);
+                }
+            }
+            if (base + ROWS < end) fetch();
+            over_lanes<R, LANES>(top, sh, larger);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (top[r] == -CUDART_INF_F) top[r] = 0.0f;  // no expert left, or no row: every power is 0
+                float2 sum = both(0.0f), pull = both(0.0f);
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    const float2 t2 = mul2(fma2(v[r][h], both(1.0f), both(-top[r])), both(LOG2_E));
+                    v[r][h] = make_float2(power_of_two(t2.x), power_of_two(t2.y));
+                    sum = fma2(v[r][h], both(1.0f), sum);
+                    pull = fma2(c[h], v[r][h], pull);
+                }
+                two[2 * r] = sum.x + sum.y;
+                two[2 * r + 1] = pull.x + pull.y;
+            }
+            over_lanes<2 * R, LANES>(two, sh, [](float x, float y) { return x + y; });
+            float *d = d_at;
+#pragma unroll
+            for (int r = 0; r < R; ++r, d += n) {
+                const bool empty = two[2 * r] == 0.0f;
+                const float by_sum = empty ? 0.0f : __fdividef(1.0f, two[2 * r]), lse = empty ? 0.0f : top[r] + logf(two[2 * r]);
+                const float pull = fmaf(two[2 * r + 1], -by_sum, by_z * lse) * by_sum;
+                lse2 = fmaf(lse, lse, lse2);
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    p[h] = fma2(v[r][h], both(by_sum), p[h]);
+                    v[r][h] = mul2(v[r][h], fma2(c[h], both(by_sum), both(pull)));
+                }
+                if (GRAD && r < left) mine.store(d, v[r]);
+            }
+            if constexpr (GRAD) d_at += (int64_t)ROWS * n;
+        }
+        if (lane == 0) z += (double)lse2;
         // the block's sums of this sequence: rows of a warp, then warps
 #pragma unroll
         for (int off = LANES; off < 32; off <<= 1)
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) p[u][i] += __shfl_xor_sync(0xffffffffu, p[u][i], off);
-        float *to = w.part + ((int64_t)blockIdx.x + s) * n;
+            for (int h = 0; h < H; ++h) {
+                p[h].x += __shfl_xor_sync(0xffffffffu, p[h].x, off);
+                p[h].y += __shfl_xor_sync(0xffffffffu, p[h].y, off);
+            }
+        float *to = w.part + ((int64_t)block + s) * n;
         if constexpr (LANES > 32) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (column(u) < n) p[u].store(to + column(u));
+            mine.store(to + lane * VEC, p);
         } else {
             __syncthreads();
-            if ((threadIdx.x & 31) < LANES)
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (column(u) < n) p[u].store(sums + (threadIdx.x >> 5) * n + column(u));
+            if ((threadIdx.x & 31) < LANES) mine.store(sums + (threadIdx.x >> 5) * n + lane * VEC, p);
             __syncthreads();
             for (int32_t j = threadIdx.x; j < n; j += THREADS) {
                 float v = sums[j];
@@ -279,39 +349,59 @@ __global__ void __launch_bounds__(THREADS) router_rows_kernel(const RouterLossAr
         at = end;
         if (at >= t.y) ++s;
     }
-    z = sum_of_block(z, wide);
-    if (threadIdx.x == 0) w.z[blockIdx.x] = z;
+    z = sum_of_block<WARPS>(z, wide);
+    if (threadIdx.x == 0) w.z[block] = z;
+}
+template <int LANES, int U, int VEC, int R, bool GRAD>
+__global__ void __launch_bounds__(THREADS, U * VEC <= 16 ? 2 : 1) router_rows_kernel(const RouterLossArgs a, const Scratch w, int32_t chunk_rows) {
+    extern __shared__ __align__(16) float sums[];  // [WARPS][n]
+    __shared__ float sh[2 * WARPS];
+    __shared__ double wide[WARPS];
+    const int32_t first = (int32_t)blockIdx.x * chunk_rows, last = min(first + chunk_rows, (int32_t)a.T);
+    wait_previous_kernel();
+    router_rows<LANES, U, VEC, R, GRAD>(a, w, blockIdx.x, first, last, sums, wide, sh);
 }
 
-// prob_sums of a sequence's 32 columns from the chunks that it lies in, and the two losses by the last block to be done
-__global__ void __launch_bounds__(THREADS) router_sums_kernel(const RouterLossArgs a, const Scratch w, int32_t chunk_rows, int32_t chunks) {
-    __shared__ double wide[WARPS], cols[WARPS][32];
+// What `v`, of every warp's lanes' columns, comes to: prob_sums and the sequence's part of the balance loss
+__device__ __forceinline__ double put_sums(const RouterLossArgs &a, const Scratch &w, int32_t s, int32_t j, double v) {
+    if (j >= a.n) return 0.0;
+    if (a.prob_sums) a.prob_sums[(int64_t)s * a.n + j] = (float)v;
+    const int32_t live = w.live[s];
+    return live > 0 ? v * (double)a.counts[(int64_t)s * a.n + j] / live : 0.0;
+}
+__device__ __forceinline__ void put_losses(const RouterLossArgs &a, double all, double balance, double z) {
+    a.losses[0] = all > 0.0 ? (float)((double)a.w_balance * a.n / ((double)a.k * all) * balance) : 0.0f;
+    a.losses[1] = all > 0.0 ? (float)((double)a.w_z / all * z) : 0.0f;
+}
+// prob_sums of a sequence's 32 columns from the chunks that it lies in, by the warps of a block together (their loads at once) or, where sequences are short, by one of them; and the
+// two losses by the last block to be done
+template <bool BLOCK>
+__global__ void __launch_bounds__(SUM_WARPS * 32) router_sums_kernel(const RouterLossArgs a, const Scratch w, int32_t chunk_rows, int32_t chunks) {
+    __shared__ double wide[SUM_WARPS], cols[SUM_WARPS][33];
     __shared__ bool last_one;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t groups = (a.n + 31) / 32;
+    const int64_t items = (int64_t)a.S * groups;
     wait_previous_kernel();
-    double all = 0.0, balance = 0.0;
-    for (int32_t s = threadIdx.x; s < a.S; s += THREADS) all += (double)w.live[s];
-    all = sum_of_block(all, wide);
-    for (int64_t item = blockIdx.x; item < (int64_t)a.S * groups; item += gridDim.x) {
+    double balance = 0.0;
+    for (int64_t item = BLOCK ? blockIdx.x : (int64_t)blockIdx.x * SUM_WARPS + warp; item < items; item += (int64_t)gridDim.x * (BLOCK ? 1 : SUM_WARPS)) {
         const int32_t s = (int32_t)(item / groups), j = (int32_t)(item % groups) * 32 + lane;
         const int2 t = tokens_of(a, s);
         double v = 0.0;
         if (t.y > t.x && j < a.n)
-#pragma unroll 4
-            for (int32_t c = t.x / chunk_rows + warp; c <= (t.y - 1) / chunk_rows; c += WARPS) v += (double)w.part[((int64_t)c + s) * a.n + j];
-        __syncthreads();
-        cols[warp][lane] = v;
-        __syncthreads();
-        if (warp == 0 && j < a.n) {
-#pragma unroll
-            for (int q = 1; q < WARPS; ++q) v += cols[q][lane];
-            if (a.prob_sums) a.prob_sums[(int64_t)s * a.n + j] = (float)v;
-            const int32_t live = w.live[s];
-            if (live > 0) balance += v * (double)a.counts[(int64_t)s * a.n + j] / live;
+#pragma unroll 5
+            for (int32_t c = t.x / chunk_rows + (BLOCK ? warp : 0); c <= (t.y - 1) / chunk_rows; c += BLOCK ? SUM_WARPS : 1) v += (double)w.part[((int64_t)c + s) * a.n + j];
+        if constexpr (BLOCK) {
+            __syncthreads();
+            cols[warp][lane] = v;
+            __syncthreads();
+            v = warp_sum(cols[lane][warp]);  // of column `warp`
+            if (lane == 0) balance += put_sums(a, w, s, j - lane + warp, v);
+        } else {
+            balance += put_sums(a, w, s, j, v);
         }
     }
-    balance = sum_of_block(balance, wide);
+    balance = sum_of_block<SUM_WARPS>(balance, wide);
     if (threadIdx.x == 0) {
         w.balance[blockIdx.x] = balance;
         __threadfence();
@@ -321,62 +411,116 @@ __global__ void __launch_bounds__(THREADS) router_sums_kernel(const RouterLossAr
     if (!last_one) return;
     __threadfence();
     balance = 0.0;
-    double z = 0.0;
-    for (int32_t i = threadIdx.x; i < (int32_t)gridDim.x; i += THREADS) balance += __ldcg(w.balance + i);
-    for (int32_t i = threadIdx.x; i < chunks; i += THREADS) z += w.z[i];
-    balance = sum_of_block(balance, wide);
-    z = sum_of_block(z, wide);
-    if (threadIdx.x == 0) {
-        a.losses[0] = all > 0.0 ? (float)((double)a.w_balance * a.n / ((double)a.k * all) * balance) : 0.0f;
-        a.losses[1] = all > 0.0 ? (float)((double)a.w_z / all * z) : 0.0f;
-    }
+    double z = 0.0, all = 0.0;
+    for (int32_t i = threadIdx.x; i < (int32_t)gridDim.x; i += SUM_WARPS * 32) balance += __ldcg(w.balance + i);
+    for (int32_t i = threadIdx.x; i < chunks; i += SUM_WARPS * 32) z += w.z[i];
+    for (int32_t s = threadIdx.x; s < a.S; s += SUM_WARPS * 32) all += (double)w.live[s];
+    balance = warp_sum(balance);
+    z = warp_sum(z);
+    all = warp_sum(all);
+    if (lane == 0) { cols[0][warp] = balance; cols[1][warp] = z; cols[2][warp] = all; }
+    __syncthreads();
+    if (warp > 0) return;
+    balance = warp_sum(cols[0][lane]);
+    z = warp_sum(cols[1][lane]);
+    all = warp_sum(cols[2][lane]);
+    if (lane == 0) put_losses(a, all, balance, z);
 }
 
-template <int LANES, int U, int VEC> int32_t rows(const RouterLossArgs &a, const Scratch &w, cudaStream_t st) {
+// Everything by one block, for a few rows
+template <int LANES, int U, int VEC, int R, bool GRAD>
+__global__ void __launch_bounds__(THREADS) router_small_kernel(const RouterLossArgs a, const Scratch w, const Divisor by_k) {
+    extern __shared__ __align__(16) float sums[];  // [WARPS][n], and the counts [n + 1] of a sequence before
+    __shared__ float sh[2 * WARPS];
+    __shared__ double wide[WARPS];
+    wait_previous_kernel();
+    int32_t *hist = reinterpret_cast<int32_t *>(sums);
+    for (int32_t s = 0; s < a.S; ++s) {
+        for (int32_t j = threadIdx.x; j <= a.n; j += THREADS) hist[j] = 0;
+        __syncthreads();
+        count_choices(a, by_k, s, 0, 1, hist);
+        __syncthreads();
+        for (int32_t j = threadIdx.x; j <= a.n; j += THREADS) {
+            if (j < a.n) a.counts[(int64_t)s * a.n + j] = hist[j];
+            else w.live[s] = hist[j];
+        }
+        __syncthreads();
+    }
+    router_rows<LANES, U, VEC, R, GRAD>(a, w, 0, 0, (int32_t)a.T, sums, wide, sh);
+    __syncthreads();
+    double balance = 0.0, all = 0.0;
+    for (int32_t i = threadIdx.x; i < a.S * a.n; i += THREADS) {
+        const int32_t s = i / a.n, j = i - s * a.n;
+        const int2 t = tokens_of(a, s);
+        balance += put_sums(a, w, s, j, t.y > t.x ? (double)w.part[(int64_t)s * a.n + j] : 0.0);
+    }
+    for (int32_t s = threadIdx.x; s < a.S; s += THREADS) all += (double)w.live[s];
+    balance = sum_of_block<WARPS>(balance, wide);
+    all = sum_of_block<WARPS>(all, wide);
+    if (threadIdx.x == 0) put_losses(a, all, balance, w.z[0]);
+}
+
+// One block: as many rows and columns as it has done while a second launch would begin
+constexpr int64_t SMALL = 8192;
+bool small(const RouterLossArgs &a) { return a.T * a.n <= SMALL && (int64_t)a.S * a.n <= SMALL && a.n <= 1024 && a.S <= 16; }
+
+template <int LANES, int U, int VEC, int R> int32_t rows(const RouterLossArgs &a, const Scratch &w, cudaStream_t st) {
     const size_t bytes = LANES > 32 ? 0 : (size_t)WARPS * a.n * sizeof(float);  // at most 32 KiB
-    const unsigned grid = (unsigned)chunks_of(a.T);
-    const int32_t chunk = (int32_t)rows_of_chunk(a.T);
-    if (a.dlogits) launch_kernel(router_rows_kernel<LANES, U, VEC, true>, grid, THREADS, bytes, st, a, w, chunk);
-    else launch_kernel(router_rows_kernel<LANES, U, VEC, false>, grid, THREADS, bytes, st, a, w, chunk);
+    if constexpr (LANES <= 32) {
+        if (small(a)) {
+            const size_t both = imax((int64_t)bytes, (a.n + 1) * 4);
+            launch_kernel(a.dlogits ? router_small_kernel<LANES, U, VEC, R, true> : router_small_kernel<LANES, U, VEC, R, false>, dim3(1), dim3(THREADS), both, st, a, w, Divisor::of(a.k));
+            MOE_LAUNCHED();
+            return MOE_OK;
+        }
+    }
+    launch_kernel(a.dlogits ? router_rows_kernel<LANES, U, VEC, R, true> : router_rows_kernel<LANES, U, VEC, R, false>, dim3((unsigned)chunks_of(a.T)), dim3(THREADS), bytes, st, a, w,
+                  (int32_t)rows_of_chunk(a.T));
     MOE_LAUNCHED();
     return MOE_OK;
 }
 int32_t launch_rows(const RouterLossArgs &a, const Scratch &w, cudaStream_t st) {
     if (a.n % 4 == 0) {
-        if (a.n <= 32) return rows<8, 1, 4>(a, w, st);
-        if (a.n <= 64) return rows<16, 1, 4>(a, w, st);
-        if (a.n <= 128) return rows<32, 1, 4>(a, w, st);
-        if (a.n <= 256) return rows<32, 2, 4>(a, w, st);
-        if (a.n <= 512) return rows<32, 4, 4>(a, w, st);
-        if (a.n <= 1024) return rows<32, 8, 4>(a, w, st);
-        if (a.n <= 2048) return rows<256, 2, 4>(a, w, st);
-        return rows<256, 8, 4>(a, w, st);
+        if (a.n <= 32) return rows<8, 1, 4, 4>(a, w, st);
+        if (a.n <= 64) return rows<16, 1, 4, 4>(a, w, st);
+        if (a.n <= 128) return rows<32, 1, 4, 4>(a, w, st);
+        if (a.n <= 256) return rows<32, 2, 4, 4>(a, w, st);
+        if (a.n <= 512) return rows<32, 4, 4, 1>(a, w, st);
+        if (a.n <= 1024) return rows<32, 8, 4, 1>(a, w, st);
+        if (a.n <= 2048) return rows<256, 2, 4, 1>(a, w, st);
+        return rows<256, 8, 4, 1>(a, w, st);
     }
-    if (a.n <= 32) return rows<32, 1, 1>(a, w, st);
-    if (a.n <= 128) return rows<32, 4, 1>(a, w, st);
-    if (a.n <= 512) return rows<32, 16, 1>(a, w, st);
-    if (a.n <= 1024) return rows<32, 32, 1>(a, w, st);
-    if (a.n <= 2048) return rows<256, 8, 1>(a, w, st);
-    return rows<256, 32, 1>(a, w, st);
+    if (a.n <= 32) return rows<16, 2, 1, 4>(a, w, st);
+    if (a.n <= 128) return rows<32, 4, 1, 4>(a, w, st);
+    if (a.n <= 512) return rows<32, 16, 1, 1>(a, w, st);
+    if (a.n <= 1024) return rows<32, 32, 1, 1>(a, w, st);
+    if (a.n <= 2048) return rows<256, 8, 1, 1>(a, w, st);
+    return rows<256, 32, 1, 1>(a, w, st);
 }
 
 int32_t launch_counts(const RouterLossArgs &a, const Scratch &w, cudaStream_t st) {
     const size_t bytes = (size_t)(a.n + 1) * sizeof(int32_t);  // at most 32 KiB and a word
-    // one block a sequence once there are enough of them for most SMs
-    if (a.S * COUNT_CLUSTER > 148) {
-        launch_kernel(router_counts_kernel<false>, dim3((unsigned)a.S), dim3(THREADS), bytes, st, a, w);
+    // blocks for a sequence, so that most SMs have one
+    const int parts = a.S <= 9 ? 16 : a.S <= 18 ? 8 : a.S <= 37 ? 4 : a.S <= 74 ? 2 : 1;
+    if (parts == 1) {
+        launch_kernel(router_counts_kernel<false>, dim3((unsigned)a.S), dim3(COUNT_THREADS), bytes, st, a, w, Divisor::of(a.k), 1);
         MOE_LAUNCHED();
         return MOE_OK;
     }
+    static PerDevice wide;
+    const bool sixteen = wide.get([]() {
+        return cudaFuncSetAttribute(reinterpret_cast<const void *>(router_counts_kernel<true>), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess ? 1 : 0;
+    }) > 0;
+    if (!sixteen) return MOE_ERR_CUDA;
     cudaLaunchAttribute attrs[2];
     attrs[0].id = cudaLaunchAttributeClusterDimension;
-    attrs[0].val.clusterDim.x = COUNT_CLUSTER; attrs[0].val.clusterDim.y = 1; attrs[0].val.clusterDim.z = 1;
+    attrs[0].val.clusterDim.x = parts; attrs[0].val.clusterDim.y = 1; attrs[0].val.clusterDim.z = 1;
     attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // as launch_kernel
     attrs[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.S * COUNT_CLUSTER); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = bytes; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(a.S * parts)); cfg.blockDim = dim3(COUNT_THREADS); cfg.dynamicSmemBytes = bytes; cfg.stream = st;
     cfg.attrs = attrs; cfg.numAttrs = 2;
-    cudaLaunchKernelEx(&cfg, router_counts_kernel<true>, a, w);
+    cudaLaunchKernelEx(&cfg, router_counts_kernel<true>, a, w, Divisor::of(a.k), parts);
     MOE_LAUNCHED();
     return MOE_OK;
 }
@@ -392,10 +536,14 @@ int64_t router_losses_bytes(int64_t T, int32_t n, int32_t S) {
 int32_t launch_router_losses(const RouterLossArgs &a, void *ws, cudaStream_t st) {
     Carver cv(ws);
     const Scratch w = scratch_at(cv, a.T, a.n, a.S);
-    MOE_TRY(launch_counts(a, w, st));
+    const bool one = small(a);
+    if (!one) MOE_TRY(launch_counts(a, w, st));
     MOE_TRY(launch_rows(a, w, st));
-    const int64_t items = (int64_t)a.S * cdiv(a.n, 32);
-    launch_kernel(router_sums_kernel, dim3((unsigned)imin(items, SUM_BLOCKS)), dim3(THREADS), 0, st, a, w, (int32_t)rows_of_chunk(a.T), (int32_t)chunks_of(a.T));
+    if (one) return MOE_OK;
+    const int64_t items = (int64_t)a.S * cdiv(a.n, 32), chunk = rows_of_chunk(a.T);
+    const bool blocks = a.T > 4 * chunk * a.S;  // a warp each where a sequence lies in four chunks or fewer
+    launch_kernel(blocks ? router_sums_kernel<true> : router_sums_kernel<false>, dim3((unsigned)imin(blocks ? items : cdiv(items, SUM_WARPS), SUM_BLOCKS)), dim3(SUM_WARPS * 32), 0, st, a, w,
+                  (int32_t)chunk, (int32_t)chunks_of(a.T));
     MOE_LAUNCHED();
     return MOE_OK;
 }
