@@ -21,11 +21,10 @@ constexpr int CHUNK = THREADS * EACH * TURNS;  // elements of a block
 constexpr int64_t MOST_X = (int64_t)1 << 30;   // bytes of X of a launch (one matrix at least)
 
 struct Passes {
-    double *part;     // [matrices][chunks] sums of squares
-    __half *x;
+    double *part;     // a sum of squares for every block of the first pass
     int32_t *done;    // [matrices]
     int32_t *next, *status;
-    int32_t chunks, clear_status, nesterov;
+    int32_t clear_status, nesterov;
     float momentum, eps, grad_scale;
     const moe_muon_rates *rates;
 };
@@ -104,10 +103,21 @@ __device__ __forceinline__ double momentum_chunk(const GT *g, MT *m, int64_t at,
     return sum;
 }
 template <bool VECTORS>
+__device__ __forceinline__ double momentum_block(const MuonEntry &t, int64_t at, int64_t end, float grad_scale, const Passes &k) {
+    switch (t.kind & 6) {
+        case 0: return momentum_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k);
+        case 2: return momentum_chunk<bf16, float, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k);
+        case 4: return momentum_chunk<float, bf16, VECTORS>(static_cast<const float *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k);
+        default: return momentum_chunk<bf16, bf16, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k);
+    }
+}
 __global__ void __launch_bounds__(THREADS) muon_momentum_kernel(const __grid_constant__ MuonBatch b, const Passes k) {
     __shared__ double sh[WARPS];
     wait_previous_kernel();
-    const int32_t matrix = blockIdx.x / k.chunks, chunk = blockIdx.x % k.chunks;
+    int q = 0;
+    while (q + 1 < b.shapes && (int32_t)blockIdx.x >= b.s[q + 1].chunks_before) ++q;
+    const MuonShape &s = b.s[q];
+    const int32_t here = (int32_t)blockIdx.x - s.chunks_before, in_shape = here / s.chunks, chunk = here - in_shape * s.chunks, matrix = s.first + in_shape;
     if (threadIdx.x == 0 && chunk == 0) {
         k.done[matrix] = 0;
         if (matrix == 0) {
@@ -116,18 +126,12 @@ __global__ void __launch_bounds__(THREADS) muon_momentum_kernel(const __grid_con
         }
     }
     const int32_t i = b.entry_of(matrix);
-    const MuonEntry &t = b.t[i];
-    const int64_t each = (int64_t)b.rows * b.cols, first = (matrix - b.first[i]) * each, at = first + (int64_t)chunk * CHUNK, end = min(at + CHUNK, first + each);
+    const int64_t each = (int64_t)s.rows * s.cols, first = (matrix - b.before[i]) * each, at = first + (int64_t)chunk * CHUNK, end = min(at + CHUNK, first + each);
     const float grad_scale = k.rates ? k.rates->grad_scale : k.grad_scale;
-    double s;
-    switch (t.kind & 6) {
-        case 0: s = momentum_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k); break;
-        case 2: s = momentum_chunk<bf16, float, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k); break;
-        case 4: s = momentum_chunk<float, bf16, VECTORS>(static_cast<const float *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k); break;
-        default: s = momentum_chunk<bf16, bf16, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k); break;
-    }
-    s = sum_of_block(s, sh);
-    if (threadIdx.x == 0) k.part[blockIdx.x] = s;
+    // vectors of eight where every matrix begins at one
+    double v = each % EACH == 0 ? momentum_block<true>(b.t[i], at, end, grad_scale, k) : momentum_block<false>(b.t[i], at, end, grad_scale, k);
+    v = sum_of_block(v, sh);
+    if (threadIdx.x == 0) k.part[blockIdx.x] = v;
 }
 
 // X in rows of ld elements, zeros behind the columns: a block has CHUNK of them, a piece of eight a thread at a time
@@ -159,26 +163,34 @@ __device__ __forceinline__ void normalise_chunk(const GT *g, const MT *m, int64_
     }
 }
 template <bool VECTORS>
-__global__ void __launch_bounds__(THREADS) muon_normalise_kernel(const __grid_constant__ MuonBatch b, const Passes k, int32_t blocks, int32_t ld) {
+__device__ __forceinline__ void normalise_block(const MuonEntry &t, const MuonShape &s, int64_t first, __half *x, int64_t begin, float grad_scale, float by, const Passes &k) {
+    const int64_t pieces = (int64_t)s.rows * (s.ld / EACH);
+    switch (t.kind & 6) {
+        case 0: return normalise_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<const float *>(t.m), first, x, begin, pieces, s.cols, s.ld, grad_scale, by, k);
+        case 2: return normalise_chunk<bf16, float, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<const float *>(t.m), first, x, begin, pieces, s.cols, s.ld, grad_scale, by, k);
+        case 4: return normalise_chunk<float, bf16, VECTORS>(static_cast<const float *>(t.g), static_cast<const bf16 *>(t.m), first, x, begin, pieces, s.cols, s.ld, grad_scale, by, k);
+        default: return normalise_chunk<bf16, bf16, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<const bf16 *>(t.m), first, x, begin, pieces, s.cols, s.ld, grad_scale, by, k);
+    }
+}
+__global__ void __launch_bounds__(THREADS) muon_normalise_kernel(const __grid_constant__ MuonBatch b, const Passes k) {
     __shared__ double sh[WARPS];
     wait_previous_kernel();
-    const int32_t matrix = blockIdx.x / blocks, block = blockIdx.x % blocks;
-    double s = 0.0;
-    for (int32_t c = threadIdx.x; c < k.chunks; c += THREADS) s += k.part[(int64_t)matrix * k.chunks + c];
-    s = sqrt(sum_of_block(s, sh)) + (double)k.eps;
+    int q = 0;
+    while (q + 1 < b.shapes && (int32_t)blockIdx.x >= b.s[q + 1].blocks_before) ++q;
+    const MuonShape &s = b.s[q];
+    const int32_t here = (int32_t)blockIdx.x - s.blocks_before, in_shape = here / s.blocks, block = here - in_shape * s.blocks, matrix = s.first + in_shape;
+    double v = 0.0;
+    for (int32_t c = threadIdx.x; c < s.chunks; c += THREADS) v += k.part[s.chunks_before + (int64_t)in_shape * s.chunks + c];
+    v = sqrt(sum_of_block(v, sh)) + (double)k.eps;
     // a matrix whose norm is no finite number becomes NaN as a whole
-    const float by = s <= (double)FLT_MAX ? (float)((double)MUON_UNIT / s) : CUDART_NAN_F;
+    const float by = v <= (double)FLT_MAX ? (float)((double)MUON_UNIT / v) : CUDART_NAN_F;
     const int32_t i = b.entry_of(matrix);
-    const MuonEntry &t = b.t[i];
-    const int64_t first = (int64_t)(matrix - b.first[i]) * b.rows * b.cols, pieces = (int64_t)b.rows * (ld / EACH), begin = (int64_t)block * (CHUNK / EACH);
-    __half *x = k.x + (int64_t)matrix * b.rows * ld;
+    const int64_t first = (int64_t)(matrix - b.before[i]) * s.rows * s.cols, begin = (int64_t)block * (CHUNK / EACH);
+    __half *x = s.x + (int64_t)in_shape * s.rows * s.ld;
     const float grad_scale = k.rates ? k.rates->grad_scale : k.grad_scale;
-    switch (t.kind & 6) {
-        case 0: normalise_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<const float *>(t.m), first, x, begin, pieces, b.cols, ld, grad_scale, by, k); break;
-        case 2: normalise_chunk<bf16, float, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<const float *>(t.m), first, x, begin, pieces, b.cols, ld, grad_scale, by, k); break;
-        case 4: normalise_chunk<float, bf16, VECTORS>(static_cast<const float *>(t.g), static_cast<const bf16 *>(t.m), first, x, begin, pieces, b.cols, ld, grad_scale, by, k); break;
-        default: normalise_chunk<bf16, bf16, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<const bf16 *>(t.m), first, x, begin, pieces, b.cols, ld, grad_scale, by, k); break;
-    }
+    // vectors of eight where every row begins at one
+    if (s.cols % EACH == 0) normalise_block<true>(b.t[i], s, first, x, begin, grad_scale, by, k);
+    else normalise_block<false>(b.t[i], s, first, x, begin, grad_scale, by, k);
 }
 
 int32_t check_tensor(const moe_muon_tensor &t) {
@@ -194,67 +206,112 @@ int32_t check_tensor(const moe_muon_tensor &t) {
     return MOE_OK;
 }
 
-// What is launched together: matrices of one shape, as many as X has room for
-struct Launch {
-    MuonBatch batch;
-    int64_t matrices() const { return batch.first[batch.n]; }
+// The list's shapes, each with its tensors in the list's order
+struct Shape {
+    int32_t rows, cols;
+    int64_t matrices;
+    std::vector<int32_t> tensors;
+    int64_t x_bytes() const { return matrices * rows * muon_ld(cols) * 2; }
 };
-// The tensors in launches, shape by shape as they come first; `run` is given each
-template <typename Run> int32_t for_each_launch(const moe_muon_tensor *tensors, int32_t count, Run run) {
-    std::vector<char> taken;
-    try {
-        taken.assign((size_t)count, 0);
-    } catch (...) {
-        return MOE_ERR_WORKSPACE;
-    }
-    Launch l;
-    for (int32_t i = 0; i < count; ++i) {
-        if (taken[i] || tensors[i].count == 0) continue;
-        const int32_t rows = tensors[i].rows, cols = tensors[i].cols;
-        const int64_t each = (int64_t)rows * cols, most = imin((int64_t)1 << 20, imax(1, MOST_X / ((int64_t)rows * muon_ld(cols) * 2)));
-        l.batch.rows = rows; l.batch.cols = cols; l.batch.n = l.batch.first[0] = 0;
-        auto flush = [&]() -> int32_t {
-            if (l.batch.n == 0) return MOE_OK;
-            MOE_TRY(run(l));
-            l.batch.n = 0;
-            return MOE_OK;
-        };
-        for (int32_t j = i; j < count; ++j) {
-            const moe_muon_tensor &t = tensors[j];
-            if (taken[j] || t.count == 0 || t.rows != rows || t.cols != cols) continue;
-            taken[j] = 1;
-            for (int64_t from = 0; from < t.count;) {
-                if (l.batch.n == MUON_MAX_LIST || l.matrices() >= most) MOE_TRY(flush());
-                const int64_t here = imin(t.count - from, most - (l.batch.n ? l.matrices() : 0)), at = from * each;
-                auto on = [&](const void *p, int32_t type) { return static_cast<char *>(const_cast<void *>(p)) + at * (int64_t)act_bytes(type); };
-                MuonEntry &e = l.batch.t[l.batch.n];
+// Matrices from * matrices / parts on, up to those of the next part, of every shape; false: more tensors than a launch takes
+bool fill_batch(const moe_muon_tensor *tensors, const Shape *const *shapes, int n, int64_t part, int64_t parts, MuonBatch *b) {
+    b->n = b->shapes = b->before[0] = 0;
+    int64_t chunks = 0, blocks = 0;
+    for (int q = 0; q < n; ++q) {
+        const Shape &h = *shapes[q];
+        const int64_t from = h.matrices * part / parts, to = h.matrices * (part + 1) / parts, each = (int64_t)h.rows * h.cols;
+        if (from == to) continue;
+        MuonShape &s = b->s[b->shapes++];
+        s.rows = h.rows; s.cols = h.cols; s.ld = (int32_t)muon_ld(h.cols);
+        s.first = b->before[b->n]; s.matrices = (int32_t)(to - from);
+        s.chunks = (int32_t)cdiv(each, CHUNK); s.blocks = (int32_t)cdiv((int64_t)s.rows * s.ld, CHUNK);
+        s.chunks_before = (int32_t)chunks; s.blocks_before = (int32_t)blocks;
+        s.x = nullptr;
+        chunks += (to - from) * s.chunks; blocks += (to - from) * s.blocks;
+        if (chunks > INT32_MAX || blocks > INT32_MAX) return false;
+        int64_t at = 0;
+        for (int32_t i : h.tensors) {
+            const moe_muon_tensor &t = tensors[i];
+            const int64_t a = imax(from, at), z = imin(to, at + t.count);
+            if (a < z) {
+                if (b->n == MUON_MAX_LIST) return false;
+                auto on = [&](const void *p, int32_t type) { return static_cast<char *>(const_cast<void *>(p)) + (a - at) * each * (int64_t)act_bytes(type); };
+                MuonEntry &e = b->t[b->n];
                 e.w = on(t.w, t.w_type); e.g = on(t.g, t.g_type); e.m = on(t.m, t.m_type);
-                e.master = t.master ? t.master + at : nullptr;
+                e.master = t.master ? t.master + (a - at) * each : nullptr;
                 e.scale = t.scale; e.decay = t.weight_decay;
                 e.kind = (t.w_type == MOE_BF16 ? 1 : 0) | (t.g_type == MOE_BF16 ? 2 : 0) | (t.m_type == MOE_BF16 ? 4 : 0) | (t.master ? 8 : 0);
-                l.batch.first[l.batch.n + 1] = l.batch.first[l.batch.n] + (int32_t)here;
-                ++l.batch.n;
-                from += here;
+                b->before[b->n + 1] = b->before[b->n] + (int32_t)(z - a);
+                ++b->n;
+            }
+            at += t.count;
+        }
+    }
+    return true;
+}
+// The list in launches; `run` is given each. Shapes that fill the tiles of SM pairs go together, and those that do not; these go along with the others where they are an eighth of
+// their tiles or less: the chain of a gate's products then runs beside the experts'.
+template <typename Run> int32_t for_each_launch(const moe_muon_tensor *tensors, int32_t count, Run run) try {
+    std::vector<Shape> all;
+    for (int32_t i = 0; i < count; ++i) {
+        const moe_muon_tensor &t = tensors[i];
+        if (t.count == 0) continue;
+        size_t q = 0;
+        while (q < all.size() && (all[q].rows != t.rows || all[q].cols != t.cols)) ++q;
+        if (q == all.size()) all.push_back({t.rows, t.cols, 0, {}});
+        all[q].matrices += t.count;
+        all[q].tensors.push_back(i);
+    }
+    std::vector<const Shape *> kinds[2];  // single SMs, pairs
+    int64_t single = 0, paired = 0;
+    for (const Shape &s : all) {
+        const bool pair = ns_pairs(s.rows, s.cols);
+        kinds[pair].push_back(&s);
+        (pair ? paired : single) += s.matrices * ns_tiles(s.rows, s.cols, true);
+    }
+    if (single * 8 <= paired && kinds[0].size() + kinds[1].size() <= (size_t)MUON_MAX_SHAPES) {
+        kinds[1].insert(kinds[1].end(), kinds[0].begin(), kinds[0].end());
+        kinds[0].clear();
+    }
+    MuonBatch b;
+    for (int pair = 1; pair >= 0; --pair)
+        for (size_t from = 0; from < kinds[pair].size(); from += MUON_MAX_SHAPES) {
+            const Shape *const *shapes = kinds[pair].data() + from;
+            const int n = (int)imin(MUON_MAX_SHAPES, (int64_t)(kinds[pair].size() - from));
+            int64_t bytes = 0, most = 0;
+            for (int q = 0; q < n; ++q) { bytes += shapes[q]->x_bytes(); most = imax(most, shapes[q]->matrices); }
+            int64_t parts = imin(most, cdiv(bytes, MOST_X));
+            for (int64_t part = 0; part < parts; ++part)
+                if (!fill_batch(tensors, shapes, n, part, parts, &b)) {
+                    if (parts >= most) return MOE_ERR_UNSUPPORTED;
+                    parts = imin(most, 2 * parts);
+                    part = -1;
+                }
+            for (int64_t part = 0; part < parts; ++part) {
+                fill_batch(tensors, shapes, n, part, parts, &b);
+                if (b.n) MOE_TRY(run(b, pair != 0));
             }
         }
-        MOE_TRY(flush());
-    }
     return MOE_OK;
+} catch (...) {
+    return MOE_ERR_WORKSPACE;
 }
 struct Scratch {
     int32_t *done, *next;
     double *part;
-    __half *x;
     void *products;
 };
-Scratch scratch_of(Carver &cv, const Launch &l) {
-    const int64_t each = (int64_t)l.batch.rows * l.batch.cols;
+int64_t blocks_of(const MuonBatch &b, bool second) {
+    const MuonShape &s = b.s[b.shapes - 1];
+    return second ? s.blocks_before + (int64_t)s.matrices * s.blocks : s.chunks_before + (int64_t)s.matrices * s.chunks;
+}
+Scratch scratch_of(Carver &cv, MuonBatch &b, bool pair) {
     Scratch s;
     s.next = cv.take<int32_t>(1);
-    s.done = cv.take<int32_t>(l.matrices());
-    s.part = cv.take<double>(l.matrices() * cdiv(each, CHUNK));
-    s.x = cv.take<__half>(l.matrices() * l.batch.rows * muon_ld(l.batch.cols));
-    s.products = cv.take_bytes(ns_scratch_bytes(l.batch.rows, l.batch.cols, l.matrices()));
+    s.done = cv.take<int32_t>(b.matrices());
+    s.part = cv.take<double>(blocks_of(b, false));
+    for (int q = 0; q < b.shapes; ++q) b.s[q].x = cv.take<__half>((int64_t)b.s[q].matrices * b.s[q].rows * b.s[q].ld);
+    s.products = cv.take_bytes(ns_scratch_bytes(b, pair));
     return s;
 }
 
@@ -267,10 +324,10 @@ int32_t muon_check(const moe_muon_tensor *tensors, int32_t count) {
 
 int32_t muon_bytes(const moe_muon_tensor *tensors, int32_t count, int64_t *bytes) {
     *bytes = kWsHeader;
-    return for_each_launch(tensors, count, [&](const Launch &l) -> int32_t {
+    return for_each_launch(tensors, count, [&](MuonBatch &b, bool pair) -> int32_t {
         Carver cv(nullptr);
         cv.take_bytes(kWsHeader);
-        scratch_of(cv, l);
+        scratch_of(cv, b, pair);
         *bytes = imax(*bytes, (int64_t)cv.off);
         return MOE_OK;
     });
@@ -278,24 +335,19 @@ int32_t muon_bytes(const moe_muon_tensor *tensors, int32_t count, int64_t *bytes
 
 int32_t launch_muon(const moe_muon_tensor *tensors, int32_t count, const moe_muon_params &p, const moe_muon_rates *rates, void *ws, cudaStream_t st) {
     bool first = true;
-    return for_each_launch(tensors, count, [&](const Launch &l) -> int32_t {
+    return for_each_launch(tensors, count, [&](MuonBatch &b, bool pair) -> int32_t {
         Carver cv(ws);
         int32_t *status = static_cast<int32_t *>(cv.take_bytes(kWsHeader));
-        const Scratch s = scratch_of(cv, l);
-        const int64_t each = (int64_t)l.batch.rows * l.batch.cols, ld = muon_ld(l.batch.cols);
+        const Scratch s = scratch_of(cv, b, pair);
         Passes k = {};
-        k.part = s.part; k.x = s.x; k.done = s.done; k.next = s.next; k.status = status;
-        k.chunks = (int32_t)cdiv(each, CHUNK); k.clear_status = first; k.nesterov = p.nesterov;
+        k.part = s.part; k.done = s.done; k.next = s.next; k.status = status;
+        k.clear_status = first; k.nesterov = p.nesterov;
         k.momentum = (float)p.momentum; k.eps = (float)p.eps; k.grad_scale = (float)p.grad_scale; k.rates = rates;
-        const int64_t blocks = cdiv((int64_t)l.batch.rows * ld, CHUNK);
-        if (l.matrices() * imax(blocks, k.chunks) > INT32_MAX) return MOE_ERR_UNSUPPORTED;
-        const dim3 grid((unsigned)(l.matrices() * k.chunks)), grid2((unsigned)(l.matrices() * blocks));
-        // vectors of eight where every matrix, or every row, begins at one
-        launch_kernel(each % EACH == 0 ? muon_momentum_kernel<true> : muon_momentum_kernel<false>, grid, dim3(THREADS), 0, st, l.batch, k);
+        launch_kernel(muon_momentum_kernel, dim3((unsigned)blocks_of(b, false)), dim3(THREADS), 0, st, b, k);
         MOE_LAUNCHED();
-        launch_kernel(l.batch.cols % EACH == 0 ? muon_normalise_kernel<true> : muon_normalise_kernel<false>, grid2, dim3(THREADS), 0, st, l.batch, k, (int32_t)blocks, (int32_t)ld);
+        launch_kernel(muon_normalise_kernel, dim3((unsigned)blocks_of(b, true)), dim3(THREADS), 0, st, b, k);
         MOE_LAUNCHED();
-        const NsWork w = {&l.batch, (int32_t)l.matrices(), p.steps, s.x, s.done, s.next, status, s.products, (float)p.lr, rates};
+        const NsWork w = {&b, pair, p.steps, s.done, s.next, status, s.products, (float)p.lr, rates};
         MOE_TRY(launch_newton_schulz(w, st));
         first = false;
         return MOE_OK;

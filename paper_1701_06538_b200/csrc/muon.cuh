@@ -1,4 +1,4 @@
-// The Muon step's matrices of one shape, and the launcher of their Newton-Schulz products (newton_schulz.cu)
+// The matrices of a Muon step's launches, and the launcher of their Newton-Schulz products (newton_schulz.cu)
 #pragma once
 
 #include <cuda_fp16.h>
@@ -7,8 +7,8 @@
 
 namespace moe {
 
-constexpr int MUON_MAX_LIST = 64;           // tensors of a launch (a launch's parameters hold them: 3 KiB)
-constexpr float MUON_UNIT = 1024.0f;        // what 1 is held as in the products' 16-bit operands
+constexpr int MUON_MAX_LIST = 128, MUON_MAX_SHAPES = 6;  // tensors and shapes of a launch (its parameters hold them: 6 KiB, and 1.5 KiB of tensor maps a shape)
+constexpr float MUON_UNIT = 1024.0f;                     // what 1 is held as in the products' 16-bit operands
 struct MuonEntry {
     void *w, *m;
     const void *g;
@@ -16,27 +16,36 @@ struct MuonEntry {
     float scale, decay;
     int32_t kind;  // bit 0: bf16 weights, 1: bf16 gradients, 2: bf16 momentum, 3: float masters
 };
-// Matrices [rows, cols] of up to MUON_MAX_LIST tensors, numbered through
+struct MuonShape {
+    int32_t rows, cols, ld;      // ld: elements between rows of the operands, zeros behind the columns
+    int32_t first, matrices;     // its matrices are first .. first + matrices - 1
+    int32_t chunks, blocks;      // blocks a matrix takes in the first and the second pass
+    int32_t chunks_before, blocks_before;  // of the shapes before
+    __half *x;                   // [matrices][rows][ld] the updates over their norms, times MUON_UNIT; overwritten
+};
+// Matrices of up to MUON_MAX_LIST tensors, shape by shape, numbered through
 struct MuonBatch {
     MuonEntry t[MUON_MAX_LIST];
-    int32_t first[MUON_MAX_LIST + 1];  // matrices of the tensors before
-    int32_t n, rows, cols;
+    int32_t before[MUON_MAX_LIST + 1];  // matrices of the tensors before
+    MuonShape s[MUON_MAX_SHAPES];
+    int32_t n, shapes;
+    __host__ __device__ __forceinline__ int32_t matrices() const { return before[n]; }
     __device__ __forceinline__ int32_t entry_of(int32_t matrix) const {
         int32_t lo = 0, hi = n;
         while (hi - lo > 1) {
             const int32_t mid = (lo + hi) >> 1;
-            if (first[mid] <= matrix) lo = mid; else hi = mid;
+            if (before[mid] <= matrix) lo = mid; else hi = mid;
         }
         return lo;
     }
 };
-static inline int64_t muon_ld(int64_t cols) { return cdiv(cols, 64) * 64; }  // elements between rows of the operands, zeros behind the columns
+static inline int64_t muon_ld(int64_t cols) { return cdiv(cols, 64) * 64; }
 
-// Newton-Schulz products of a batch's matrices and the step on their weights. Scratch: ns_scratch_bytes behind 256 bytes
+// Newton-Schulz products of a batch's matrices and the step on their weights. Scratch: ns_scratch_bytes
 struct NsWork {
     const MuonBatch *batch;
-    int32_t matrices, steps;
-    __half *x;          // [matrices][rows][ld] the updates over their norms, times MUON_UNIT; overwritten
+    bool pair;          // see ns_pairs
+    int32_t steps;
     int32_t *done;      // [matrices] zeros
     int32_t *next;      // a zero
     int32_t *status;
@@ -44,7 +53,9 @@ struct NsWork {
     float lr;
     const moe_muon_rates *rates;  // or nullptr
 };
-int64_t ns_scratch_bytes(int32_t rows, int32_t cols, int64_t matrices);
+static inline bool ns_pairs(int32_t rows, int32_t cols) { return imin(rows, cols) > 128; }  // whether a shape fills tiles of SM pairs
+int64_t ns_tiles(int32_t rows, int32_t cols, bool pair);                                   // of a matrix, a step
+int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair);
 int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st);
 
 }  // namespace moe

@@ -12,17 +12,18 @@
 // An element's rounding error off the diagonal is one of many in a singular value and averages out; on the diagonal it scales a whole row, and near the singular value 1.2 a step
 // multiplies such an error by 5 (a gate of 512 x 32, whose A is nearly diagonal, was off by 3e-3 with rounded diagonals). Accumulators are float, and the last X is not rounded at all.
 //
-// All products of all matrices are one launch: tiles are drawn one after the other in an order in which what a tile reads is always drawn before it (group of matrices, step, product,
-// matrix, tile), and a count of stored tiles for every matrix tells when it is there. With a group of matrices that fills the SMs more than once, what a tile waits for was stored long
-// ago. (A launch for every product leaves its last wave of tiles half empty: 3 tiles of A and B and 8 of X for each of 512 x 1024.) Whoever waits does so for tiles of blocks that run
-// already, so that no number of resident blocks is presumed.
+// All products of all matrices, of several shapes, are one launch: tiles are drawn one after the other in an order in which what a tile reads is always drawn before it (group of
+// matrices, step, product, shape, matrix, tile), and a count of stored tiles for every matrix tells when it is there. With a group that fills the SMs more than once, what a tile waits
+// for was stored long ago, and the chain of a lone matrix' products (a gate's) runs beside the others'. (A launch for every product leaves its last wave of tiles half empty: 3 tiles of A and B
+// and 8 of X for each of 512 x 1024.) Whoever waits does so for tiles of blocks that run already, so that no number of resident blocks is presumed.
 //
 // PAIR: two CTAs (an SM pair) have a tile of 256 x 256 by cta_group::2, each stages 128 rows of A's operand and half of B's columns. Otherwise, for M up to 128, a CTA has 128 x 128.
-// Warp 0 copies operands, warp 1 issues the products, warps 2 to 9 store results, warp 10 draws tiles. Every wait is bounded (2 s); on expiry the CTA records MOE_ERR_TIMEOUT
-// in the workspace's status word and drains.
+// Warp 0 copies operands, warp 1 issues the products, warps 2 to 9 make results of accumulators, warp 10 draws tiles, warp 11 stores results and counts them. Every wait is bounded
+// (2 s); on expiry the CTA records MOE_ERR_TIMEOUT in the workspace's status word and drains.
 #include <string.h>
 
 #include "muon.cuh"
+#include "pairs.cuh"
 #include "tc.cuh"
 
 namespace moe {
@@ -31,57 +32,79 @@ namespace {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr int RING = 2;                       // tiles drawn ahead
-constexpr int NS_THREADS = 352;
+constexpr int NS_THREADS = 384;
 constexpr int NS_STAGES = 5;
-constexpr uint32_t BOX = 4096;                // a warp's 32 rows of 64 columns: what a result needs of the operand it is added to, then the result
-constexpr int NS_DATA = NS_STAGES * STAGE2_BYTES + 2 * 8 * BOX, NS_SMEM = NS_DATA + 1024 + 512;
+constexpr uint32_t BOX = 4096;                // a warp's 32 rows of 64 columns
+constexpr int NS_DATA = NS_STAGES * STAGE2_BYTES + 2 * 8 * BOX, NS_SMEM = NS_DATA + 1024 /*alignment*/ + 512 /*barriers, ring*/ + 8 * 128 /*factors*/;
 
 enum { FIRST = 0, SECOND = 1, THIRD = 2 };    // A, B, X
 struct NsMaps { CUtensorMap x_k[2], x_mn[2], x_box[2], a_k, a_mn, a_box, b_k, b_mn, b_box; };  // x[0]: all matrices, the others: a ring of slots
-struct NsArgs {
-    int32_t rows, cols, ld, M, Mld, matrices, steps, left;
+struct NsShape {
+    int32_t rows, cols, ld, M, Mld, first, matrices, left;
     int32_t square, cols3, tiles3;            // tiles of A and B (lower half), tiles of X beside each other, of X
-    int32_t group, slots, total;
-    int32_t *done, *next, *status;
+    int32_t group, slots;
+    const __half *x[2], *a;
     float *d, *r;                             // [slots][M] diagonals of A and B
+};
+struct NsArgs {
+    NsShape s[MUON_MAX_SHAPES];
+    int32_t shapes, steps, groups;
+    int32_t *done, *next, *status;
     float lr;
     const moe_muon_rates *rates;
 };
-struct NsTile { int32_t matrix, step, product, row, col; };
+struct NsAllMaps { NsMaps m[MUON_MAX_SHAPES]; };
+struct NsTile { int32_t matrix, shape, step, product, row, col; };
 
 template <bool PAIR> constexpr int tile_side() { return PAIR ? 256 : 128; }
-template <bool PAIR> constexpr int arrivals() { return PAIR ? 16 : 8; }  // of a stored tile: warps
+template <bool PAIR> constexpr int arrivals() { return PAIR ? 2 : 1; }  // of a stored tile: CTAs
 
-// Tile number `id`: {matrix or -1, step * 4 + product, row, column}
-template <bool PAIR> __device__ __forceinline__ int4 find_ns_tile(const NsArgs &p, int32_t id) {
-    if (id >= p.total) return make_int4(-1, 0, 0, 0);
-    const int32_t each = 2 * p.square + p.tiles3, per_group = p.group * p.steps * each;
-    const int32_t g = id / per_group, here = min(p.group, p.matrices - g * p.group);
-    int32_t r = id - g * per_group;
-    const int32_t step = r / (here * each);
-    r -= step * here * each;
-    int32_t product = FIRST, tiles = p.square;
-    if (r >= 2 * here * p.square) { product = THIRD; r -= 2 * here * p.square; tiles = p.tiles3; }
-    else if (r >= here * p.square) { product = SECOND; r -= here * p.square; }
-    const int32_t m = r / tiles;
-    int32_t t = r - m * tiles, row, col;
-    if (product == THIRD) {
-        row = t / p.cols3;
-        col = t - row * p.cols3;
-    } else {
-        for (row = 0; t > row; ++row) t -= row + 1;
-        col = t;
+// The tiles in their order: {matrix or -1, shape << 16 | step << 2 | product, row, column} of ascending numbers
+template <bool PAIR> struct NsOrder {
+    const NsArgs &p;
+    int32_t group, base, each;  // the group that is at, its first number, its tiles a step
+    __device__ __forceinline__ explicit NsOrder(const NsArgs &p_) : p(p_), group(0), base(0) { each = tiles_of(); }
+    __device__ __forceinline__ int32_t here(int s) const { return min(p.s[s].group, max(0, p.s[s].matrices - group * p.s[s].group)); }
+    __device__ __forceinline__ int32_t tiles_of() const {
+        int32_t n = 0;
+        for (int s = 0; s < p.shapes; ++s) n += here(s) * (2 * p.s[s].square + p.s[s].tiles3);
+        return n;
     }
-    return make_int4(g * p.group + m, step * 4 + product, row * tile_side<PAIR>(), col * tile_side<PAIR>());
-}
+    __device__ __forceinline__ int4 find(int32_t id) {
+        while (group < p.groups && id - base >= each * p.steps) {
+            base += each * p.steps;
+            ++group;
+            each = tiles_of();
+        }
+        if (group >= p.groups) return make_int4(-1, 0, 0, 0);
+        int32_t r = id - base;
+        const int32_t step = r / each;
+        r -= step * each;
+        for (int product = FIRST;; ++product)
+            for (int s = 0; s < p.shapes; ++s) {
+                const int32_t tiles = product == THIRD ? p.s[s].tiles3 : p.s[s].square, all = here(s) * tiles;
+                if (r >= all) { r -= all; continue; }
+                const int32_t m = r / tiles;
+                int32_t t = r - m * tiles, row, col;
+                if (product == THIRD) {
+                    row = t / p.s[s].cols3;
+                    col = t - row * p.s[s].cols3;
+                } else {
+                    for (row = 0; t > row; ++row) t -= row + 1;
+                    col = t;
+                }
+                return make_int4(group * p.s[s].group + m, s << 16 | step << 2 | product, row * tile_side<PAIR>(), col * tile_side<PAIR>());
+            }
+    }
+};
 __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
     int32_t v;
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
 // Arrivals that a matrix has when everything before this product is stored
-template <bool PAIR> __device__ __forceinline__ int32_t wanted(const NsArgs &p, const NsTile &t) {
-    return arrivals<PAIR>() * (t.step * (2 * p.square + p.tiles3) + t.product * p.square);
+template <bool PAIR> __device__ __forceinline__ int32_t wanted(const NsShape &s, const NsTile &t) {
+    return arrivals<PAIR>() * (t.step * (2 * s.square + s.tiles3) + t.product * s.square);
 }
 __device__ __forceinline__ bool wait_count(const int32_t *count, int32_t at_least, volatile int *abort_flag, int32_t *status) {
     if (load_acquire(count) >= at_least) return true;
@@ -129,17 +152,17 @@ template <bool PAIR> struct NsRing {
             else mbar_arrive(empty);
         }
         ++i;
-        t.matrix = a.x; t.step = a.y >> 2; t.product = a.y & 3; t.row = a.z; t.col = a.w;
+        t.matrix = a.x; t.shape = a.y >> 16; t.step = a.y >> 2 & 0x3fff; t.product = a.y & 3; t.row = a.z; t.col = a.w;
         return a.x >= 0;
     }
 };
 
 // 32 rows of 32 columns of the last X, which lie in `box` as floats, onto the weights: eight lanes a row, so that a row's 32 columns are read and written together
 template <bool BF16, bool MASTER, bool VECTORS>
-__device__ __forceinline__ void step_box(const NsArgs &p, const MuonEntry &e, int64_t first, int32_t rows_left, int32_t cols_left, const float *box, int lane, float lr) {
+__device__ __forceinline__ void step_box(int32_t cols, const MuonEntry &e, int64_t first, int32_t rows_left, int32_t cols_left, const float *box, int lane, float lr) {
     const int32_t c = (lane & 7) * 4;
     float4 w[8];
-    auto at = [&](int i) { return first + (int64_t)(4 * i + (lane >> 3)) * p.cols + c; };
+    auto at = [&](int i) { return first + (int64_t)(4 * i + (lane >> 3)) * cols + c; };
     auto in = [&](int i) { return 4 * i + (lane >> 3) < rows_left && c < cols_left; };
     const float *floats = MASTER ? e.master : static_cast<const float *>(e.w);
     bf16 *halves = static_cast<bf16 *>(e.w);
@@ -189,8 +212,51 @@ __device__ __forceinline__ void step_box(const NsArgs &p, const MuonEntry &e, in
     }
 }
 
+// What a result is, besides the accumulator
+enum Result { K_FIRST, K_SECOND, K_THIRD, K_LAST };
+// 32 columns of 32 rows, a row a lane. old: 32 halves of the operand that is added, row_factor and cols: the diagonal's elements of the row and of the columns (shared memory)
+template <int KIND, bool COLS>
+__device__ __forceinline__ void finish(float2 (&v)[16], const uint32_t *old, float row_factor, const float *cols) {
+    constexpr float UNIT = 1.0f / MUON_UNIT;
+    constexpr float by = KIND == K_SECOND ? NS_C * UNIT : KIND == K_LAST ? UNIT * UNIT : UNIT;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        float4 c = make_float4(row_factor, row_factor, row_factor, row_factor);
+        if constexpr (COLS) {
+            const float4 of = *reinterpret_cast<const float4 *>(cols + 4 * q);
+            c = KIND == K_SECOND ? make_float4(c.x + of.x, c.y + of.y, c.z + of.z, c.w + of.w) : of;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float2 &y = v[2 * q + j];
+            if constexpr (KIND == K_FIRST) {
+                y = mul2(y, both(by));
+            } else {
+                float2 f = j ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
+                if constexpr (KIND == K_SECOND) f = fma2(f, both(NS_C), both(NS_B));
+                if constexpr (KIND == K_LAST) f = mul2(f, both(UNIT));
+                const float2 o = __half22float2(*reinterpret_cast<const __half2 *>(old + 2 * q + j));
+                y = fma2(y, both(by), mul2(o, f));
+            }
+        }
+    }
+}
+// 64 halves of a row: what another SM's copies have stored
+__device__ __forceinline__ void load_old(const __half *from, bool in, uint32_t (&old)[32]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t *r = old + 8 * q;
+        if (in)
+            asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(from + 16 * q) : "memory");
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] = 0u;
+    }
+}
+
 template <bool PAIR>
-__global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsArgs p, const __grid_constant__ MuonBatch batch) {
+__global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __grid_constant__ NsAllMaps all_maps, const __grid_constant__ NsArgs p, const __grid_constant__ MuonBatch batch) {
     constexpr int SIDE = tile_side<PAIR>(), NST = NS_STAGES, STAGE = STAGE2_BYTES, ACC = SIDE;  // ACC: columns of an accumulator
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -200,7 +266,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
     auto empty_bar = [&](int s) { return bars + 8u * (NST + s); };
     auto tfull_bar = [&](int a) { return bars + 8u * (2 * NST + a); };
     auto tempty_bar = [&](int a) { return bars + 8u * (2 * NST + 2 + a); };
-    const uint32_t ring_full0 = bars + 128, ring_empty0 = bars + 160, ring = bars + 256, box_bar0 = bars + 320;
+    const uint32_t ring_full0 = bars + 128, ring_empty0 = bars + 160, box_ready0 = bars + 208, box_empty0 = bars + 224, ring = bars + 256;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + NS_DATA + 192);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + NS_DATA + 200);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -208,10 +274,10 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < NST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), arrivals<PAIR>()); }
-        // readers of a record: producer and 8 epilogue warps in each CTA, the MMA warp of the even one
-        for (int q = 0; q < RING; ++q) { mbar_init(ring_full0 + 8u * q, 1); mbar_init(ring_empty0 + 8u * q, PAIR ? 19 : 10); }
-        for (int q = 0; q < 16; ++q) mbar_init(box_bar0 + 8u * q, 1);
+        for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), PAIR ? 16 : 8); }
+        // readers of a record: producer, 8 epilogue warps and storer in each CTA, the MMA warp of the even one
+        for (int q = 0; q < RING; ++q) { mbar_init(ring_full0 + 8u * q, 1); mbar_init(ring_empty0 + 8u * q, PAIR ? 21 : 11); }
+        for (int u = 0; u < 2; ++u) { mbar_init(box_ready0 + 8u * u, 8); mbar_init(box_empty0 + 8u * u, 1); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -231,15 +297,24 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
     const uint32_t tmem_base = *tmem_slot;
     wait_previous_kernel();
 
-    const int kblocks1 = ((p.left ? p.cols : p.rows) + BK - 1) / BK, kblocks2 = (p.M + BK - 1) / BK;
-    auto kblocks_of = [&](const NsTile &t) { return t.product == FIRST ? kblocks1 : kblocks2; };
+    auto kblocks_of = [&](const NsShape &s, const NsTile &t) { return ((t.product == FIRST ? (s.left ? s.cols : s.rows) : s.M) + BK - 1) / BK; };
     // columns that exist of a tile's output, and of the product (both CTAs' halves of B's operand begin at multiples of 64)
-    auto cols_out = [&](const NsTile &t) { return t.product == THIRD ? p.ld : p.Mld; };
-    auto width_of = [&](const NsTile &t) { return PAIR && cols_out(t) - t.col > 128 ? 256 : 128; };
+    auto cols_out = [&](const NsShape &s, const NsTile &t) { return t.product == THIRD ? s.ld : s.Mld; };
+    auto width_of = [&](const NsShape &s, const NsTile &t) { return PAIR && cols_out(s, t) - t.col > 128 ? 256 : 128; };
     // Where an operand lies in a product whose contraction runs along the shorter side: block kb of it is in the lower half for rows from `at` on, or has to be transposed
     auto upper = [&](int kb, int32_t at) { return kb * BK / SIDE > at / SIDE; };
-    auto a_is_mn = [&](const NsTile &t, int kb) { return t.product == FIRST ? !p.left : t.product == THIRD && !p.left ? false : upper(kb, t.row); };
-    auto b_is_mn = [&](const NsTile &t, int kb) { return t.product == FIRST ? !p.left : t.product == THIRD && p.left ? true : upper(kb, t.col); };
+    auto a_is_mn = [&](const NsShape &s, const NsTile &t, int kb) { return t.product == FIRST ? !s.left : t.product == THIRD && !s.left ? false : upper(kb, t.row); };
+    auto b_is_mn = [&](const NsShape &s, const NsTile &t, int kb) { return t.product == FIRST ? !s.left : t.product == THIRD && s.left ? true : upper(kb, t.col); };
+    // a warp's boxes of a tile: the rows, the first column and how many there are
+    auto boxes_of = [&](const NsShape &s, const NsTile &t, int w, int32_t &row0, int32_t &first) {
+        const int32_t width = width_of(s, t);
+        row0 = t.row + 128 * (int)rank + 32 * ((w + 2) & 3);  // (epilogue warps are warps 2 to 9, and their quarter of the accumulator's rows is warp % 4)
+        first = t.col + (w >> 2) * (width / 2);
+        return row0 < (t.product == THIRD ? s.rows : s.M) ? max(0, min(width / 128, (cols_out(s, t) - first) / 64)) : 0;
+    };
+    auto gave_up = [&]() {  // copies in flight have landed long before a millisecond is over, and only then may the CTA exit
+        for (const unsigned long long t0 = global_ns(); global_ns() - t0 < 1000000ull;) {}
+    };
 
     if (warp == 0) {
         // ------------------------------------------------------------------ bulk tensor copies (both CTAs)
@@ -250,18 +325,21 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, false, true, 0};
             NsTile t;
             while (ok && tiles.next(t)) {
-                ok = wait_count(p.done + t.matrix, wanted<PAIR>(p, t), abort_flag, p.status);
-                if (ok && t.step == 0 && t.product == FIRST && t.matrix >= p.slots)  // the slot's last user has read what is overwritten now
-                    ok = wait_count(p.done + t.matrix - p.slots, arrivals<PAIR>() * p.steps * (2 * p.square + p.tiles3), abort_flag, p.status);
+                const NsShape &h = p.s[t.shape];
+                const NsMaps &maps = all_maps.m[t.shape];
+                const int32_t *count = p.done + h.first + t.matrix;
+                ok = wait_count(count, wanted<PAIR>(h, t), abort_flag, p.status);
+                if (ok && t.step == 0 && t.product == FIRST && t.matrix >= h.slots)  // the slot's last user has read what is overwritten now
+                    ok = wait_count(count - h.slots, arrivals<PAIR>() * p.steps * (2 * h.square + h.tiles3), abort_flag, p.status);
                 if (!ok) break;
                 fence_async();  // what other SMs' copies have stored, before this thread's copies read it
-                const int slot = t.matrix % p.slots, x = t.step & 1, xm = x ? slot : t.matrix;
-                const bool a_x = t.product == FIRST || (t.product == THIRD && !p.left), b_x = t.product == FIRST || (t.product == THIRD && p.left);
+                const int slot = t.matrix % h.slots, x = t.step & 1, xm = x ? slot : t.matrix;
+                const bool a_x = t.product == FIRST || (t.product == THIRD && !h.left), b_x = t.product == FIRST || (t.product == THIRD && h.left);
                 const CUtensorMap *sym_k = t.product == SECOND ? &maps.a_k : &maps.b_k, *sym_mn = t.product == SECOND ? &maps.a_mn : &maps.b_mn;
                 const CUtensorMap *ak = a_x ? &maps.x_k[x] : sym_k, *an = a_x ? &maps.x_mn[x] : sym_mn, *bk = b_x ? &maps.x_k[x] : sym_k, *bn = b_x ? &maps.x_mn[x] : sym_mn;
                 const int am = a_x ? xm : slot, bm = b_x ? xm : slot;
-                const int a0 = t.row + 128 * (int)rank, b0 = t.col + (PAIR ? width_of(t) / 2 * (int)rank : 0);
-                const int kblocks = kblocks_of(t);
+                const int a0 = t.row + 128 * (int)rank, b0 = t.col + (PAIR ? width_of(h, t) / 2 * (int)rank : 0);
+                const int kblocks = kblocks_of(h, t);
                 for (int kb = 0; kb < kblocks; ++kb) {
                     ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.status);
                     if (!ok) break;
@@ -275,14 +353,12 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                             else tma_load_3d(dst, k_map, full_bar(s), kb * BK, at, matrix);
                         }
                     };
-                    load(base + s * STAGE, a_is_mn(t, kb), ak, an, a0, am);
-                    load(base + s * STAGE + A2_BYTES, b_is_mn(t, kb), bk, bn, b0, bm);
+                    load(base + s * STAGE, a_is_mn(h, t, kb), ak, an, a0, am);
+                    load(base + s * STAGE + A2_BYTES, b_is_mn(h, t, kb), bk, bn, b0, bm);
                     if (++s == NST) { s = 0; ph ^= 1u; }
                 }
             }
-            // gave up: copies in flight have landed long before a millisecond is over, and only then may the CTA exit
-            if (!ok)
-                for (const unsigned long long t0 = global_ns(); global_ns() - t0 < 1000000ull;) {}
+            if (!ok) gave_up();
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (one thread, even CTA only)
@@ -293,16 +369,17 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, false, true, 0};
             NsTile t;
             while (ok && tiles.next(t)) {
+                const NsShape &h = p.s[t.shape];
                 ok = mbar_wait(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * ACC;
-                const int kblocks = kblocks_of(t), width = width_of(t);
+                const int kblocks = kblocks_of(h, t), width = width_of(h, t);
                 for (int kb = 0; kb < kblocks; ++kb) {
+                    const bool a_mn = a_is_mn(h, t, kb), b_mn = b_is_mn(h, t, kb);
                     ok = mbar_wait(full_bar(s), ph, abort_flag, p.status);
                     if (!ok) break;
                     tc_fence_after();
-                    const bool a_mn = a_is_mn(t, kb), b_mn = b_is_mn(t, kb);
                     const uint32_t a_src = base + s * STAGE, b_src = a_src + A2_BYTES, idesc = idesc_of(PAIR, a_mn, b_mn, width);
                     const uint64_t ad = a_mn ? desc_mnmajor(a_src) : desc_kmajor(a_src), bd = b_mn ? desc_mnmajor(b_src) : desc_kmajor(b_src);
                     const uint64_t a_step = a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = b_mn ? (16 * 128) >> 4 : 32 >> 4;
@@ -325,6 +402,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
         // ------------------------------------------------------------------ drawing tiles (even CTA, one thread)
         if (rank == 0 && lane == 0) {
             const uint32_t peer_ring = PAIR ? peer_smem_addr(ring, 1) : 0u, peer_full0 = PAIR ? peer_smem_addr(ring_full0, 1) : 0u;
+            NsOrder<PAIR> order(p);
             for (int i = 0;; ++i) {
                 const uint32_t slot = (uint32_t)i % RING;
                 if (i >= RING) {  // every reader of the record this slot held has its copy
@@ -332,7 +410,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                     if (!mbar_wait(ring_empty0 + 8u * slot, par, abort_flag, p.status)) break;
                     if (PAIR) mbar_try_wait_cluster(ring_empty0 + 8u * slot, par);
                 }
-                const int4 a = find_ns_tile<PAIR>(p, atomicAdd(p.next, 1));
+                const int4 a = order.find(atomicAdd(p.next, 1));
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ring + 16u * slot), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
                 if (PAIR) st_cluster_v4(peer_ring + 16u * slot, a);
                 mbar_arrive(ring_full0 + 8u * slot);
@@ -340,40 +418,86 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                 if (a.x < 0) break;
             }
         }
+    } else if (warp == 11) {
+        // ------------------------------------------------------------------ storing results (both CTAs, one thread)
+        if (lane == 0) {
+            uint32_t ph = 0;
+            bool ok = true;
+            NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, false, true, 0};
+            NsTile t;
+            while (ok && tiles.next(t)) {
+                const NsShape &h = p.s[t.shape];
+                const NsMaps &maps = all_maps.m[t.shape];
+                const bool last = t.product == THIRD && t.step + 1 == p.steps;
+                const int to = (t.step & 1) ^ 1;  // of X
+                const CUtensorMap *out = t.product == FIRST ? &maps.a_box : t.product == SECOND ? &maps.b_box : &maps.x_box[to];
+                const int matrix = t.product == THIRD && !to ? t.matrix : t.matrix % h.slots;
+                for (int u = 0; u < 2 && ok; ++u) {
+                    ok = mbar_wait(box_ready0 + 8u * u, ph, abort_flag, p.status);
+                    if (!ok) break;
+                    if (last) continue;
+                    for (int w = 0; w < 8; ++w) {
+                        int32_t row0, first;
+                        if (u < boxes_of(h, t, w, row0, first)) store_box_3d(out, base + NST * STAGE + (w * 2 + u) * BOX, first + 64 * u, row0, matrix);
+                    }
+                    tma_store_commit();
+                }
+                if (!ok) break;
+                ph ^= 1u;
+                tma_store_wait_read_but_one();
+                mbar_arrive(box_empty0);
+                tma_store_wait_read();
+                mbar_arrive(box_empty0 + 8u);
+                tma_store_wait_all();
+                fence_async();
+                asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + h.first + t.matrix) : "memory");
+            }
+            tma_store_wait_all();  // no bulk store may outlive the CTA's shared memory
+        }
     } else {
-        // ------------------------------------------------------------------ epilogue (warps 2..9, both CTAs)
+        // ------------------------------------------------------------------ results (warps 2..9, both CTAs)
         // Two warps share each quarter of the accumulator's rows and take half of its columns each, in boxes of 64.
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        uint8_t *boxes_at = smem + NST * STAGE + (warp - 2) * 2 * BOX;
-        const uint32_t box_bar = box_bar0 + 16u * (warp - 2);
+        const int w = warp - 2, quarter = warp & 3, half = w >> 2;
+        uint8_t *boxes_at = smem + NST * STAGE + w * 2 * BOX;
+        float *factors = reinterpret_cast<float *>(smem + NS_DATA + 512 + w * 128);
         const float lr = p.rates ? p.rates->lr : p.lr;
         int acc = 0;
-        uint32_t acc_ph = 0, box_ph[2] = {0, 0};
+        uint32_t acc_ph = 0, box_ph = 0;
         NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, true, lane == 0, 0};
         NsTile t;
         bool ok = true;
         while (ok && tiles.next(t)) {
-            const int32_t row0 = t.row + 128 * (int)rank + 32 * quarter, first = t.col + half * (width_of(t) / 2), row = row0 + lane;
-            const int32_t rows_out = t.product == THIRD ? p.rows : p.M;
+            const NsShape &h = p.s[t.shape];
+            int32_t row0, first;
+            const int boxes = boxes_of(h, t, w, row0, first);
+            const int32_t row = row0 + lane;
+            const int slot = t.matrix % h.slots, x = t.step & 1;
             const bool last = t.product == THIRD && t.step + 1 == p.steps;
-            const int boxes = row0 < rows_out ? max(0, min(width_of(t) / 128, (cols_out(t) - first) / 64)) : 0;
-            const int slot = t.matrix % p.slots, x = t.step & 1;
-            // What the result is added to, box by box, is on its way while the products run: A' or X as it was
+            float *d = h.d + (int64_t)slot * h.M, *r = h.r + (int64_t)slot * h.M;
+            // What the result is added to, box by box, is on its way while the products run: A' or X as it was, and the diagonals' elements of this lane's row and of its columns
+            const __half *from = t.product == SECOND ? h.a + ((int64_t)slot * h.M + row) * h.Mld + first : h.x[x] + ((int64_t)(x ? slot : t.matrix) * h.rows + row) * h.ld + first;
+            const bool in = t.product != FIRST && row < (t.product == SECOND ? h.M : h.rows);
+            const float *of_cols = t.product == SECOND ? d : t.product == THIRD && !h.left ? r : nullptr;
+            uint32_t old[2][32];
+            float of_row = 0.0f, of_col[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             if (t.product != FIRST) {
-                ok = wait_count(p.done + t.matrix, wanted<PAIR>(p, t), abort_flag, p.status);  // (the copying thread has seen it, and this one has to)
-                if (ok && lane == 0) {
-                    fence_async();
-                    for (int u = 0; u < boxes; ++u) {
-                        mbar_expect_tx(box_bar + 8u * u, BOX);
-                        tma_load_3d(smem_u32(boxes_at + u * BOX), t.product == SECOND ? &maps.a_box : &maps.x_box[x], box_bar + 8u * u, first + 64 * u, row0,
-                                    t.product == THIRD && !x ? t.matrix : slot);
+                ok = wait_count(p.done + h.first + t.matrix, wanted<PAIR>(h, t), abort_flag, p.status);  // (the copying thread has seen it, and this one has to)
+                if (ok) {
+                    if (row < h.M && (t.product == SECOND || h.left)) of_row = __ldcg((t.product == SECOND ? d : r) + row);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        load_old(from + 64 * u, in && u < boxes, old[u]);
+                        if (of_cols && u < boxes)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+                                if (first + 64 * u + 32 * j + lane < h.M) of_col[2 * u + j] = __ldcg(of_cols + first + 64 * u + 32 * j + lane);
                     }
                 }
             }
             ok = __all_sync(0xffffffffu, ok && mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.status));
             if (!ok) break;
             tc_fence_after();
-            const uint32_t mine = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * ACC + half * (width_of(t) / 2);
+            const uint32_t mine = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * ACC + half * (width_of(h, t) / 2);
             auto release = [&]() {  // the warp's part of the accumulator is in registers: the buffer goes back
                 tc_fence_before();
                 __syncwarp();
@@ -382,111 +506,78 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                     else mbar_arrive(tempty_bar(acc));
                 }
             };
-            float *d = p.d + (int64_t)slot * p.M, *r = p.r + (int64_t)slot * p.M;
-            // of this lane's row: SECOND d_i, THIRD r_i (X has rows of B)
-            const float of_row = t.product == FIRST || row >= p.M || (t.product == THIRD && !p.left) ? 0.0f : __ldcg((t.product == SECOND ? d : r) + row);
-            const float *of_cols = t.product == SECOND ? d : t.product == THIRD && !p.left ? r : nullptr;
-#pragma unroll 1
-            for (int u = 0; u < boxes; ++u) {
-                const int32_t col = first + 64 * u;
-                uint8_t *box = boxes_at + u * BOX;
-                uint32_t v[2][32];
-                tc_ld_32x32(mine + 64 * u, v[0]);
-                tc_ld_32x32(mine + 64 * u + 32, v[1]);
-                if (t.product != FIRST) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(box_bar + 8u * u, box_ph[u], abort_flag, p.status));
-                    box_ph[u] ^= 1u;
-                }
-                tc_ld_wait();
-                if (u + 1 == boxes) release();
-                if (!ok) break;
-                const bool diagonal = t.product != THIRD && row >= col && row < col + 64 && row < p.M;
-                const float by = last ? 1.0f / (MUON_UNIT * MUON_UNIT) : 1.0f / MUON_UNIT;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    uint4 *place = reinterpret_cast<uint4 *>(box + lane * 128 + ((q ^ (lane & 7)) << 4));
-                    uint4 old = make_uint4(0u, 0u, 0u, 0u);
-                    if (t.product != FIRST) old = *place;
-                    float cs[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) cs[j] = of_row;
-                    if (of_cols)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) cs[j] += col + 8 * q + j < p.M ? __ldcg(of_cols + col + 8 * q + j) : 0.0f;
-                    if (t.product == SECOND)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) cs[j] = fmaf(NS_C, cs[j], NS_B);
-                    const uint32_t *raw = reinterpret_cast<const uint32_t *>(&old);
-                    uint32_t packed[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int at = 8 * q + 2 * j;
-                        float2 y = make_float2(__uint_as_float(v[at >> 5][at & 31]), __uint_as_float(v[at >> 5][(at & 31) + 1]));
-                        if (diagonal && (at == row - col || at + 1 == row - col)) {  // kept in float; no part of the operand
-                            float &own = at == row - col ? y.x : y.y;
-                            const float sum = own * (1.0f / (MUON_UNIT * MUON_UNIT));
-                            if (t.product == FIRST) d[row] = sum;
-                            else r[row] = fmaf(NS_C, fmaf(of_row, of_row, sum), fmaf(NS_B, of_row, NS_A));
-                            own = 0.0f;  // (and A' has a zero here)
-                        }
-                        const float2 o = __half22float2(*reinterpret_cast<const __half2 *>(&raw[j]));
-                        const float unit = t.product == SECOND ? NS_C / MUON_UNIT : by, scale = last ? 1.0f / MUON_UNIT : 1.0f;
-                        y.x = fmaf(y.x, unit, o.x * (cs[2 * j] * scale));
-                        y.y = fmaf(y.y, unit, o.y * (cs[2 * j + 1] * scale));
-                        if (last) {
-                            v[at >> 5][at & 31] = __float_as_uint(y.x);
-                            v[at >> 5][(at & 31) + 1] = __float_as_uint(y.y);
-                        } else {
-                            const __half2 h = __floats2half2_rn(y.x, y.y);
-                            packed[j] = *reinterpret_cast<const uint32_t *>(&h);
-                        }
-                    }
-                    if (!last) *place = make_uint4(packed[0], packed[1], packed[2], packed[3]);
-                }
-                if (last) {
-                    const int32_t i = batch.entry_of(t.matrix);
-                    const MuonEntry &e = batch.t[i];
-                    const int64_t in_entry = (int64_t)(t.matrix - batch.first[i]) * p.rows * p.cols;
+            for (int u = 0; u < 2; ++u) {
+                // The last tile's box has been stored: what a warp without one waits for too, whose report below would else count for that tile's
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(box_empty0 + 8u * u, box_ph ^ 1u, abort_flag, p.status));
+                if (ok && u < boxes) {
+                    const int32_t col = first + 64 * u;
+                    uint8_t *box = boxes_at + u * BOX;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        if (col + 32 * j >= p.cols) break;
-                        __syncwarp();
-                        float *floats = reinterpret_cast<float *>(box);
+                        uint32_t raw[32];
+                        tc_ld_32x32(mine + 64 * u + 32 * j, raw);
+                        tc_ld_wait();
+                        if (u + 1 == boxes && j == 1) release();
+                        float2 v[16];
 #pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            *reinterpret_cast<uint4 *>(floats + lane * 32 + ((q ^ (lane & 7)) << 2)) = make_uint4(v[j][4 * q], v[j][4 * q + 1], v[j][4 * q + 2], v[j][4 * q + 3]);
-                        __syncwarp();
-                        const int64_t at = in_entry + (int64_t)row0 * p.cols + col + 32 * j;
-                        const int32_t rl = p.rows - row0, cl = p.cols - col - 32 * j;
-                        const bool vectors = p.cols % 4 == 0;
-                        if (e.kind & 8) vectors ? step_box<true, true, true>(p, e, at, rl, cl, floats, lane, lr) : step_box<true, true, false>(p, e, at, rl, cl, floats, lane, lr);
-                        else if (e.kind & 1) vectors ? step_box<true, false, true>(p, e, at, rl, cl, floats, lane, lr) : step_box<true, false, false>(p, e, at, rl, cl, floats, lane, lr);
-                        else vectors ? step_box<false, false, true>(p, e, at, rl, cl, floats, lane, lr) : step_box<false, false, false>(p, e, at, rl, cl, floats, lane, lr);
+                        for (int i = 0; i < 16; ++i) v[i] = make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
+                        if (of_cols) {
+                            __syncwarp();
+                            factors[lane] = of_col[2 * u + j];
+                            __syncwarp();
+                        }
+                        if (t.product != THIRD && col + 32 * j == row0) {  // the diagonal: kept in float; no part of the operand (and A' has a zero here)
+                            float own = 0.0f;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                float &e = i & 1 ? v[i / 2].y : v[i / 2].x;
+                                if (i == lane) { own = e; e = 0.0f; }
+                            }
+                            own *= 1.0f / (MUON_UNIT * MUON_UNIT);
+                            if (row < h.M) (t.product == FIRST ? d : r)[row] = t.product == FIRST ? own : fmaf(NS_C, fmaf(of_row, of_row, own), fmaf(NS_B, of_row, NS_A));
+                        }
+                        if (t.product == FIRST) finish<K_FIRST, false>(v, old[u] + 16 * j, 0.0f, factors);
+                        else if (t.product == SECOND) finish<K_SECOND, true>(v, old[u] + 16 * j, of_row, factors);
+                        else if (!last) of_cols ? finish<K_THIRD, true>(v, old[u] + 16 * j, of_row, factors) : finish<K_THIRD, false>(v, old[u] + 16 * j, of_row, factors);
+                        else of_cols ? finish<K_LAST, true>(v, old[u] + 16 * j, of_row, factors) : finish<K_LAST, false>(v, old[u] + 16 * j, of_row, factors);
+                        if (!last) {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                uint32_t packed[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const __half2 two = __floats2half2_rn(v[4 * q + i].x, v[4 * q + i].y);
+                                    packed[i] = *reinterpret_cast<const uint32_t *>(&two);
+                                }
+                                *reinterpret_cast<uint4 *>(box + lane * 128 + (((4 * j + q) ^ (lane & 7)) << 4)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+                            }
+                        } else if (col + 32 * j < h.cols) {  // onto the weights
+                            const int32_t matrix = h.first + t.matrix, i = batch.entry_of(matrix);
+                            const MuonEntry &e = batch.t[i];
+                            __syncwarp();
+                            float *floats = reinterpret_cast<float *>(box);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                *reinterpret_cast<float4 *>(floats + lane * 32 + ((q ^ (lane & 7)) << 2)) = make_float4(v[2 * q].x, v[2 * q].y, v[2 * q + 1].x, v[2 * q + 1].y);
+                            __syncwarp();
+                            const int64_t at = ((int64_t)(matrix - batch.before[i]) * h.rows + row0) * h.cols + col + 32 * j;
+                            const int32_t rl = h.rows - row0, cl = h.cols - col - 32 * j;
+                            const bool vectors = h.cols % 4 == 0;
+                            if (e.kind & 8) vectors ? step_box<true, true, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<true, true, false>(h.cols, e, at, rl, cl, floats, lane, lr);
+                            else if (e.kind & 1) vectors ? step_box<true, false, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<true, false, false>(h.cols, e, at, rl, cl, floats, lane, lr);
+                            else vectors ? step_box<false, false, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<false, false, false>(h.cols, e, at, rl, cl, floats, lane, lr);
+                        }
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the box is copied into again
-                    continue;
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
-                    const CUtensorMap *out = t.product == FIRST ? &maps.a_box : t.product == SECOND ? &maps.b_box : &maps.x_box[x ^ 1];
-                    store_box_3d(out, smem_u32(box), col, row0, t.product == THIRD && x ? t.matrix : slot);
-                    tma_store_commit();
-                }
+                if (lane == 0) mbar_arrive(box_ready0 + 8u * u);
             }
             if (boxes == 0) release();
+            box_ph ^= 1u;
             if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
-            __syncwarp();
-            if (lane == 0) {
-                tma_store_wait_all();
-                fence_async();
-                asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + t.matrix) : "memory");
-            }
-            __syncwarp();
         }
-        if (!ok)  // gave up, see above
-            for (const unsigned long long t0 = global_ns(); global_ns() - t0 < 1000000ull;) {}
-        if (lane == 0) tma_store_wait_all();  // no bulk store may outlive the CTA's shared memory
     }
 
     tc_fence_before();
@@ -500,38 +591,43 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
 }
 
 // ------------------------------------------------------------------------------------------ host
-struct NsPlan {
-    bool pair;
-    int32_t square, rows3, cols3;
-    int64_t M, Mld, ld, group, slots;
-};
-NsPlan plan_of(int32_t rows, int32_t cols, int64_t matrices) {
-    NsPlan q;
-    q.M = imin(rows, cols);
-    q.Mld = muon_ld(q.M);
-    q.ld = muon_ld(cols);
-    q.pair = q.M > 128;
-    const int side = q.pair ? 256 : 128;
-    const int64_t s = cdiv(q.M, side);
-    q.square = (int32_t)(s * (s + 1) / 2);
-    q.rows3 = (int32_t)cdiv(rows, side);
-    q.cols3 = (int32_t)cdiv(cols, side);
-    // as many matrices as give every SM pair (SM) more than one tile of A
-    q.group = imin(matrices, cdiv(5 * (q.pair ? 74 : 148), 4 * (int64_t)q.square));
-    q.slots = imin(matrices, 2 * q.group);
-    return q;
+constexpr int64_t GROUP_TILES = 96;  // of A in a group, on SM pairs (74): more than one for each; twice as many on single SMs
+void tiles_of(int32_t rows, int32_t cols, bool pair, NsShape *s) {
+    const int side = pair ? 256 : 128;
+    const int64_t edge = cdiv(imin(rows, cols), side);
+    s->square = (int32_t)(edge * (edge + 1) / 2);
+    s->cols3 = (int32_t)cdiv(cols, side);
+    s->tiles3 = (int32_t)cdiv(rows, side) * s->cols3;
 }
-struct NsScratch { __half *x, *a, *b; float *d, *r; };
-NsScratch ns_scratch(Carver &cv, const NsPlan &q, int64_t rows) {
-    NsScratch s;
-    s.x = cv.take<__half>(q.slots * rows * q.ld);
-    s.a = cv.take<__half>(q.slots * q.M * q.Mld);
-    s.b = cv.take<__half>(q.slots * q.M * q.Mld);
-    s.d = cv.take<float>(q.slots * q.M);
-    s.r = cv.take<float>(q.slots * q.M);
+int64_t groups_of(const MuonBatch &b, bool pair) {
+    int64_t square = 0;
+    for (int i = 0; i < b.shapes; ++i) {
+        NsShape s;
+        tiles_of(b.s[i].rows, b.s[i].cols, pair, &s);
+        square += (int64_t)s.square * b.s[i].matrices;
+    }
+    return imax(1, square / (pair ? GROUP_TILES : 2 * GROUP_TILES));
+}
+struct NsScratch { __half *x, *a, *b; };
+// Everything about a shape but its place in memory, and with scratch that too
+NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, Carver &cv, NsScratch *at) {
+    NsShape s = {};
+    tiles_of(m.rows, m.cols, pair, &s);
+    s.rows = m.rows; s.cols = m.cols; s.ld = m.ld;
+    s.M = (int32_t)imin(m.rows, m.cols);
+    s.Mld = (int32_t)muon_ld(s.M);
+    s.first = m.first; s.matrices = m.matrices; s.left = m.rows <= m.cols;
+    s.group = (int32_t)cdiv(m.matrices, groups);
+    s.slots = (int32_t)imin(m.matrices, 2 * (int64_t)s.group);  // a group's begin while the last one's end
+    at->x = cv.take<__half>((int64_t)s.slots * s.rows * s.ld);
+    at->a = cv.take<__half>((int64_t)s.slots * s.M * s.Mld);
+    at->b = cv.take<__half>((int64_t)s.slots * s.M * s.Mld);
+    s.d = cv.take<float>((int64_t)s.slots * s.M);
+    s.r = cv.take<float>((int64_t)s.slots * s.M);
+    s.x[0] = m.x; s.x[1] = at->x; s.a = at->a;
     return s;
 }
-// [count][rows][ld] halves: boxes of 64 columns x 128 rows, of 64 rows x two pieces of 64 columns, and the epilogue's of 64 columns x 32 rows
+// [count][rows][ld] halves: boxes of 64 columns x 128 rows, of 64 rows x two pieces of 64 columns, and for stores of 64 columns x 32 rows
 int32_t maps_of(const __half *at, int64_t count, int64_t rows, int64_t ld, CUtensorMap *k, CUtensorMap *mn, CUtensorMap *box32) {
     const uint64_t dims[3] = {(uint64_t)ld, (uint64_t)rows, (uint64_t)count}, str[2] = {(uint64_t)ld * 2, (uint64_t)(rows * ld) * 2};
     const uint32_t box[3] = {64, 128, 1}, box_out[3] = {64, 32, 1};
@@ -542,7 +638,7 @@ int32_t maps_of(const __half *at, int64_t count, int64_t rows, int64_t ld, CUten
     return tc_make_map(mn, at, 4, dims4, str4, box4);
 }
 
-template <bool PAIR> int32_t launch_ns(const NsMaps &maps, const NsArgs &p, const MuonBatch &batch, cudaStream_t st) {
+template <bool PAIR> int32_t launch_ns(const NsAllMaps &maps, const NsArgs &p, const MuonBatch &batch, int64_t total, cudaStream_t st) {
     static PerDevice most;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
@@ -562,7 +658,7 @@ template <bool PAIR> int32_t launch_ns(const NsMaps &maps, const NsArgs &p, cons
         return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
     });
     if (workers <= 0) return MOE_ERR_CUDA;
-    cfg.gridDim = dim3((PAIR ? 2 : 1) * (unsigned)imin(p.total, workers));
+    cfg.gridDim = dim3((PAIR ? 2 : 1) * (unsigned)imin(total, workers));
     MOE_CUDA(cudaLaunchKernelEx(&cfg, kernel, maps, p, batch));
     MOE_LAUNCHED();
     return MOE_OK;
@@ -570,32 +666,43 @@ template <bool PAIR> int32_t launch_ns(const NsMaps &maps, const NsArgs &p, cons
 
 }  // namespace
 
-int64_t ns_scratch_bytes(int32_t rows, int32_t cols, int64_t matrices) {
+int64_t ns_tiles(int32_t rows, int32_t cols, bool pair) {
+    NsShape s;
+    tiles_of(rows, cols, pair, &s);
+    return 2 * (int64_t)s.square + s.tiles3;
+}
+
+int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair) {
     Carver cv(nullptr);
-    ns_scratch(cv, plan_of(rows, cols, matrices), rows);
+    const int64_t groups = groups_of(batch, pair);
+    NsScratch at;
+    for (int i = 0; i < batch.shapes; ++i) shape_of(batch.s[i], pair, groups, cv, &at);
     return (int64_t)cv.off;
 }
 
 int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st) {
-    const int32_t rows = w.batch->rows, cols = w.batch->cols;
-    const NsPlan q = plan_of(rows, cols, w.matrices);
+    const MuonBatch &b = *w.batch;
     Carver cv(w.scratch);
-    const NsScratch s = ns_scratch(cv, q, rows);
-    NsMaps maps;
-    MOE_TRY(maps_of(w.x, w.matrices, rows, q.ld, &maps.x_k[0], &maps.x_mn[0], &maps.x_box[0]));
-    MOE_TRY(maps_of(s.x, q.slots, rows, q.ld, &maps.x_k[1], &maps.x_mn[1], &maps.x_box[1]));
-    MOE_TRY(maps_of(s.a, q.slots, q.M, q.Mld, &maps.a_k, &maps.a_mn, &maps.a_box));
-    MOE_TRY(maps_of(s.b, q.slots, q.M, q.Mld, &maps.b_k, &maps.b_mn, &maps.b_box));
+    const int64_t groups = groups_of(b, w.pair);
+    NsAllMaps maps;
     NsArgs p = {};
-    p.rows = rows; p.cols = cols; p.ld = (int32_t)q.ld; p.M = (int32_t)q.M; p.Mld = (int32_t)q.Mld;
-    p.matrices = w.matrices; p.steps = w.steps; p.left = rows <= cols;
-    p.square = q.square; p.cols3 = q.cols3; p.tiles3 = q.rows3 * q.cols3;
-    p.group = (int32_t)q.group; p.slots = (int32_t)q.slots;
-    const int64_t total = (int64_t)w.matrices * w.steps * (2 * (int64_t)p.square + p.tiles3);
+    int64_t total = 0;
+    p.shapes = b.shapes; p.steps = w.steps;
+    for (int i = 0; i < b.shapes; ++i) {
+        NsScratch at;
+        NsShape &s = p.s[i];
+        NsMaps &m = maps.m[i];
+        s = shape_of(b.s[i], w.pair, groups, cv, &at);
+        MOE_TRY(maps_of(b.s[i].x, s.matrices, s.rows, s.ld, &m.x_k[0], &m.x_mn[0], &m.x_box[0]));
+        MOE_TRY(maps_of(at.x, s.slots, s.rows, s.ld, &m.x_k[1], &m.x_mn[1], &m.x_box[1]));
+        MOE_TRY(maps_of(at.a, s.slots, s.M, s.Mld, &m.a_k, &m.a_mn, &m.a_box));
+        MOE_TRY(maps_of(at.b, s.slots, s.M, s.Mld, &m.b_k, &m.b_mn, &m.b_box));
+        total += (int64_t)s.matrices * w.steps * (2 * (int64_t)s.square + s.tiles3);
+        p.groups = (int32_t)imax(p.groups, cdiv(s.matrices, s.group));
+    }
     if (total > (int64_t)1 << 30) return MOE_ERR_UNSUPPORTED;
-    p.total = (int32_t)total;
-    p.done = w.done; p.next = w.next; p.status = w.status; p.d = s.d; p.r = s.r; p.lr = w.lr; p.rates = w.rates;
-    return q.pair ? launch_ns<true>(maps, p, *w.batch, st) : launch_ns<false>(maps, p, *w.batch, st);
+    p.done = w.done; p.next = w.next; p.status = w.status; p.lr = w.lr; p.rates = w.rates;
+    return w.pair ? launch_ns<true>(maps, p, b, total, st) : launch_ns<false>(maps, p, b, total, st);
 }
 
 }  // namespace moe
