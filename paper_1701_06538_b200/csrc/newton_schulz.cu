@@ -22,6 +22,8 @@
 // (2 s); on expiry the CTA records MOE_ERR_TIMEOUT in the workspace's status word and drains.
 #include <string.h>
 
+#include <type_traits>
+
 #include "muon.cuh"
 #include "pairs.cuh"
 #include "tc.cuh"
@@ -31,14 +33,14 @@ namespace moe {
 namespace {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
-constexpr int RING = 2;                       // tiles drawn ahead
+constexpr int RING = 3;                       // tiles drawn ahead
 constexpr int NS_THREADS = 384;
 constexpr int NS_STAGES = 5;
 constexpr uint32_t BOX = 4096;                // a warp's 32 rows of 64 columns
 constexpr int NS_DATA = NS_STAGES * STAGE2_BYTES + 2 * 8 * BOX, NS_SMEM = NS_DATA + 1024 /*alignment*/ + 512 /*barriers, ring*/ + 8 * 128 /*factors*/;
 
 enum { FIRST = 0, SECOND = 1, THIRD = 2 };    // A, B, X
-struct NsMaps { CUtensorMap x_k[2], x_mn[2], x_box[2], a_k, a_mn, a_box, b_k, b_mn, b_box; };  // x[0]: all matrices, the others: a ring of slots
+struct NsMaps { CUtensorMap x_k[2], x_mn[2], a_k, a_mn, b_k, b_mn; };  // x[0]: all matrices, the others: a ring of slots
 struct NsShape {
     int32_t rows, cols, ld, M, Mld, first, matrices, left;
     int32_t square, cols3, tiles3;            // tiles of A and B (lower half), tiles of X beside each other, of X
@@ -54,12 +56,12 @@ struct NsArgs {
     const moe_muon_rates *rates;
 };
 struct NsAllMaps { NsMaps m[MUON_MAX_SHAPES]; };
-struct NsTile { int32_t matrix, shape, step, product, row, col; };
+struct NsTile { int32_t matrix, shape, step, product, row, col, slot; };
 
 template <bool PAIR> constexpr int tile_side() { return PAIR ? 256 : 128; }
 template <bool PAIR> constexpr int arrivals() { return PAIR ? 2 : 1; }  // of a stored tile: CTAs
 
-// The tiles in their order: {matrix or -1, shape << 16 | step << 2 | product, row, column} of ascending numbers
+// The tiles in their order: {matrix or -1, shape << 16 | step << 2 | product, tile's row << 16 | column, slot} of ascending numbers
 template <bool PAIR> struct NsOrder {
     const NsArgs &p;
     int32_t group, base, each;  // the group that is at, its first number, its tiles a step
@@ -93,7 +95,8 @@ template <bool PAIR> struct NsOrder {
                     for (row = 0; t > row; ++row) t -= row + 1;
                     col = t;
                 }
-                return make_int4(group * p.s[s].group + m, s << 16 | step << 2 | product, row * tile_side<PAIR>(), col * tile_side<PAIR>());
+                const int32_t matrix = group * p.s[s].group + m;
+                return make_int4(matrix, s << 16 | step << 2 | product, row << 16 | col, matrix % p.s[s].slots);
             }
     }
 };
@@ -101,10 +104,6 @@ __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
     int32_t v;
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
-}
-// Arrivals that a matrix has when everything before this product is stored
-template <bool PAIR> __device__ __forceinline__ int32_t wanted(const NsShape &s, const NsTile &t) {
-    return arrivals<PAIR>() * (t.step * (2 * s.square + s.tiles3) + t.product * s.square);
 }
 __device__ __forceinline__ bool wait_count(const int32_t *count, int32_t at_least, volatile int *abort_flag, int32_t *status) {
     if (load_acquire(count) >= at_least) return true;
@@ -152,7 +151,8 @@ template <bool PAIR> struct NsRing {
             else mbar_arrive(empty);
         }
         ++i;
-        t.matrix = a.x; t.shape = a.y >> 16; t.step = a.y >> 2 & 0x3fff; t.product = a.y & 3; t.row = a.z; t.col = a.w;
+        t.matrix = a.x; t.shape = a.y >> 16; t.step = a.y >> 2 & 0x3fff; t.product = a.y & 3;
+        t.row = (a.z >> 16) * tile_side<PAIR>(); t.col = (a.z & 0xffff) * tile_side<PAIR>(); t.slot = a.w;
         return a.x >= 0;
     }
 };
@@ -241,18 +241,174 @@ __device__ __forceinline__ void finish(float2 (&v)[16], const uint32_t *old, flo
         }
     }
 }
-// 64 halves of a row: what another SM's copies have stored
-__device__ __forceinline__ void load_old(const __half *from, bool in, uint32_t (&old)[32]) {
+// 32 bytes at a time (a whole sector), of what another SM may have written in the meantime
+__device__ __forceinline__ void load_32B(const void *from, uint32_t *r) {
+    asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(from) : "memory");
+}
+__device__ __forceinline__ void store_32B(void *to, const uint32_t *r) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+// A row's 32 weights, a row a lane, where rows begin at 32 bytes: read while the products run
+struct RowOfWeights {
+    float *floats;   // what the step is taken on: float weights or masters, or nullptr
+    bf16 *halves;    // bf16 weights, or nullptr
+    float scale, decay;
+    uint32_t raw[32];
+    __device__ __forceinline__ void load(int32_t at, bool in) {
+        if (!in) return;
+        if (floats)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        uint32_t *r = old + 8 * q;
-        if (in)
-            asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(from + 16 * q) : "memory");
+            for (int q = 0; q < 4; ++q) load_32B(floats + at + 8 * q, raw + 8 * q);
         else
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = 0u;
+            for (int q = 0; q < 2; ++q) load_32B(halves + at + 16 * q, raw + 8 * q);
     }
+    __device__ __forceinline__ void step(float2 (&x)[16], float lr) const {  // x: the new weights
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 w = floats ? make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1])) : make_float2(__uint_as_float(raw[i] << 16), __uint_as_float(raw[i] & 0xffff0000u));
+            x[i] = fma2(both(-lr), fma2(x[i], both(scale), mul2(w, both(decay))), w);
+        }
+    }
+    __device__ __forceinline__ void store(int32_t at, const float2 (&x)[16]) const {
+        if (floats)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t u[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { u[2 * i] = __float_as_uint(x[4 * q + i].x); u[2 * i + 1] = __float_as_uint(x[4 * q + i].y); }
+                store_32B(floats + at + 8 * q, u);
+            }
+        if (halves)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                uint32_t u[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const __nv_bfloat162 two = __floats2bfloat162_rn(x[8 * q + i].x, x[8 * q + i].y);
+                    u[i] = *reinterpret_cast<const uint32_t *>(&two);
+                }
+                store_32B(halves + at + 16 * q, u);
+            }
+    }
+};
+
+// A warp's part of a tile, box by box (at most two): accumulators -> results -> shared memory, or the weights. What is added comes from `from` (this lane's row from the tile's first column
+// of the warp on), a box ahead; of_cols: the diagonal's elements of the columns. Each kind has its own code: with all of them in one loop instructions were fetched again and again.
+struct BoxWork {
+    uint32_t accumulator;   // in tensor memory
+    uint8_t *boxes;
+    float *factors;
+    const __half *from;
+    const float *of_cols;
+    float *diagonal;        // K_FIRST: d, K_SECOND: r
+    float of_row;
+    int32_t row0, first, boxes_n, M;
+    bool in;                // this lane's row exists
+    uint32_t box_empty0, box_ready0, box_parity;
+    volatile int *abort_flag;
+    int32_t *status;
+};
+// The operand's 32 halves of this lane's row, and the diagonal's element of a column a lane, from a box' first column on
+template <int KIND, bool COLS> __device__ __forceinline__ void fetch_half(const BoxWork &b, int32_t at, int lane, uint32_t (&old)[16], float &of_col) {
+    if constexpr (KIND != K_FIRST)
+        if (b.in) {
+            load_32B(b.from + at, old);
+            load_32B(b.from + at + 16, old + 8);
+        }
+    if constexpr (COLS)
+        if (b.first + at + lane < b.M) of_col = __ldcg(b.of_cols + b.first + at + lane);
+}
+// Half a box, 32 columns. The next box' half of the operand is asked for as soon as this one's is used up
+template <int KIND, bool COLS, bool ROWS, int J, typename Last>
+__device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, float lr, const uint32_t (&raw)[32], uint32_t (&old)[16], float &of_col, RowOfWeights &weights, int32_t weights_end,
+                                          Last onto_weights) {
+    const int32_t col = b.first + 64 * u + 32 * J;
+    uint8_t *box = b.boxes + u * 4 * BOX;
+    if constexpr (COLS) {
+        __syncwarp();
+        b.factors[lane] = of_col;
+        __syncwarp();
+    }
+    float2 v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
+    if (KIND <= K_SECOND && col == b.row0) {  // the diagonal: kept in float; no part of the operand (and A' has a zero here)
+        float own = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            float &e = i & 1 ? v[i / 2].y : v[i / 2].x;
+            if (i == lane) { own = e; e = 0.0f; }
+        }
+        own *= 1.0f / (MUON_UNIT * MUON_UNIT);
+        if (b.row0 + lane < b.M) b.diagonal[b.row0 + lane] = KIND == K_FIRST ? own : fmaf(NS_C, fmaf(b.of_row, b.of_row, own), fmaf(NS_B, b.of_row, NS_A));
+    }
+    finish<KIND, COLS>(v, old, b.of_row, b.factors);
+    if (u + 1 < b.boxes_n) fetch_half<KIND, COLS>(b, 64 + 32 * J, lane, old, of_col);
+    if constexpr (KIND != K_LAST) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t packed[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __half2 two = __floats2half2_rn(v[4 * q + i].x, v[4 * q + i].y);
+                packed[i] = *reinterpret_cast<const uint32_t *>(&two);
+            }
+            *reinterpret_cast<uint4 *>(box + lane * 128 + (((4 * J + q) ^ (lane & 7)) << 4)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+        }
+    } else if constexpr (ROWS) {
+        const bool live = b.in && col < weights_end;
+        if (live) weights.step(v, lr);
+        weights.load(col + 32, (J == 0 || u + 1 < b.boxes_n) && b.in && col + 32 < weights_end);
+        if (live) weights.store(col, v);
+    } else {
+        __syncwarp();
+        float *floats = reinterpret_cast<float *>(box);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            *reinterpret_cast<float4 *>(floats + lane * 32 + ((q ^ (lane & 7)) << 2)) = make_float4(v[2 * q].x, v[2 * q].y, v[2 * q + 1].x, v[2 * q + 1].y);
+        __syncwarp();
+        onto_weights(col, floats);
+    }
+}
+// ROWS: the weights row by row (K_LAST), else by `onto_weights` through shared memory
+template <int KIND, bool COLS, bool ROWS, typename Wait, typename Release, typename Last>
+__device__ __forceinline__ bool make_boxes(const BoxWork &b, int lane, float lr, RowOfWeights &weights, int32_t weights_end, Wait wait_accumulator, Release release, Last onto_weights) {
+    uint32_t old0[16], old1[16];
+    float of_col0 = 0.0f, of_col1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) old0[i] = old1[i] = 0u;
+    if (b.boxes_n > 0) {  // (on their way while the products run)
+        fetch_half<KIND, COLS>(b, 0, lane, old0, of_col0);
+        fetch_half<KIND, COLS>(b, 32, lane, old1, of_col1);
+        if constexpr (ROWS) weights.load(b.first, b.in && b.first < weights_end);
+    }
+    bool ok = wait_accumulator();
+    if (ok && b.boxes_n == 0) release();
+#pragma unroll 1
+    for (int u = 0; u < 2; ++u) {
+        // The last tile's box has been stored: what a warp without one waits for too, whose report below would else count for that tile's
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(b.box_empty0 + 8u * u, b.box_parity, b.abort_flag, b.status));
+        if (ok && u < b.boxes_n) {
+            uint32_t raw0[32], raw1[32];
+            tc_ld_32x32(b.accumulator + 64 * u, raw0);
+            if constexpr (KIND != K_LAST) tc_ld_32x32(b.accumulator + 64 * u + 32, raw1);  // (beside the weights there are no registers for both)
+            tc_ld_wait();
+            if (KIND != K_LAST && u + 1 == b.boxes_n) release();
+            make_half<KIND, COLS, ROWS, 0>(b, u, lane, lr, raw0, old0, of_col0, weights, weights_end, onto_weights);
+            if constexpr (KIND == K_LAST) {
+                tc_ld_32x32(b.accumulator + 64 * u + 32, raw1);
+                tc_ld_wait();
+                if (u + 1 == b.boxes_n) release();
+            }
+            make_half<KIND, COLS, ROWS, 1>(b, u, lane, lr, raw1, old1, of_col1, weights, weights_end, onto_weights);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b.box_ready0 + 8u * u);
+    }
+    return ok;
 }
 
 template <bool PAIR>
@@ -327,13 +483,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             while (ok && tiles.next(t)) {
                 const NsShape &h = p.s[t.shape];
                 const NsMaps &maps = all_maps.m[t.shape];
-                const int32_t *count = p.done + h.first + t.matrix;
-                ok = wait_count(count, wanted<PAIR>(h, t), abort_flag, p.status);
-                if (ok && t.step == 0 && t.product == FIRST && t.matrix >= h.slots)  // the slot's last user has read what is overwritten now
-                    ok = wait_count(count - h.slots, arrivals<PAIR>() * p.steps * (2 * h.square + h.tiles3), abort_flag, p.status);
-                if (!ok) break;
-                fence_async();  // what other SMs' copies have stored, before this thread's copies read it
-                const int slot = t.matrix % h.slots, x = t.step & 1, xm = x ? slot : t.matrix;
+                const int slot = t.slot, x = t.step & 1, xm = x ? slot : t.matrix;
                 const bool a_x = t.product == FIRST || (t.product == THIRD && !h.left), b_x = t.product == FIRST || (t.product == THIRD && h.left);
                 const CUtensorMap *sym_k = t.product == SECOND ? &maps.a_k : &maps.b_k, *sym_mn = t.product == SECOND ? &maps.a_mn : &maps.b_mn;
                 const CUtensorMap *ak = a_x ? &maps.x_k[x] : sym_k, *an = a_x ? &maps.x_mn[x] : sym_mn, *bk = b_x ? &maps.x_k[x] : sym_k, *bn = b_x ? &maps.x_mn[x] : sym_mn;
@@ -411,6 +561,15 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                     if (PAIR) mbar_try_wait_cluster(ring_empty0 + 8u * slot, par);
                 }
                 const int4 a = order.find(atomicAdd(p.next, 1));
+                if (a.x >= 0) {  // handed out when what it reads is there: then nobody else has to look
+                    const NsShape &h = p.s[a.y >> 16];
+                    const int32_t *count = p.done + h.first + a.x, step = a.y >> 2 & 0x3fff, product = a.y & 3, each = 2 * h.square + h.tiles3;
+                    bool ok = wait_count(count, arrivals<PAIR>() * (step * each + product * h.square), abort_flag, p.status);
+                    if (ok && step == 0 && product == FIRST && a.x >= h.slots)  // and the slot's last user has read what is overwritten now
+                        ok = wait_count(count - h.slots, arrivals<PAIR>() * p.steps * each, abort_flag, p.status);
+                    if (!ok) break;
+                    fence_async();  // what other SMs' copies have stored, before copies read it
+                }
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ring + 16u * slot), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
                 if (PAIR) st_cluster_v4(peer_ring + 16u * slot, a);
                 mbar_arrive(ring_full0 + 8u * slot);
@@ -430,16 +589,19 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                 const NsMaps &maps = all_maps.m[t.shape];
                 const bool last = t.product == THIRD && t.step + 1 == p.steps;
                 const int to = (t.step & 1) ^ 1;  // of X
-                const CUtensorMap *out = t.product == FIRST ? &maps.a_box : t.product == SECOND ? &maps.b_box : &maps.x_box[to];
-                const int matrix = t.product == THIRD && !to ? t.matrix : t.matrix % h.slots;
+                const CUtensorMap *out = t.product == FIRST ? &maps.a_k : t.product == SECOND ? &maps.b_k : &maps.x_k[to];
+                const int matrix = t.product == THIRD && !to ? t.matrix : t.slot;
+                const int32_t row0 = t.row + 128 * (int)rank, cols = cols_out(h, t), width = width_of(h, t);
+                const bool here = row0 < (t.product == THIRD ? h.rows : h.M);
                 for (int u = 0; u < 2 && ok; ++u) {
                     ok = mbar_wait(box_ready0 + 8u * u, ph, abort_flag, p.status);
                     if (!ok) break;
                     if (last) continue;
-                    for (int w = 0; w < 8; ++w) {
-                        int32_t row0, first;
-                        if (u < boxes_of(h, t, w, row0, first)) store_box_3d(out, base + NST * STAGE + (w * 2 + u) * BOX, first + 64 * u, row0, matrix);
-                    }
+                    if (here)
+                        for (int half = 0; half < 2; ++half) {
+                            const int32_t col = t.col + half * (width / 2) + 64 * u;
+                            if (64 * u < width / 2 && col < cols) store_box_3d(out, base + NST * STAGE + (half * 2 + u) * 4 * BOX, col, row0, matrix);
+                        }
                     tma_store_commit();
                 }
                 if (!ok) break;
@@ -458,7 +620,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
         // ------------------------------------------------------------------ results (warps 2..9, both CTAs)
         // Two warps share each quarter of the accumulator's rows and take half of its columns each, in boxes of 64.
         const int w = warp - 2, quarter = warp & 3, half = w >> 2;
-        uint8_t *boxes_at = smem + NST * STAGE + w * 2 * BOX;
+        uint8_t *boxes_at = smem + NST * STAGE + (half * 8 + quarter) * BOX;  // of the first box; the second one's are 4 boxes on: the four quarters' rows lie together
         float *factors = reinterpret_cast<float *>(smem + NS_DATA + 512 + w * 128);
         const float lr = p.rates ? p.rates->lr : p.lr;
         int acc = 0;
@@ -468,36 +630,28 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
         bool ok = true;
         while (ok && tiles.next(t)) {
             const NsShape &h = p.s[t.shape];
-            int32_t row0, first;
-            const int boxes = boxes_of(h, t, w, row0, first);
-            const int32_t row = row0 + lane;
-            const int slot = t.matrix % h.slots, x = t.step & 1;
+            BoxWork b;
+            b.boxes_n = boxes_of(h, t, w, b.row0, b.first);
+            const int32_t row = b.row0 + lane;
+            const int slot = t.slot, x = t.step & 1;
             const bool last = t.product == THIRD && t.step + 1 == p.steps;
             float *d = h.d + (int64_t)slot * h.M, *r = h.r + (int64_t)slot * h.M;
-            // What the result is added to, box by box, is on its way while the products run: A' or X as it was, and the diagonals' elements of this lane's row and of its columns
-            const __half *from = t.product == SECOND ? h.a + ((int64_t)slot * h.M + row) * h.Mld + first : h.x[x] + ((int64_t)(x ? slot : t.matrix) * h.rows + row) * h.ld + first;
-            const bool in = t.product != FIRST && row < (t.product == SECOND ? h.M : h.rows);
-            const float *of_cols = t.product == SECOND ? d : t.product == THIRD && !h.left ? r : nullptr;
-            uint32_t old[2][32];
-            float of_row = 0.0f, of_col[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (t.product != FIRST) {
-                ok = wait_count(p.done + h.first + t.matrix, wanted<PAIR>(h, t), abort_flag, p.status);  // (the copying thread has seen it, and this one has to)
-                if (ok) {
-                    if (row < h.M && (t.product == SECOND || h.left)) of_row = __ldcg((t.product == SECOND ? d : r) + row);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        load_old(from + 64 * u, in && u < boxes, old[u]);
-                        if (of_cols && u < boxes)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                if (first + 64 * u + 32 * j + lane < h.M) of_col[2 * u + j] = __ldcg(of_cols + first + 64 * u + 32 * j + lane);
-                    }
-                }
-            }
-            ok = __all_sync(0xffffffffu, ok && mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.status));
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t mine = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * ACC + half * (width_of(h, t) / 2);
+            b.boxes = boxes_at; b.factors = factors; b.M = h.M;
+            b.box_empty0 = box_empty0; b.box_ready0 = box_ready0; b.box_parity = box_ph ^ 1u;
+            b.abort_flag = abort_flag; b.status = p.status;
+            b.diagonal = t.product == FIRST ? d : r;
+            // What the result is added to: A' or X as it was, and the diagonals' elements of this lane's row and of its columns
+            b.from = t.product == SECOND ? h.a + ((int64_t)slot * h.M + row) * h.Mld + b.first : h.x[x] + ((int64_t)(x ? slot : t.matrix) * h.rows + row) * h.ld + b.first;
+            b.in = row < (t.product == SECOND ? h.M : h.rows);
+            b.of_cols = t.product == SECOND ? d : r;
+            b.of_row = 0.0f;
+            if (t.product != FIRST && row < h.M && (t.product == SECOND || h.left)) b.of_row = __ldcg((t.product == SECOND ? d : r) + row);
+            auto wait_accumulator = [&]() {
+                const bool full = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.status));
+                tc_fence_after();
+                return full;
+            };
+            b.accumulator = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * ACC + half * (width_of(h, t) / 2);
             auto release = [&]() {  // the warp's part of the accumulator is in registers: the buffer goes back
                 tc_fence_before();
                 __syncwarp();
@@ -506,75 +660,37 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                     else mbar_arrive(tempty_bar(acc));
                 }
             };
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                // The last tile's box has been stored: what a warp without one waits for too, whose report below would else count for that tile's
-                ok = ok && __all_sync(0xffffffffu, mbar_wait(box_empty0 + 8u * u, box_ph ^ 1u, abort_flag, p.status));
-                if (ok && u < boxes) {
-                    const int32_t col = first + 64 * u;
-                    uint8_t *box = boxes_at + u * BOX;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        uint32_t raw[32];
-                        tc_ld_32x32(mine + 64 * u + 32 * j, raw);
-                        tc_ld_wait();
-                        if (u + 1 == boxes && j == 1) release();
-                        float2 v[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] = make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
-                        if (of_cols) {
-                            __syncwarp();
-                            factors[lane] = of_col[2 * u + j];
-                            __syncwarp();
-                        }
-                        if (t.product != THIRD && col + 32 * j == row0) {  // the diagonal: kept in float; no part of the operand (and A' has a zero here)
-                            float own = 0.0f;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                float &e = i & 1 ? v[i / 2].y : v[i / 2].x;
-                                if (i == lane) { own = e; e = 0.0f; }
-                            }
-                            own *= 1.0f / (MUON_UNIT * MUON_UNIT);
-                            if (row < h.M) (t.product == FIRST ? d : r)[row] = t.product == FIRST ? own : fmaf(NS_C, fmaf(of_row, of_row, own), fmaf(NS_B, of_row, NS_A));
-                        }
-                        if (t.product == FIRST) finish<K_FIRST, false>(v, old[u] + 16 * j, 0.0f, factors);
-                        else if (t.product == SECOND) finish<K_SECOND, true>(v, old[u] + 16 * j, of_row, factors);
-                        else if (!last) of_cols ? finish<K_THIRD, true>(v, old[u] + 16 * j, of_row, factors) : finish<K_THIRD, false>(v, old[u] + 16 * j, of_row, factors);
-                        else of_cols ? finish<K_LAST, true>(v, old[u] + 16 * j, of_row, factors) : finish<K_LAST, false>(v, old[u] + 16 * j, of_row, factors);
-                        if (!last) {
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                uint32_t packed[4];
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const __half2 two = __floats2half2_rn(v[4 * q + i].x, v[4 * q + i].y);
-                                    packed[i] = *reinterpret_cast<const uint32_t *>(&two);
-                                }
-                                *reinterpret_cast<uint4 *>(box + lane * 128 + (((4 * j + q) ^ (lane & 7)) << 4)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
-                            }
-                        } else if (col + 32 * j < h.cols) {  // onto the weights
-                            const int32_t matrix = h.first + t.matrix, i = batch.entry_of(matrix);
-                            const MuonEntry &e = batch.t[i];
-                            __syncwarp();
-                            float *floats = reinterpret_cast<float *>(box);
-#pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                *reinterpret_cast<float4 *>(floats + lane * 32 + ((q ^ (lane & 7)) << 2)) = make_float4(v[2 * q].x, v[2 * q].y, v[2 * q + 1].x, v[2 * q + 1].y);
-                            __syncwarp();
-                            const int64_t at = ((int64_t)(matrix - batch.before[i]) * h.rows + row0) * h.cols + col + 32 * j;
-                            const int32_t rl = h.rows - row0, cl = h.cols - col - 32 * j;
-                            const bool vectors = h.cols % 4 == 0;
-                            if (e.kind & 8) vectors ? step_box<true, true, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<true, true, false>(h.cols, e, at, rl, cl, floats, lane, lr);
-                            else if (e.kind & 1) vectors ? step_box<true, false, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<true, false, false>(h.cols, e, at, rl, cl, floats, lane, lr);
-                            else vectors ? step_box<false, false, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<false, false, false>(h.cols, e, at, rl, cl, floats, lane, lr);
-                        }
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(box_ready0 + 8u * u);
+            const int32_t entry = last ? batch.entry_of(h.first + t.matrix) : 0;
+            const MuonEntry &e = batch.t[entry];
+            const int64_t weights_at = ((int64_t)(h.first + t.matrix - batch.before[entry]) * h.rows + b.row0) * h.cols;
+            RowOfWeights weights;
+            weights.floats = nullptr;
+            weights.halves = nullptr;
+            if (last) {
+                const int64_t at = weights_at + (int64_t)lane * h.cols;
+                weights.floats = e.kind & 8 ? e.master + at : e.kind & 1 ? nullptr : static_cast<float *>(e.w) + at;
+                weights.halves = e.kind & 1 ? static_cast<bf16 *>(e.w) + at : nullptr;
+                weights.scale = e.scale; weights.decay = e.decay;
             }
-            if (boxes == 0) release();
+            auto onto_weights = [&](int32_t col, const float *floats) {
+                if (col >= h.cols) return;
+                const int64_t at = weights_at + col;
+                const int32_t rl = h.rows - b.row0, cl = h.cols - col;
+                const bool vectors = h.cols % 4 == 0;
+                if (e.kind & 8) vectors ? step_box<true, true, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<true, true, false>(h.cols, e, at, rl, cl, floats, lane, lr);
+                else if (e.kind & 1) vectors ? step_box<true, false, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<true, false, false>(h.cols, e, at, rl, cl, floats, lane, lr);
+                else vectors ? step_box<false, false, true>(h.cols, e, at, rl, cl, floats, lane, lr) : step_box<false, false, false>(h.cols, e, at, rl, cl, floats, lane, lr);
+            };
+            auto make = [&](auto kind, auto cols, auto rows) {
+                return make_boxes<decltype(kind)::value, decltype(cols)::value, decltype(rows)::value>(b, lane, lr, weights, h.cols, wait_accumulator, release, onto_weights);
+            };
+            using Yes = std::true_type;
+            using No = std::false_type;
+            if (t.product == FIRST) ok = make(std::integral_constant<int, K_FIRST>(), No(), No());
+            else if (t.product == SECOND) ok = make(std::integral_constant<int, K_SECOND>(), Yes(), No());
+            else if (!last) ok = h.left ? make(std::integral_constant<int, K_THIRD>(), No(), No()) : make(std::integral_constant<int, K_THIRD>(), Yes(), No());
+            else if (h.cols % 32 == 0) ok = h.left ? make(std::integral_constant<int, K_LAST>(), No(), Yes()) : make(std::integral_constant<int, K_LAST>(), Yes(), Yes());
+            else ok = h.left ? make(std::integral_constant<int, K_LAST>(), No(), No()) : make(std::integral_constant<int, K_LAST>(), Yes(), No());
             box_ph ^= 1u;
             if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
         }
@@ -591,7 +707,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
 }
 
 // ------------------------------------------------------------------------------------------ host
-constexpr int64_t GROUP_TILES = 96;  // of A in a group, on SM pairs (74): more than one for each; twice as many on single SMs
+constexpr int64_t GROUP_TILES = 222;  // of A in a group, on SM pairs (74): three for each; twice as many on single SMs
 void tiles_of(int32_t rows, int32_t cols, bool pair, NsShape *s) {
     const int side = pair ? 256 : 128;
     const int64_t edge = cdiv(imin(rows, cols), side);
@@ -627,12 +743,11 @@ NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, Carver &cv, NsSc
     s.x[0] = m.x; s.x[1] = at->x; s.a = at->a;
     return s;
 }
-// [count][rows][ld] halves: boxes of 64 columns x 128 rows, of 64 rows x two pieces of 64 columns, and for stores of 64 columns x 32 rows
-int32_t maps_of(const __half *at, int64_t count, int64_t rows, int64_t ld, CUtensorMap *k, CUtensorMap *mn, CUtensorMap *box32) {
+// [count][rows][ld] halves: boxes of 64 columns x 128 rows (of stores too), and of 64 rows x two pieces of 64 columns
+int32_t maps_of(const __half *at, int64_t count, int64_t rows, int64_t ld, CUtensorMap *k, CUtensorMap *mn) {
     const uint64_t dims[3] = {(uint64_t)ld, (uint64_t)rows, (uint64_t)count}, str[2] = {(uint64_t)ld * 2, (uint64_t)(rows * ld) * 2};
-    const uint32_t box[3] = {64, 128, 1}, box_out[3] = {64, 32, 1};
+    const uint32_t box[3] = {64, 128, 1};
     MOE_TRY(tc_make_map(k, at, 3, dims, str, box));
-    MOE_TRY(tc_make_map(box32, at, 3, dims, str, box_out));
     const uint64_t dims4[4] = {64, (uint64_t)rows, (uint64_t)(ld / 64), (uint64_t)count}, str4[3] = {(uint64_t)ld * 2, 128, (uint64_t)(rows * ld) * 2};
     const uint32_t box4[4] = {64, BK, 2, 1};
     return tc_make_map(mn, at, 4, dims4, str4, box4);
@@ -693,10 +808,10 @@ int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st) {
         NsShape &s = p.s[i];
         NsMaps &m = maps.m[i];
         s = shape_of(b.s[i], w.pair, groups, cv, &at);
-        MOE_TRY(maps_of(b.s[i].x, s.matrices, s.rows, s.ld, &m.x_k[0], &m.x_mn[0], &m.x_box[0]));
-        MOE_TRY(maps_of(at.x, s.slots, s.rows, s.ld, &m.x_k[1], &m.x_mn[1], &m.x_box[1]));
-        MOE_TRY(maps_of(at.a, s.slots, s.M, s.Mld, &m.a_k, &m.a_mn, &m.a_box));
-        MOE_TRY(maps_of(at.b, s.slots, s.M, s.Mld, &m.b_k, &m.b_mn, &m.b_box));
+        MOE_TRY(maps_of(b.s[i].x, s.matrices, s.rows, s.ld, &m.x_k[0], &m.x_mn[0]));
+        MOE_TRY(maps_of(at.x, s.slots, s.rows, s.ld, &m.x_k[1], &m.x_mn[1]));
+        MOE_TRY(maps_of(at.a, s.slots, s.M, s.Mld, &m.a_k, &m.a_mn));
+        MOE_TRY(maps_of(at.b, s.slots, s.M, s.Mld, &m.b_k, &m.b_mn));
         total += (int64_t)s.matrices * w.steps * (2 * (int64_t)s.square + s.tiles3);
         p.groups = (int32_t)imax(p.groups, cdiv(s.matrices, s.group));
     }
