@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "muon.cuh"
+#include "muon_passes.cuh"
 #include "pairs.cuh"
 #include "tc.cuh"
 #include "vectors.cuh"
@@ -16,56 +17,8 @@ namespace moe {
 
 namespace {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32, EACH = 8, TURNS = 4;
-constexpr int CHUNK = THREADS * EACH * TURNS;  // elements of a block
+constexpr int THREADS = PASS_THREADS, WARPS = THREADS / 32, CHUNK = PASS_CHUNK;
 constexpr int64_t MOST_X = (int64_t)1 << 30;   // bytes of X of a launch (one matrix at least)
-
-struct Passes {
-    double *part;     // a sum of squares for every block of the first pass
-    int32_t *done;    // [matrices]
-    int32_t *next, *status;
-    int32_t clear_status, nesterov;
-    float momentum, eps, grad_scale;
-    const moe_muon_rates *rates;
-};
-
-// Eight elements from p + at, or those of them that there are
-template <typename T, bool VECTORS> __device__ __forceinline__ void load8(const T *p, int64_t at, int64_t live, float (&v)[EACH]) {
-    if constexpr (VECTORS) {
-        constexpr int N = Vec<T>::N;
-#pragma unroll
-        for (int i = 0; i < EACH / N; ++i) {
-            Vec<T> q;
-            q.raw = *reinterpret_cast<const uint4 *>(p + at + i * N);
-#pragma unroll
-            for (int j = 0; j < N; j += 2) {
-                const float2 f = q.get(j);
-                v[i * N + j] = f.x;
-                v[i * N + j + 1] = f.y;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) v[i] = i < live ? to_f32(p[at + i]) : 0.0f;
-    }
-}
-template <typename T, bool VECTORS> __device__ __forceinline__ void store8(T *p, int64_t at, int64_t live, const float (&v)[EACH]) {
-    if constexpr (VECTORS) {
-        constexpr int N = Vec<T>::N;
-#pragma unroll
-        for (int i = 0; i < EACH / N; ++i) {
-            Vec<T> q;
-#pragma unroll
-            for (int j = 0; j < N; j += 2) q.set(j, make_float2(v[i * N + j], v[i * N + j + 1]));
-            *reinterpret_cast<uint4 *>(p + at + i * N) = q.raw;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (i < live) p[at + i] = from_f32<T>(v[i]);
-    }
-}
-template <typename T> __device__ __forceinline__ float held(float v) { return to_f32(from_f32<T>(v)); }
 
 __device__ __forceinline__ double sum_of_block(double v, double *sh) {
 #pragma unroll
@@ -78,40 +31,7 @@ __device__ __forceinline__ double sum_of_block(double v, double *sh) {
     return s;
 }
 
-// Squares are added up in float over eight elements, then in double
-template <typename GT, typename MT, bool VECTORS>
-__device__ __forceinline__ double momentum_chunk(const GT *g, MT *m, int64_t at, int64_t end, float grad_scale, const Passes &k) {
-    double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < TURNS; ++i) {
-        const int64_t here = at + (int64_t)(i * THREADS + threadIdx.x) * EACH, live = end - here;
-        if (live <= 0) break;
-        float gv[EACH], mv[EACH];
-        load8<GT, VECTORS>(g, here, live, gv);
-        load8<MT, VECTORS>(m, here, live, mv);
-        float s = 0.0f;
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            gv[j] *= grad_scale;
-            mv[j] = held<MT>(fmaf(k.momentum, mv[j], gv[j]));
-            const float u = k.nesterov ? fmaf(k.momentum, mv[j], gv[j]) : mv[j];
-            s = fmaf(u, u, s);
-        }
-        store8<MT, VECTORS>(m, here, live, mv);
-        sum += (double)s;
-    }
-    return sum;
-}
-template <bool VECTORS>
-__device__ __forceinline__ double momentum_block(const MuonEntry &t, int64_t at, int64_t end, float grad_scale, const Passes &k) {
-    switch (t.kind & 6) {
-        case 0: return momentum_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k);
-        case 2: return momentum_chunk<bf16, float, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k);
-        case 4: return momentum_chunk<float, bf16, VECTORS>(static_cast<const float *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k);
-        default: return momentum_chunk<bf16, bf16, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k);
-    }
-}
-__global__ void __launch_bounds__(THREADS) muon_momentum_kernel(const __grid_constant__ MuonBatch b, const Passes k) {
+__global__ void __launch_bounds__(THREADS) muon_momentum_kernel(const __grid_constant__ MuonBatch b, const MuonPasses k) {
     __shared__ double sh[WARPS];
     wait_previous_kernel();
     int q = 0;
@@ -137,7 +57,7 @@ __global__ void __launch_bounds__(THREADS) muon_momentum_kernel(const __grid_con
 // X in rows of ld elements, zeros behind the columns: a block has CHUNK of them, a piece of eight a thread at a time
 template <typename GT, typename MT, bool VECTORS>
 __device__ __forceinline__ void normalise_chunk(const GT *g, const MT *m, int64_t first, __half *x, int64_t begin, int64_t pieces, int32_t cols, int32_t ld, float grad_scale, float by,
-                                                const Passes &k) {
+                                                const MuonPasses &k) {
     const int32_t in_row = ld / EACH;
 #pragma unroll
     for (int i = 0; i < TURNS; ++i) {
@@ -163,7 +83,7 @@ __device__ __forceinline__ void normalise_chunk(const GT *g, const MT *m, int64_
     }
 }
 template <bool VECTORS>
-__device__ __forceinline__ void normalise_block(const MuonEntry &t, const MuonShape &s, int64_t first, __half *x, int64_t begin, float grad_scale, float by, const Passes &k) {
+__device__ __forceinline__ void normalise_block(const MuonEntry &t, const MuonShape &s, int64_t first, __half *x, int64_t begin, float grad_scale, float by, const MuonPasses &k) {
     const int64_t pieces = (int64_t)s.rows * (s.ld / EACH);
     switch (t.kind & 6) {
         case 0: return normalise_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<const float *>(t.m), first, x, begin, pieces, s.cols, s.ld, grad_scale, by, k);
@@ -172,7 +92,7 @@ __device__ __forceinline__ void normalise_block(const MuonEntry &t, const MuonSh
         default: return normalise_chunk<bf16, bf16, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<const bf16 *>(t.m), first, x, begin, pieces, s.cols, s.ld, grad_scale, by, k);
     }
 }
-__global__ void __launch_bounds__(THREADS) muon_normalise_kernel(const __grid_constant__ MuonBatch b, const Passes k) {
+__global__ void __launch_bounds__(THREADS) muon_normalise_kernel(const __grid_constant__ MuonBatch b, const MuonPasses k) {
     __shared__ double sh[WARPS];
     wait_previous_kernel();
     int q = 0;
@@ -249,8 +169,9 @@ bool fill_batch(const moe_muon_tensor *tensors, const Shape *const *shapes, int 
     }
     return true;
 }
-// The list in launches; `run` is given each. Shapes that fill the tiles of SM pairs go together, and those that do not; these go along with the others where they are an eighth of
-// their tiles or less: the chain of a gate's products then runs beside the experts'.
+// The list in launches; `run` is given each. Shapes that fill the tiles of SM pairs go together, those that one block does from beginning to end, and the others. Where there are SM pairs'
+// tiles and these are an eighth of them or less, they go along: the chain of a gate's products then runs beside the experts'.
+enum How { SMALL = 0, SINGLE = 1, PAIRS = 2 };
 template <typename Run> int32_t for_each_launch(const moe_muon_tensor *tensors, int32_t count, Run run) try {
     std::vector<Shape> all;
     for (int32_t i = 0; i < count; ++i) {
@@ -262,24 +183,30 @@ template <typename Run> int32_t for_each_launch(const moe_muon_tensor *tensors, 
         all[q].matrices += t.count;
         all[q].tensors.push_back(i);
     }
-    std::vector<const Shape *> kinds[2];  // single SMs, pairs
-    int64_t single = 0, paired = 0;
+    std::vector<const Shape *> kinds[3];
+    int64_t others = 0, paired = 0;
+    size_t shapes_of_all = 0;
     for (const Shape &s : all) {
-        const bool pair = ns_pairs(s.rows, s.cols);
-        kinds[pair].push_back(&s);
-        (pair ? paired : single) += s.matrices * ns_tiles(s.rows, s.cols, true);
+        const How how = ns_pairs(s.rows, s.cols) ? PAIRS : muon_is_small(s.rows, s.cols) ? SMALL : SINGLE;
+        kinds[how].push_back(&s);
+        (how == PAIRS ? paired : others) += s.matrices * ns_tiles(s.rows, s.cols, true);
+        ++shapes_of_all;
     }
-    if (single * 8 <= paired && kinds[0].size() + kinds[1].size() <= (size_t)MUON_MAX_SHAPES) {
-        kinds[1].insert(kinds[1].end(), kinds[0].begin(), kinds[0].end());
-        kinds[0].clear();
-    }
+    if (others * 8 <= paired && shapes_of_all <= (size_t)MUON_MAX_SHAPES)
+        for (int how = SMALL; how < PAIRS; ++how) {
+            kinds[PAIRS].insert(kinds[PAIRS].end(), kinds[how].begin(), kinds[how].end());
+            kinds[how].clear();
+        }
     MuonBatch b;
-    for (int pair = 1; pair >= 0; --pair)
-        for (size_t from = 0; from < kinds[pair].size(); from += MUON_MAX_SHAPES) {
-            const Shape *const *shapes = kinds[pair].data() + from;
-            const int n = (int)imin(MUON_MAX_SHAPES, (int64_t)(kinds[pair].size() - from));
-            int64_t bytes = 0, most = 0;
-            for (int q = 0; q < n; ++q) { bytes += shapes[q]->x_bytes(); most = imax(most, shapes[q]->matrices); }
+    for (int how = PAIRS; how >= SMALL; --how)
+        for (size_t from = 0; from < kinds[how].size(); from += MUON_MAX_SHAPES) {
+            const Shape *const *shapes = kinds[how].data() + from;
+            const int n = (int)imin(MUON_MAX_SHAPES, (int64_t)(kinds[how].size() - from));
+            int64_t bytes = 1, most = 0;
+            for (int q = 0; q < n; ++q) {
+                if (how != SMALL) bytes += shapes[q]->x_bytes();
+                most = imax(most, shapes[q]->matrices);
+            }
             int64_t parts = imin(most, cdiv(bytes, MOST_X));
             for (int64_t part = 0; part < parts; ++part)
                 if (!fill_batch(tensors, shapes, n, part, parts, &b)) {
@@ -289,7 +216,7 @@ template <typename Run> int32_t for_each_launch(const moe_muon_tensor *tensors, 
                 }
             for (int64_t part = 0; part < parts; ++part) {
                 fill_batch(tensors, shapes, n, part, parts, &b);
-                if (b.n) MOE_TRY(run(b, pair != 0));
+                if (b.n) MOE_TRY(run(b, (How)how));
             }
         }
     return MOE_OK;
@@ -324,10 +251,11 @@ int32_t muon_check(const moe_muon_tensor *tensors, int32_t count) {
 
 int32_t muon_bytes(const moe_muon_tensor *tensors, int32_t count, int64_t *bytes) {
     *bytes = kWsHeader;
-    return for_each_launch(tensors, count, [&](MuonBatch &b, bool pair) -> int32_t {
+    return for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
+        if (how == SMALL) return MOE_OK;
         Carver cv(nullptr);
         cv.take_bytes(kWsHeader);
-        scratch_of(cv, b, pair);
+        scratch_of(cv, b, how == PAIRS);
         *bytes = imax(*bytes, (int64_t)cv.off);
         return MOE_OK;
     });
@@ -335,22 +263,24 @@ int32_t muon_bytes(const moe_muon_tensor *tensors, int32_t count, int64_t *bytes
 
 int32_t launch_muon(const moe_muon_tensor *tensors, int32_t count, const moe_muon_params &p, const moe_muon_rates *rates, void *ws, cudaStream_t st) {
     bool first = true;
-    return for_each_launch(tensors, count, [&](MuonBatch &b, bool pair) -> int32_t {
+    return for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
+        const bool pair = how == PAIRS;
         Carver cv(ws);
         int32_t *status = static_cast<int32_t *>(cv.take_bytes(kWsHeader));
-        const Scratch s = scratch_of(cv, b, pair);
-        Passes k = {};
-        k.part = s.part; k.done = s.done; k.next = s.next; k.status = status;
+        MuonPasses k = {};
+        k.status = status;
         k.clear_status = first; k.nesterov = p.nesterov;
         k.momentum = (float)p.momentum; k.eps = (float)p.eps; k.grad_scale = (float)p.grad_scale; k.rates = rates;
+        first = false;
+        if (how == SMALL) return launch_muon_small(b, k, (float)p.lr, p.steps, st);
+        const Scratch s = scratch_of(cv, b, pair);
+        k.part = s.part; k.done = s.done; k.next = s.next;
         launch_kernel(muon_momentum_kernel, dim3((unsigned)blocks_of(b, false)), dim3(THREADS), 0, st, b, k);
         MOE_LAUNCHED();
         launch_kernel(muon_normalise_kernel, dim3((unsigned)blocks_of(b, true)), dim3(THREADS), 0, st, b, k);
         MOE_LAUNCHED();
         const NsWork w = {&b, pair, p.steps, s.done, s.next, status, s.products, (float)p.lr, rates};
-        MOE_TRY(launch_newton_schulz(w, st));
-        first = false;
-        return MOE_OK;
+        return launch_newton_schulz(w, st);
     });
 }
 

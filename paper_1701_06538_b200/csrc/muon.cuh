@@ -41,6 +41,19 @@ struct MuonBatch {
 };
 static inline int64_t muon_ld(int64_t cols) { return cdiv(cols, 64) * 64; }
 
+struct MuonPasses {
+    double *part;     // a sum of squares for every block of the first pass
+    int32_t *done;    // [matrices]
+    int32_t *next, *status;
+    int32_t clear_status, nesterov;
+    float momentum, eps, grad_scale;
+    const moe_muon_rates *rates;
+};
+
+// The whole step by a block a matrix, for small ones (muon_small.cu)
+bool muon_is_small(int32_t rows, int32_t cols);
+int32_t launch_muon_small(const MuonBatch &b, const MuonPasses &k, float lr, int32_t steps, cudaStream_t st);
+
 // Newton-Schulz products of a batch's matrices and the step on their weights. Scratch: ns_scratch_bytes
 struct NsWork {
     const MuonBatch *batch;

@@ -1,0 +1,95 @@
+// The first pass of the Muon step over a block's elements, 256 threads a chunk (muon.cu, muon_small.cu): m = momentum m + g and the squares of u
+#pragma once
+
+#include "muon.cuh"
+#include "vectors.cuh"
+
+namespace moe {
+
+namespace {
+
+constexpr int PASS_THREADS = 256, EACH = 8, TURNS = 4;
+constexpr int PASS_CHUNK = PASS_THREADS * EACH * TURNS;  // elements of a block
+
+// Eight elements from p + at, or those of them that there are
+template <typename T, bool VECTORS> __device__ __forceinline__ void load8(const T *p, int64_t at, int64_t live, float (&v)[EACH]) {
+    if constexpr (VECTORS) {
+        constexpr int N = Vec<T>::N;
+#pragma unroll
+        for (int i = 0; i < EACH / N; ++i) {
+            Vec<T> q;
+            q.raw = *reinterpret_cast<const uint4 *>(p + at + i * N);
+#pragma unroll
+            for (int j = 0; j < N; j += 2) {
+                const float2 f = q.get(j);
+                v[i * N + j] = f.x;
+                v[i * N + j + 1] = f.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) v[i] = i < live ? to_f32(p[at + i]) : 0.0f;
+    }
+}
+template <typename T, bool VECTORS> __device__ __forceinline__ void store8(T *p, int64_t at, int64_t live, const float (&v)[EACH]) {
+    if constexpr (VECTORS) {
+        constexpr int N = Vec<T>::N;
+#pragma unroll
+        for (int i = 0; i < EACH / N; ++i) {
+            Vec<T> q;
+#pragma unroll
+            for (int j = 0; j < N; j += 2) q.set(j, make_float2(v[i * N + j], v[i * N + j + 1]));
+            *reinterpret_cast<uint4 *>(p + at + i * N) = q.raw;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (i < live) p[at + i] = from_f32<T>(v[i]);
+    }
+}
+template <typename T> __device__ __forceinline__ float held(float v) { return to_f32(from_f32<T>(v)); }
+
+// Squares are added up in float over eight elements, then in double
+template <typename GT, typename MT, bool VECTORS>
+__device__ __forceinline__ double momentum_chunk(const GT *g, MT *m, int64_t at, int64_t end, float grad_scale, const MuonPasses &k) {
+    double sum = 0.0;
+    const int64_t first = at + (int64_t)(threadIdx.x % PASS_THREADS) * EACH;
+    float gv[TURNS][EACH], mv[TURNS][EACH];  // all loads before the first store
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const int64_t here = first + (int64_t)i * (PASS_THREADS * EACH), live = end - here;
+        if (live > 0) {
+            load8<GT, VECTORS>(g, here, live, gv[i]);
+            load8<MT, VECTORS>(m, here, live, mv[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const int64_t here = first + (int64_t)i * (PASS_THREADS * EACH), live = end - here;
+        if (live <= 0) continue;
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const float gj = gv[i][j] * grad_scale;
+            mv[i][j] = held<MT>(fmaf(k.momentum, mv[i][j], gj));
+            const float u = k.nesterov ? fmaf(k.momentum, mv[i][j], gj) : mv[i][j];
+            s = fmaf(u, u, s);
+        }
+        store8<MT, VECTORS>(m, here, live, mv[i]);
+        sum += (double)s;
+    }
+    return sum;
+}
+template <bool VECTORS>
+__device__ __forceinline__ double momentum_block(const MuonEntry &t, int64_t at, int64_t end, float grad_scale, const MuonPasses &k) {
+    switch (t.kind & 6) {
+        case 0: return momentum_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k);
+        case 2: return momentum_chunk<bf16, float, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<float *>(t.m), at, end, grad_scale, k);
+        case 4: return momentum_chunk<float, bf16, VECTORS>(static_cast<const float *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k);
+        default: return momentum_chunk<bf16, bf16, VECTORS>(static_cast<const bf16 *>(t.g), static_cast<bf16 *>(t.m), at, end, grad_scale, k);
+    }
+}
+
+}  // namespace
+
+}  // namespace moe

@@ -26,6 +26,7 @@
 
 #include "muon.cuh"
 #include "pairs.cuh"
+#include "short_wait.cuh"
 #include "tc.cuh"
 
 namespace moe {
@@ -106,7 +107,8 @@ __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
     return v;
 }
 __device__ __forceinline__ bool wait_count(const int32_t *count, int32_t at_least, volatile int *abort_flag, int32_t *status) {
-    if (load_acquire(count) >= at_least) return true;
+    for (int i = 0; i < 64; ++i)
+        if (load_acquire(count) >= at_least) return true;
     const unsigned long long t0 = global_ns();
     while (load_acquire(count) < at_least) {
         if (*abort_flag) return false;
@@ -137,7 +139,7 @@ template <bool PAIR> struct NsRing {
     int i;
     __device__ __forceinline__ bool next(NsTile &t) {
         const uint32_t slot = (uint32_t)i % RING, par = ((uint32_t)i / RING) & 1u, full = full0 + 8u * slot;
-        bool ok = mbar_wait(full, par, abort_flag, p.status);
+        bool ok = short_wait(full, par, abort_flag, p.status);
         if (warp_wide) ok = __all_sync(0xffffffffu, ok);
         if (!ok) return false;
         if (PAIR) mbar_try_wait_cluster(full, par);  // acquire at cluster scope: the record came from the other CTA's thread
@@ -389,7 +391,7 @@ __device__ __forceinline__ bool make_boxes(const BoxWork &b, int lane, float lr,
 #pragma unroll 1
     for (int u = 0; u < 2; ++u) {
         // The last tile's box has been stored: what a warp without one waits for too, whose report below would else count for that tile's
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(b.box_empty0 + 8u * u, b.box_parity, b.abort_flag, b.status));
+        ok = ok && __all_sync(0xffffffffu, short_wait(b.box_empty0 + 8u * u, b.box_parity, b.abort_flag, b.status));
         if (ok && u < b.boxes_n) {
             uint32_t raw0[32], raw1[32];
             tc_ld_32x32(b.accumulator + 64 * u, raw0);
@@ -491,7 +493,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                 const int a0 = t.row + 128 * (int)rank, b0 = t.col + (PAIR ? width_of(h, t) / 2 * (int)rank : 0);
                 const int kblocks = kblocks_of(h, t);
                 for (int kb = 0; kb < kblocks; ++kb) {
-                    ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.status);
+                    ok = short_wait(empty_bar(s), ph ^ 1u, abort_flag, p.status);
                     if (!ok) break;
                     if (rank == 0) mbar_expect_tx(full_bar(s), PAIR ? 2 * STAGE : STAGE);
                     auto load = [&](uint32_t dst, bool mn, const CUtensorMap *k_map, const CUtensorMap *mn_map, int at, int matrix) {
@@ -511,40 +513,40 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             if (!ok) gave_up();
         }
     } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer (one thread, even CTA only)
-        if (rank == 0 && lane == 0) {
+        // ------------------------------------------------------------------ MMA issuer (even CTA only; the warp stays together)
+        if (rank == 0) {
             int s = 0, acc = 0;
             uint32_t ph = 0, acc_ph = 0;
             bool ok = true;
-            NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, false, true, 0};
+            NsRing<PAIR> tiles{p, ring, ring_full0, ring_empty0, abort_flag, true, lane == 0, 0};
             NsTile t;
             while (ok && tiles.next(t)) {
                 const NsShape &h = p.s[t.shape];
-                ok = mbar_wait(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.status);
+                ok = __all_sync(0xffffffffu, short_wait(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.status));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * ACC;
                 const int kblocks = kblocks_of(h, t), width = width_of(h, t);
                 for (int kb = 0; kb < kblocks; ++kb) {
                     const bool a_mn = a_is_mn(h, t, kb), b_mn = b_is_mn(h, t, kb);
-                    ok = mbar_wait(full_bar(s), ph, abort_flag, p.status);
+                    ok = __all_sync(0xffffffffu, short_wait(full_bar(s), ph, abort_flag, p.status));
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t a_src = base + s * STAGE, b_src = a_src + A2_BYTES, idesc = idesc_of(PAIR, a_mn, b_mn, width);
                     const uint64_t ad = a_mn ? desc_mnmajor(a_src) : desc_kmajor(a_src), bd = b_mn ? desc_mnmajor(b_src) : desc_kmajor(b_src);
-                    const uint64_t a_step = a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = b_mn ? (16 * 128) >> 4 : 32 >> 4;
+                    const uint32_t a_step = a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = b_mn ? (16 * 128) >> 4 : 32 >> 4;
 #pragma unroll
                     for (int k = 0; k < BK / 16; ++k) {
-                        if (PAIR) tc_mma2_bf16(d_tmem, ad + k * a_step, bd + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
-                        else tc_mma_bf16(d_tmem, ad + k * a_step, bd + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                        if (PAIR) warp_mma2(d_tmem, ad + k * a_step, bd + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                        else warp_mma(d_tmem, ad + k * a_step, bd + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
                     }
-                    if (PAIR) tc_commit2(empty_bar(s));
-                    else tc_commit(empty_bar(s));
+                    if (PAIR) warp_commit2(empty_bar(s));
+                    else warp_commit(empty_bar(s));
                     if (++s == NST) { s = 0; ph ^= 1u; }
                 }
                 if (!ok) break;
-                if (PAIR) tc_commit2(tfull_bar(acc));
-                else tc_commit(tfull_bar(acc));
+                if (PAIR) warp_commit2(tfull_bar(acc));
+                else warp_commit(tfull_bar(acc));
                 if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
             }
         }
@@ -557,7 +559,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                 const uint32_t slot = (uint32_t)i % RING;
                 if (i >= RING) {  // every reader of the record this slot held has its copy
                     const uint32_t par = ((uint32_t)i / RING - 1) & 1u;
-                    if (!mbar_wait(ring_empty0 + 8u * slot, par, abort_flag, p.status)) break;
+                    if (!short_wait(ring_empty0 + 8u * slot, par, abort_flag, p.status)) break;
                     if (PAIR) mbar_try_wait_cluster(ring_empty0 + 8u * slot, par);
                 }
                 const int4 a = order.find(atomicAdd(p.next, 1));
@@ -594,7 +596,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                 const int32_t row0 = t.row + 128 * (int)rank, cols = cols_out(h, t), width = width_of(h, t);
                 const bool here = row0 < (t.product == THIRD ? h.rows : h.M);
                 for (int u = 0; u < 2 && ok; ++u) {
-                    ok = mbar_wait(box_ready0 + 8u * u, ph, abort_flag, p.status);
+                    ok = short_wait(box_ready0 + 8u * u, ph, abort_flag, p.status);
                     if (!ok) break;
                     if (last) continue;
                     if (here)
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             b.of_row = 0.0f;
             if (t.product != FIRST && row < h.M && (t.product == SECOND || h.left)) b.of_row = __ldcg((t.product == SECOND ? d : r) + row);
             auto wait_accumulator = [&]() {
-                const bool full = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.status));
+                const bool full = __all_sync(0xffffffffu, short_wait(tfull_bar(acc), acc_ph, abort_flag, p.status));
                 tc_fence_after();
                 return full;
             };

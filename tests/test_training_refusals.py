@@ -134,11 +134,12 @@ def test_muon_sizes(lib):
         return out.value
 
     one = need((256, 512, 1024))
-    assert one < 1.6 * 256 * 512 * 1024 * 2
+    assert one < 3 * 256 * 512 * 1024 * 2
     assert need((256, 512, 1024), (256, 1024, 512), (1, 512, 256)) < 2.1 * one
     assert need((100000, 512, 1024)) < 2 ** 30 + 2 ** 29                        # 1 GiB of X at a time
     assert need((128, 512, 1024), (128, 512, 1024)) == one                      # taken together
     assert need((1, 32768, 32768)) > 2 * 2 * 2 ** 30
+    assert need((1000, 64, 128), (3, 8, 768)) == 256                            # one block's work from beginning to end
 
 
 def test_muon_list_checks_its_tensors():
