@@ -216,18 +216,15 @@ __device__ __forceinline__ void step_box(int32_t cols, const MuonEntry &e, int64
 
 // What a result is, besides the accumulator
 enum Result { K_FIRST, K_SECOND, K_THIRD, K_LAST };
-// 32 columns of 32 rows, a row a lane. old: 32 halves of the operand that is added, row_factor and cols: the diagonal's elements of the row and of the columns (shared memory)
+// 32 columns of 32 rows, a row a lane. old: 32 halves of the operand that is added, times what the diagonals make of it: `of_row`, and of the columns `cols` (shared memory). See factor_of
 template <int KIND, bool COLS>
-__device__ __forceinline__ void finish(float2 (&v)[16], const uint32_t *old, float row_factor, const float *cols) {
+__device__ __forceinline__ void finish(float2 (&v)[16], const uint32_t *old, float of_row, const float *cols) {
     constexpr float UNIT = 1.0f / MUON_UNIT;
     constexpr float by = KIND == K_SECOND ? NS_C * UNIT : KIND == K_LAST ? UNIT * UNIT : UNIT;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        float4 c = make_float4(row_factor, row_factor, row_factor, row_factor);
-        if constexpr (COLS) {
-            const float4 of = *reinterpret_cast<const float4 *>(cols + 4 * q);
-            c = KIND == K_SECOND ? make_float4(c.x + of.x, c.y + of.y, c.z + of.z, c.w + of.w) : of;
-        }
+        float4 c = make_float4(of_row, of_row, of_row, of_row);
+        if constexpr (COLS) c = *reinterpret_cast<const float4 *>(cols + 4 * q);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             float2 &y = v[2 * q + j];
@@ -235,13 +232,16 @@ __device__ __forceinline__ void finish(float2 (&v)[16], const uint32_t *old, flo
                 y = mul2(y, both(by));
             } else {
                 float2 f = j ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
-                if constexpr (KIND == K_SECOND) f = fma2(f, both(NS_C), both(NS_B));
-                if constexpr (KIND == K_LAST) f = mul2(f, both(UNIT));
+                if constexpr (KIND == K_SECOND) f = fma2(f, both(1.0f), both(of_row));
                 const float2 o = __half22float2(*reinterpret_cast<const __half2 *>(old + 2 * q + j));
                 y = fma2(y, both(by), mul2(o, f));
             }
         }
     }
+}
+// c (d_i + d_j) + b of A' for B, r of X for X; the last X is wanted without MUON_UNIT
+template <int KIND> __device__ __forceinline__ float factor_of(float diagonal, bool column) {
+    return KIND == K_SECOND ? fmaf(NS_C, diagonal, column ? NS_B : 0.0f) : KIND == K_LAST ? diagonal * (1.0f / MUON_UNIT) : diagonal;
 }
 // 32 bytes at a time (a whole sector), of what another SM may have written in the meantime
 __device__ __forceinline__ void load_32B(const void *from, uint32_t *r) {
@@ -330,7 +330,7 @@ __device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, flo
     uint8_t *box = b.boxes + u * 4 * BOX;
     if constexpr (COLS) {
         __syncwarp();
-        b.factors[lane] = of_col;
+        b.factors[lane] = factor_of<KIND>(of_col, true);
         __syncwarp();
     }
     float2 v[16];
@@ -346,7 +346,7 @@ __device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, flo
         own *= 1.0f / (MUON_UNIT * MUON_UNIT);
         if (b.row0 + lane < b.M) b.diagonal[b.row0 + lane] = KIND == K_FIRST ? own : fmaf(NS_C, fmaf(b.of_row, b.of_row, own), fmaf(NS_B, b.of_row, NS_A));
     }
-    finish<KIND, COLS>(v, old, b.of_row, b.factors);
+    finish<KIND, COLS>(v, old, factor_of<KIND>(b.of_row, false), b.factors);
     if (u + 1 < b.boxes_n) fetch_half<KIND, COLS>(b, 64 + 32 * J, lane, old, of_col);
     if constexpr (KIND != K_LAST) {
 #pragma unroll
@@ -406,7 +406,6 @@ __device__ __forceinline__ bool make_boxes(const BoxWork &b, int lane, float lr,
             }
             make_half<KIND, COLS, ROWS, 1>(b, u, lane, lr, raw1, old1, of_col1, weights, weights_end, onto_weights);
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(b.box_ready0 + 8u * u);
     }
@@ -598,20 +597,20 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                 for (int u = 0; u < 2 && ok; ++u) {
                     ok = short_wait(box_ready0 + 8u * u, ph, abort_flag, p.status);
                     if (!ok) break;
-                    if (last) continue;
-                    if (here)
-                        for (int half = 0; half < 2; ++half) {
-                            const int32_t col = t.col + half * (width / 2) + 64 * u;
-                            if (64 * u < width / 2 && col < cols) store_box_3d(out, base + NST * STAGE + (half * 2 + u) * 4 * BOX, col, row0, matrix);
-                        }
-                    tma_store_commit();
+                    if (!last) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // what the workers have written, before this thread's copies read it
+                        if (here)
+                            for (int half = 0; half < 2; ++half) {
+                                const int32_t col = t.col + half * (width / 2) + 64 * u;
+                                if (64 * u < width / 2 && col < cols) store_box_3d(out, base + NST * STAGE + (half * 2 + u) * 4 * BOX, col, row0, matrix);
+                            }
+                        tma_store_commit();
+                        tma_store_wait_read();
+                    }
+                    mbar_arrive(box_empty0 + 8u * u);
                 }
                 if (!ok) break;
                 ph ^= 1u;
-                tma_store_wait_read_but_one();
-                mbar_arrive(box_empty0);
-                tma_store_wait_read();
-                mbar_arrive(box_empty0 + 8u);
                 tma_store_wait_all();
                 fence_async();
                 asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + h.first + t.matrix) : "memory");
