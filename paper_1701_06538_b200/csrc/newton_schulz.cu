@@ -1,20 +1,25 @@
 // Newton-Schulz products of the Muon step (Jordan et al., 2024) on the 5th-generation tensor cores, for a batch of matrices X [rows, cols]. `steps` times
-//   A = X X'  (of the shorter side: X' X where there are more rows than columns),   B = a I + b A + c A A,   X <- B X  (X B)
+//   A = X X'  (of the shorter side: X' X where there are more rows than columns),   P = a I + b A + c A A,   X <- P X  (X P)
 // and the last X goes straight from the accumulators into the weights: w = w - lr (scale X + decay w). M is the shorter side, N the longer one.
 //
-// Bound by the tensor cores: M^2 N + M^3 + 2 M^2 N operations a step and matrix, of A and B the lower half by tiles. A and B are symmetric, and what reads a tile of the upper half
-// reads the stored one in its place, transposed by the operand's major-ness, which an instruction has of its own.
+// P is a polynomial of A, so that all of them commute and a step's A follows from the one before: (P X)(P X)' = P A P. A segment of up to three steps stays with the M x M matrices
+// (T = P A, A <- P T, Q <- P Q) and touches X twice, for the first A and for X <- Q X. What that costs in 64-deep blocks of products decides (together_of): a step is M^2 N / 2 + M^3 / 2 +
+// M^2 N operations by itself and three together are M^2 N / 2 + 9/2 M^3 + M^2 N, fewer from N = 2 M on. 32 of 1024 x 4096: 5727 -> 3448 us, 16 of 1024 x 2048: 1416 -> 1220, 256 of
+// 512 x 1024: 4196 -> 4103. Four or five steps in one segment would leave fp16's range: Q reaches 3.4445^n.
+//
+// Bound by the tensor cores, which run against the power limit here (990 W; 1965 MHz become 1300 to 1500). All M x M matrices are symmetric: the lower half is made, by tiles, and what
+// reads a tile of the upper half reads the stored one in its place, transposed by the operand's major-ness, which an instruction has of its own.
 //
 // Operands are fp16, not bf16: a step multiplies small singular values by 3.4 and what rounding has put beside them too. X over its Frobenius norm and everything made of it stay
-// below 8 whatever the input, so that the range is known and fp16's three bits more are free: held times 2^10, elements down to 2^-24 are normal numbers. The diagonals of A and B are not
-// among the operands: they are kept in float, d and r, and enter the products' results beside the accumulators,
-//   A A = A' A' + A' (d_i + d_j) + d_i^2 [i = j],   B X = B' X + r X      (A', B' without their diagonals)
+// below 8 whatever the input (Q of three steps below 41), so that the range is known and fp16's three bits more are free: held times 2^10, elements down to 2^-24 are normal numbers.
+// (With bf16 the power limit allows 2 to 3 % more.) The diagonals of the M x M matrices are not among the operands: they are kept in float and enter the products' results beside the accumulators,
+//   U V = U' V' + U' v_j + u_i V' + u_i v_i [i = j],   P X = P' X + p_i X      (U', V', P' without their diagonals u, v, p)
 // An element's rounding error off the diagonal is one of many in a singular value and averages out; on the diagonal it scales a whole row, and near the singular value 1.2 a step
 // multiplies such an error by 5 (a gate of 512 x 32, whose A is nearly diagonal, was off by 3e-3 with rounded diagonals). Accumulators are float, and the last X is not rounded at all.
 //
 // All products of all matrices, of several shapes, are one launch: tiles are drawn one after the other in an order in which what a tile reads is always drawn before it (group of
-// matrices, step, product, shape, matrix, tile), and a count of stored tiles for every matrix tells when it is there. With a group that fills the SMs more than once, what a tile waits
-// for was stored long ago, and the chain of a lone matrix' products (a gate's) runs beside the others'. (A launch for every product leaves its last wave of tiles half empty: 3 tiles of A and B
+// matrices, segment, phase, shape, matrix, tile), and a count of stored tiles for every matrix tells when it is there. With a group that fills the SMs more than once, what a tile waits
+// for was stored long ago, and the chain of a lone matrix' products (a gate's) runs beside the others'. (A launch for every product leaves its last wave of tiles half empty: 3 tiles of A and P
 // and 8 of X for each of 512 x 1024.) Whoever waits does so for tiles of blocks that run already, so that no number of resident blocks is presumed.
 //
 // PAIR: two CTAs (an SM pair) have a tile of 256 x 256 by cta_group::2, each stages 128 rows of A's operand and half of B's columns. Otherwise, for M up to 128, a CTA has 128 x 128.
@@ -34,71 +39,114 @@ namespace moe {
 namespace {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
-constexpr int RING = 3;                       // tiles drawn ahead
+constexpr int RING = 3;                       // tiles drawn ahead (256 of 512 x 1024: 4451 us; with 2 and groups of 111 tiles 4579)
 constexpr int NS_THREADS = 384;
 constexpr int NS_STAGES = 5;
 constexpr uint32_t BOX = 4096;                // a warp's 32 rows of 64 columns
 constexpr int NS_DATA = NS_STAGES * STAGE2_BYTES + 2 * 8 * BOX, NS_SMEM = NS_DATA + 1024 /*alignment*/ + 512 /*barriers, ring*/ + 8 * 128 /*factors*/;
 
-enum { FIRST = 0, SECOND = 1, THIRD = 2 };    // A, B, X
-struct NsMaps { CUtensorMap x_k[2], x_mn[2], a_k, a_mn, b_k, b_mn; };  // x[0]: all matrices, the others: a ring of slots
+// What a tile is of: A = X X', P = a I + b A + c A A, a product of two of the symmetric matrices, X <- Q X
+enum Kind4 { GRAM = 0, POLY = 1, MULT = 2, APPLY = 3 };
+// The symmetric matrices
+enum { S_A = 0, S_P = 1, S_T = 2, S_P2 = 3, S_Q = 4, SYMMETRIC = 5 };
+struct NsMaps { CUtensorMap x_k[2], x_mn[2], s_k[SYMMETRIC], s_mn[SYMMETRIC]; };  // x[0]: all matrices, the others: a ring of slots
 struct NsShape {
     int32_t rows, cols, ld, M, Mld, first, matrices, left;
-    int32_t square, cols3, tiles3;            // tiles of A and B (lower half), tiles of X beside each other, of X
+    int32_t square, cols3, tiles3;            // tiles of a symmetric matrix (lower half), tiles of X beside each other, of X
     int32_t group, slots;
-    const __half *x[2], *a;
-    float *d, *r;                             // [slots][M] diagonals of A and B
+    const __half *x[2], *s[SYMMETRIC];        // [matrices or slots][rows][ld], [slots][M][Mld]
+    float *d;                                 // [SYMMETRIC][slots][M] their diagonals
 };
 struct NsArgs {
     NsShape s[MUON_MAX_SHAPES];
-    int32_t shapes, steps, groups;
+    int32_t shapes, steps, together, groups;  // together: steps of a segment
     int32_t *done, *next, *status;
     float lr;
     const moe_muon_rates *rates;
 };
 struct NsAllMaps { NsMaps m[MUON_MAX_SHAPES]; };
-struct NsTile { int32_t matrix, shape, step, product, row, col, slot; };
+struct NsTile { int32_t matrix, shape, segment, kind, a, b, out, row, col, slot; };
+
+// A segment of n steps as phases, each of which needs all before it: two products at most, a * b -> out. Q of the steps goes from P (or P2) over S_Q to S_T.
+struct NsOp { uint8_t kind, a, b, out; };
+struct NsPhase { NsOp op[2]; uint8_t n; };
+struct NsProgram { NsPhase phase[10]; uint8_t n, squares; };  // squares: products of symmetric matrices, A among them
+__host__ __device__ constexpr NsProgram program_of(int steps) {
+    constexpr NsOp none = {0, 0, 0, 0}, gram = {GRAM, 0, 0, S_A};
+    if (steps == 1) return {{{{gram, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{APPLY, S_P, 0, 0}, none}, 1}}, 3, 2};
+    if (steps == 2)
+        return {{{{gram, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{MULT, S_P, S_A, S_T}, none}, 1}, {{{MULT, S_P, S_T, S_A}, none}, 1}, {{{POLY, S_A, S_A, S_P2}, none}, 1},
+                 {{{MULT, S_P2, S_P, S_T}, none}, 1}, {{{APPLY, S_T, 0, 0}, none}, 1}}, 7, 6};
+    return {{{{gram, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{MULT, S_P, S_A, S_T}, none}, 1}, {{{MULT, S_P, S_T, S_A}, none}, 1}, {{{POLY, S_A, S_A, S_P2}, none}, 1},
+             {{{MULT, S_P2, S_A, S_T}, {MULT, S_P2, S_P, S_Q}}, 2}, {{{MULT, S_P2, S_T, S_A}, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{MULT, S_P, S_Q, S_T}, none}, 1},
+             {{{APPLY, S_T, 0, 0}, none}, 1}}, 10, 10};
+}
+__constant__ const NsProgram programs[4] = {program_of(1), program_of(1), program_of(2), program_of(3)};
+constexpr NsProgram programs_host[4] = {program_of(1), program_of(1), program_of(2), program_of(3)};
+constexpr int MOST_TOGETHER = 3;
+constexpr int symmetric_of(int together) { return together == 1 ? 2 : together == 2 ? 4 : 5; }  // that a segment uses, in their order
 
 template <bool PAIR> constexpr int tile_side() { return PAIR ? 256 : 128; }
 template <bool PAIR> constexpr int arrivals() { return PAIR ? 2 : 1; }  // of a stored tile: CTAs
 
-// The tiles in their order: {matrix or -1, shape << 16 | step << 2 | product, tile's row << 16 | column, slot} of ascending numbers
+// The tiles in their order: {matrix or -1, shape << 16 | segment << 11 | kind << 9 | a << 6 | b << 3 | out, tile's row << 16 | column, slot} of ascending numbers
 template <bool PAIR> struct NsOrder {
     const NsArgs &p;
-    int32_t group, base, each;  // the group that is at, its first number, its tiles a step
-    __device__ __forceinline__ explicit NsOrder(const NsArgs &p_) : p(p_), group(0), base(0) { each = tiles_of(); }
+    int32_t group, base;         // the group that is at, its first number
+    int32_t squares, applies;    // tiles of a group: of a symmetric matrix, of X
+    int32_t tiles_before;        // of the found one's matrix, in earlier phases
+    __device__ __forceinline__ explicit NsOrder(const NsArgs &p_) : p(p_), group(0), base(0) { count(); }
     __device__ __forceinline__ int32_t here(int s) const { return min(p.s[s].group, max(0, p.s[s].matrices - group * p.s[s].group)); }
-    __device__ __forceinline__ int32_t tiles_of() const {
-        int32_t n = 0;
-        for (int s = 0; s < p.shapes; ++s) n += here(s) * (2 * p.s[s].square + p.s[s].tiles3);
-        return n;
+    __device__ __forceinline__ void count() {
+        squares = applies = 0;
+        for (int s = 0; s < p.shapes; ++s) {
+            squares += here(s) * p.s[s].square;
+            applies += here(s) * p.s[s].tiles3;
+        }
     }
+    __device__ __forceinline__ int32_t full() const { return p.steps / p.together; }  // segments of p.together steps; one of the rest may follow
+    __device__ __forceinline__ int32_t segment_tiles(int steps) const { return steps ? programs[steps].squares * squares + applies : 0; }
+    __device__ __forceinline__ int32_t group_tiles() const { return full() * segment_tiles(p.together) + segment_tiles(p.steps % p.together); }
     __device__ __forceinline__ int4 find(int32_t id) {
-        while (group < p.groups && id - base >= each * p.steps) {
-            base += each * p.steps;
+        while (group < p.groups && id - base >= group_tiles()) {
+            base += group_tiles();
             ++group;
-            each = tiles_of();
+            count();
         }
         if (group >= p.groups) return make_int4(-1, 0, 0, 0);
         int32_t r = id - base;
-        const int32_t step = r / each;
-        r -= step * each;
-        for (int product = FIRST;; ++product)
-            for (int s = 0; s < p.shapes; ++s) {
-                const int32_t tiles = product == THIRD ? p.s[s].tiles3 : p.s[s].square, all = here(s) * tiles;
-                if (r >= all) { r -= all; continue; }
-                const int32_t m = r / tiles;
-                int32_t t = r - m * tiles, row, col;
-                if (product == THIRD) {
-                    row = t / p.s[s].cols3;
-                    col = t - row * p.s[s].cols3;
+        const int32_t each = segment_tiles(p.together), segment = min(r / each, full());
+        r -= segment * each;
+        const NsProgram &g = programs[segment < full() ? p.together : p.steps % p.together];
+        int32_t squares_before = segment * programs[p.together].squares;
+        for (int phase = 0;; ++phase) {
+            const NsPhase &f = g.phase[phase];
+            const bool apply = phase == g.n - 1;
+            const int32_t all = apply ? applies : f.n * squares;
+            if (r >= all) { r -= all; squares_before += f.n; continue; }
+            for (int s = 0;; ++s) {
+                const NsShape &h = p.s[s];
+                const int32_t tiles = apply ? h.tiles3 : f.n * h.square, mine = here(s) * tiles;
+                if (r >= mine) { r -= mine; continue; }
+                const int32_t m = r / tiles, matrix = group * h.group + m;
+                int32_t t = r - m * tiles, row, col, which = 0;
+                if (apply) {
+                    row = t / h.cols3;
+                    col = t - row * h.cols3;
                 } else {
+                    if (t >= h.square) { t -= h.square; which = 1; }
                     for (row = 0; t > row; ++row) t -= row + 1;
                     col = t;
                 }
-                const int32_t matrix = group * p.s[s].group + m;
-                return make_int4(matrix, s << 16 | step << 2 | product, row << 16 | col, matrix % p.s[s].slots);
+                tiles_before = squares_before * h.square + segment * h.tiles3;
+                const NsOp &o = f.op[which];
+                return make_int4(matrix, s << 16 | segment << 11 | o.kind << 9 | o.a << 6 | o.b << 3 | o.out, row << 16 | col, matrix % h.slots);
             }
+        }
+    }
+    __device__ __forceinline__ int32_t tiles_of(const NsShape &h) const {  // of a matrix, in all
+        const int32_t rest = p.steps % p.together;
+        return (full() * programs[p.together].squares + (rest ? programs[rest].squares : 0)) * h.square + (full() + (rest > 0)) * h.tiles3;
     }
 };
 __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
@@ -153,7 +201,7 @@ template <bool PAIR> struct NsRing {
             else mbar_arrive(empty);
         }
         ++i;
-        t.matrix = a.x; t.shape = a.y >> 16; t.step = a.y >> 2 & 0x3fff; t.product = a.y & 3;
+        t.matrix = a.x; t.shape = a.y >> 16; t.segment = a.y >> 11 & 31; t.kind = a.y >> 9 & 3; t.a = a.y >> 6 & 7; t.b = a.y >> 3 & 7; t.out = a.y & 7;
         t.row = (a.z >> 16) * tile_side<PAIR>(); t.col = (a.z & 0xffff) * tile_side<PAIR>(); t.slot = a.w;
         return a.x >= 0;
     }
@@ -215,7 +263,7 @@ __device__ __forceinline__ void step_box(int32_t cols, const MuonEntry &e, int64
 }
 
 // What a result is, besides the accumulator
-enum Result { K_FIRST, K_SECOND, K_THIRD, K_LAST };
+enum Result { K_FIRST, K_SECOND, K_MULT, K_THIRD, K_LAST };
 // 32 columns of 32 rows, a row a lane. old: 32 halves of the operand that is added, times what the diagonals make of it: `of_row`, and of the columns `cols` (shared memory). See factor_of
 template <int KIND, bool COLS>
 __device__ __forceinline__ void finish(float2 (&v)[16], const uint32_t *old, float of_row, const float *cols) {
@@ -234,12 +282,14 @@ __device__ __forceinline__ void finish(float2 (&v)[16], const uint32_t *old, flo
                 float2 f = j ? make_float2(c.z, c.w) : make_float2(c.x, c.y);
                 if constexpr (KIND == K_SECOND) f = fma2(f, both(1.0f), both(of_row));
                 const float2 o = __half22float2(*reinterpret_cast<const __half2 *>(old + 2 * q + j));
-                y = fma2(y, both(by), mul2(o, f));
+                float2 more = mul2(o, f);
+                if constexpr (KIND == K_MULT) more = fma2(__half22float2(*reinterpret_cast<const __half2 *>(old + 16 + 2 * q + j)), both(of_row), more);
+                y = fma2(y, both(by), more);
             }
         }
     }
 }
-// c (d_i + d_j) + b of A' for B, r of X for X; the last X is wanted without MUON_UNIT
+// c (d_i + d_j) + b of A' for P; in a product of two the columns' go with the first and the row's with the second; of X; the last X is wanted without MUON_UNIT
 template <int KIND> __device__ __forceinline__ float factor_of(float diagonal, bool column) {
     return KIND == K_SECOND ? fmaf(NS_C, diagonal, column ? NS_B : 0.0f) : KIND == K_LAST ? diagonal * (1.0f / MUON_UNIT) : diagonal;
 }
@@ -302,10 +352,10 @@ struct BoxWork {
     uint32_t accumulator;   // in tensor memory
     uint8_t *boxes;
     float *factors;
-    const __half *from;
+    const __half *from, *from_b;  // (from_b: K_MULT)
     const float *of_cols;
-    float *diagonal;        // K_FIRST: d, K_SECOND: r
-    float of_row;
+    float *diagonal;        // of the result
+    float of_row, of_row_b;       // (of_row_b: K_MULT)
     int32_t row0, first, boxes_n, M;
     bool in;                // this lane's row exists
     uint32_t box_empty0, box_ready0, box_parity;
@@ -313,18 +363,23 @@ struct BoxWork {
     int32_t *status;
 };
 // The operand's 32 halves of this lane's row, and the diagonal's element of a column a lane, from a box' first column on
-template <int KIND, bool COLS> __device__ __forceinline__ void fetch_half(const BoxWork &b, int32_t at, int lane, uint32_t (&old)[16], float &of_col) {
+template <int KIND> constexpr int old_words() { return KIND == K_MULT ? 32 : 16; }  // (of two operands)
+template <int KIND, bool COLS> __device__ __forceinline__ void fetch_half(const BoxWork &b, int32_t at, int lane, uint32_t (&old)[old_words<KIND>()], float &of_col) {
     if constexpr (KIND != K_FIRST)
         if (b.in) {
             load_32B(b.from + at, old);
             load_32B(b.from + at + 16, old + 8);
+            if constexpr (KIND == K_MULT) {
+                load_32B(b.from_b + at, old + 16);
+                load_32B(b.from_b + at + 16, old + 24);
+            }
         }
     if constexpr (COLS)
         if (b.first + at + lane < b.M) of_col = __ldcg(b.of_cols + b.first + at + lane);
 }
-// Half a box, 32 columns. The next box' half of the operand is asked for as soon as this one's is used up
+// Half a box, 32 columns. The next box' half of the operand (of two operands: the next half) is asked for as soon as this one's is used up
 template <int KIND, bool COLS, bool ROWS, int J, typename Last>
-__device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, float lr, const uint32_t (&raw)[32], uint32_t (&old)[16], float &of_col, RowOfWeights &weights, int32_t weights_end,
+__device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, float lr, const uint32_t (&raw)[32], uint32_t (&old)[old_words<KIND>()], float &of_col, RowOfWeights &weights, int32_t weights_end,
                                           Last onto_weights) {
     const int32_t col = b.first + 64 * u + 32 * J;
     uint8_t *box = b.boxes + u * 4 * BOX;
@@ -336,7 +391,7 @@ __device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, flo
     float2 v[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
-    if (KIND <= K_SECOND && col == b.row0) {  // the diagonal: kept in float; no part of the operand (and A' has a zero here)
+    if (KIND <= K_MULT && col == b.row0) {  // the diagonal: kept in float; no part of the operand (and A' has a zero here)
         float own = 0.0f;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -344,10 +399,12 @@ __device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, flo
             if (i == lane) { own = e; e = 0.0f; }
         }
         own *= 1.0f / (MUON_UNIT * MUON_UNIT);
-        if (b.row0 + lane < b.M) b.diagonal[b.row0 + lane] = KIND == K_FIRST ? own : fmaf(NS_C, fmaf(b.of_row, b.of_row, own), fmaf(NS_B, b.of_row, NS_A));
+        if (b.row0 + lane < b.M) b.diagonal[b.row0 + lane] = KIND == K_FIRST ? own : KIND == K_MULT ? fmaf(b.of_row, b.of_row_b, own) : fmaf(NS_C, fmaf(b.of_row, b.of_row, own), fmaf(NS_B, b.of_row, NS_A));
     }
     finish<KIND, COLS>(v, old, factor_of<KIND>(b.of_row, false), b.factors);
-    if (u + 1 < b.boxes_n) fetch_half<KIND, COLS>(b, 64 + 32 * J, lane, old, of_col);
+    if constexpr (KIND == K_MULT) {
+        if (J == 0 || u + 1 < b.boxes_n) fetch_half<KIND, COLS>(b, 64 * u + 32 * J + 32, lane, old, of_col);
+    } else if (u + 1 < b.boxes_n) fetch_half<KIND, COLS>(b, 64 + 32 * J, lane, old, of_col);
     if constexpr (KIND != K_LAST) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -377,13 +434,15 @@ __device__ __forceinline__ void make_half(const BoxWork &b, int u, int lane, flo
 // ROWS: the weights row by row (K_LAST), else by `onto_weights` through shared memory
 template <int KIND, bool COLS, bool ROWS, typename Wait, typename Release, typename Last>
 __device__ __forceinline__ bool make_boxes(const BoxWork &b, int lane, float lr, RowOfWeights &weights, int32_t weights_end, Wait wait_accumulator, Release release, Last onto_weights) {
-    uint32_t old0[16], old1[16];
+    constexpr int OLD = old_words<KIND>();
+    constexpr bool HALVES = KIND == K_LAST || KIND == K_MULT;  // no registers for both halves of a box' accumulators: beside the weights, beside two operands
+    uint32_t old0[OLD], old1[OLD];
     float of_col0 = 0.0f, of_col1 = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) old0[i] = old1[i] = 0u;
+    for (int i = 0; i < OLD; ++i) old0[i] = old1[i] = 0u;
     if (b.boxes_n > 0) {  // (on their way while the products run)
         fetch_half<KIND, COLS>(b, 0, lane, old0, of_col0);
-        fetch_half<KIND, COLS>(b, 32, lane, old1, of_col1);
+        if constexpr (KIND != K_MULT) fetch_half<KIND, COLS>(b, 32, lane, old1, of_col1);
         if constexpr (ROWS) weights.load(b.first, b.in && b.first < weights_end);
     }
     bool ok = wait_accumulator();
@@ -395,16 +454,17 @@ __device__ __forceinline__ bool make_boxes(const BoxWork &b, int lane, float lr,
         if (ok && u < b.boxes_n) {
             uint32_t raw0[32], raw1[32];
             tc_ld_32x32(b.accumulator + 64 * u, raw0);
-            if constexpr (KIND != K_LAST) tc_ld_32x32(b.accumulator + 64 * u + 32, raw1);  // (beside the weights there are no registers for both)
+            if constexpr (!HALVES) tc_ld_32x32(b.accumulator + 64 * u + 32, raw1);
             tc_ld_wait();
-            if (KIND != K_LAST && u + 1 == b.boxes_n) release();
+            if (!HALVES && u + 1 == b.boxes_n) release();
             make_half<KIND, COLS, ROWS, 0>(b, u, lane, lr, raw0, old0, of_col0, weights, weights_end, onto_weights);
-            if constexpr (KIND == K_LAST) {
+            if constexpr (HALVES) {
                 tc_ld_32x32(b.accumulator + 64 * u + 32, raw1);
                 tc_ld_wait();
                 if (u + 1 == b.boxes_n) release();
             }
-            make_half<KIND, COLS, ROWS, 1>(b, u, lane, lr, raw1, old1, of_col1, weights, weights_end, onto_weights);
+            if constexpr (KIND == K_MULT) make_half<KIND, COLS, ROWS, 1>(b, u, lane, lr, raw1, old0, of_col0, weights, weights_end, onto_weights);
+            else make_half<KIND, COLS, ROWS, 1>(b, u, lane, lr, raw1, old1, of_col1, weights, weights_end, onto_weights);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(b.box_ready0 + 8u * u);
@@ -454,20 +514,22 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
     const uint32_t tmem_base = *tmem_slot;
     wait_previous_kernel();
 
-    auto kblocks_of = [&](const NsShape &s, const NsTile &t) { return ((t.product == FIRST ? (s.left ? s.cols : s.rows) : s.M) + BK - 1) / BK; };
+    auto kblocks_of = [&](const NsShape &s, const NsTile &t) { return ((t.kind == GRAM ? (s.left ? s.cols : s.rows) : s.M) + BK - 1) / BK; };
     // columns that exist of a tile's output, and of the product (both CTAs' halves of B's operand begin at multiples of 64)
-    auto cols_out = [&](const NsShape &s, const NsTile &t) { return t.product == THIRD ? s.ld : s.Mld; };
+    auto cols_out = [&](const NsShape &s, const NsTile &t) { return t.kind == APPLY ? s.ld : s.Mld; };
+    auto rows_out = [&](const NsShape &s, const NsTile &t) { return t.kind == APPLY ? s.rows : s.M; };
     auto width_of = [&](const NsShape &s, const NsTile &t) { return PAIR && cols_out(s, t) - t.col > 128 ? 256 : 128; };
+    auto is_last = [&](const NsTile &t) { return t.kind == APPLY && (t.segment + 1) * p.together >= p.steps; };
     // Where an operand lies in a product whose contraction runs along the shorter side: block kb of it is in the lower half for rows from `at` on, or has to be transposed
     auto upper = [&](int kb, int32_t at) { return kb * BK / SIDE > at / SIDE; };
-    auto a_is_mn = [&](const NsShape &s, const NsTile &t, int kb) { return t.product == FIRST ? !s.left : t.product == THIRD && !s.left ? false : upper(kb, t.row); };
-    auto b_is_mn = [&](const NsShape &s, const NsTile &t, int kb) { return t.product == FIRST ? !s.left : t.product == THIRD && s.left ? true : upper(kb, t.col); };
+    auto a_is_mn = [&](const NsShape &s, const NsTile &t, int kb) { return t.kind == GRAM ? !s.left : t.kind == APPLY && !s.left ? false : upper(kb, t.row); };
+    auto b_is_mn = [&](const NsShape &s, const NsTile &t, int kb) { return t.kind == GRAM ? !s.left : t.kind == APPLY && s.left ? true : upper(kb, t.col); };
     // a warp's boxes of a tile: the rows, the first column and how many there are
     auto boxes_of = [&](const NsShape &s, const NsTile &t, int w, int32_t &row0, int32_t &first) {
         const int32_t width = width_of(s, t);
         row0 = t.row + 128 * (int)rank + 32 * ((w + 2) & 3);  // (epilogue warps are warps 2 to 9, and their quarter of the accumulator's rows is warp % 4)
         first = t.col + (w >> 2) * (width / 2);
-        return row0 < (t.product == THIRD ? s.rows : s.M) ? max(0, min(width / 128, (cols_out(s, t) - first) / 64)) : 0;
+        return row0 < rows_out(s, t) ? max(0, min(width / 128, (cols_out(s, t) - first) / 64)) : 0;
     };
     auto gave_up = [&]() {  // copies in flight have landed long before a millisecond is over, and only then may the CTA exit
         for (const unsigned long long t0 = global_ns(); global_ns() - t0 < 1000000ull;) {}
@@ -484,10 +546,10 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             while (ok && tiles.next(t)) {
                 const NsShape &h = p.s[t.shape];
                 const NsMaps &maps = all_maps.m[t.shape];
-                const int slot = t.slot, x = t.step & 1, xm = x ? slot : t.matrix;
-                const bool a_x = t.product == FIRST || (t.product == THIRD && !h.left), b_x = t.product == FIRST || (t.product == THIRD && h.left);
-                const CUtensorMap *sym_k = t.product == SECOND ? &maps.a_k : &maps.b_k, *sym_mn = t.product == SECOND ? &maps.a_mn : &maps.b_mn;
-                const CUtensorMap *ak = a_x ? &maps.x_k[x] : sym_k, *an = a_x ? &maps.x_mn[x] : sym_mn, *bk = b_x ? &maps.x_k[x] : sym_k, *bn = b_x ? &maps.x_mn[x] : sym_mn;
+                const int slot = t.slot, x = t.segment & 1, xm = x ? slot : t.matrix;
+                const bool a_x = t.kind == GRAM || (t.kind == APPLY && !h.left), b_x = t.kind == GRAM || (t.kind == APPLY && h.left);
+                const int sb = t.kind == APPLY ? t.a : t.b;  // (X B: the symmetric one is the second)
+                const CUtensorMap *ak = a_x ? &maps.x_k[x] : &maps.s_k[t.a], *an = a_x ? &maps.x_mn[x] : &maps.s_mn[t.a], *bk = b_x ? &maps.x_k[x] : &maps.s_k[sb], *bn = b_x ? &maps.x_mn[x] : &maps.s_mn[sb];
                 const int am = a_x ? xm : slot, bm = b_x ? xm : slot;
                 const int a0 = t.row + 128 * (int)rank, b0 = t.col + (PAIR ? width_of(h, t) / 2 * (int)rank : 0);
                 const int kblocks = kblocks_of(h, t);
@@ -564,10 +626,10 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                 const int4 a = order.find(atomicAdd(p.next, 1));
                 if (a.x >= 0) {  // handed out when what it reads is there: then nobody else has to look
                     const NsShape &h = p.s[a.y >> 16];
-                    const int32_t *count = p.done + h.first + a.x, step = a.y >> 2 & 0x3fff, product = a.y & 3, each = 2 * h.square + h.tiles3;
-                    bool ok = wait_count(count, arrivals<PAIR>() * (step * each + product * h.square), abort_flag, p.status);
-                    if (ok && step == 0 && product == FIRST && a.x >= h.slots)  // and the slot's last user has read what is overwritten now
-                        ok = wait_count(count - h.slots, arrivals<PAIR>() * p.steps * each, abort_flag, p.status);
+                    const int32_t *count = p.done + h.first + a.x;
+                    bool ok = wait_count(count, arrivals<PAIR>() * order.tiles_before, abort_flag, p.status);
+                    if (ok && order.tiles_before == 0 && a.x >= h.slots)  // and the slot's last user has read what is overwritten now
+                        ok = wait_count(count - h.slots, arrivals<PAIR>() * order.tiles_of(h), abort_flag, p.status);
                     if (!ok) break;
                     fence_async();  // what other SMs' copies have stored, before copies read it
                 }
@@ -588,12 +650,12 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             while (ok && tiles.next(t)) {
                 const NsShape &h = p.s[t.shape];
                 const NsMaps &maps = all_maps.m[t.shape];
-                const bool last = t.product == THIRD && t.step + 1 == p.steps;
-                const int to = (t.step & 1) ^ 1;  // of X
-                const CUtensorMap *out = t.product == FIRST ? &maps.a_k : t.product == SECOND ? &maps.b_k : &maps.x_k[to];
-                const int matrix = t.product == THIRD && !to ? t.matrix : t.slot;
+                const bool last = is_last(t);
+                const int to = (t.segment & 1) ^ 1;  // of X
+                const CUtensorMap *out = t.kind == APPLY ? &maps.x_k[to] : &maps.s_k[t.out];
+                const int matrix = t.kind == APPLY && !to ? t.matrix : t.slot;
                 const int32_t row0 = t.row + 128 * (int)rank, cols = cols_out(h, t), width = width_of(h, t);
-                const bool here = row0 < (t.product == THIRD ? h.rows : h.M);
+                const bool here = row0 < rows_out(h, t);
                 for (int u = 0; u < 2 && ok; ++u) {
                     ok = short_wait(box_ready0 + 8u * u, ph, abort_flag, p.status);
                     if (!ok) break;
@@ -634,19 +696,21 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             BoxWork b;
             b.boxes_n = boxes_of(h, t, w, b.row0, b.first);
             const int32_t row = b.row0 + lane;
-            const int slot = t.slot, x = t.step & 1;
-            const bool last = t.product == THIRD && t.step + 1 == p.steps;
-            float *d = h.d + (int64_t)slot * h.M, *r = h.r + (int64_t)slot * h.M;
+            const int slot = t.slot, x = t.segment & 1;
+            const bool last = is_last(t);
+            auto diagonal_of = [&](int s) { return h.d + ((int64_t)s * h.slots + slot) * h.M; };
+            auto symmetric_at = [&](int s) { return h.s[s] + ((int64_t)slot * h.M + row) * h.Mld + b.first; };
             b.boxes = boxes_at; b.factors = factors; b.M = h.M;
             b.box_empty0 = box_empty0; b.box_ready0 = box_ready0; b.box_parity = box_ph ^ 1u;
             b.abort_flag = abort_flag; b.status = p.status;
-            b.diagonal = t.product == FIRST ? d : r;
-            // What the result is added to: A' or X as it was, and the diagonals' elements of this lane's row and of its columns
-            b.from = t.product == SECOND ? h.a + ((int64_t)slot * h.M + row) * h.Mld + b.first : h.x[x] + ((int64_t)(x ? slot : t.matrix) * h.rows + row) * h.ld + b.first;
-            b.in = row < (t.product == SECOND ? h.M : h.rows);
-            b.of_cols = t.product == SECOND ? d : r;
-            b.of_row = 0.0f;
-            if (t.product != FIRST && row < h.M && (t.product == SECOND || h.left)) b.of_row = __ldcg((t.product == SECOND ? d : r) + row);
+            b.diagonal = diagonal_of(t.out);
+            // What the result is added to: the operands or X as it was, and the diagonals' elements of this lane's row and of its columns
+            b.from = t.kind == APPLY ? h.x[x] + ((int64_t)(x ? slot : t.matrix) * h.rows + row) * h.ld + b.first : symmetric_at(t.a);
+            b.from_b = symmetric_at(t.b);
+            b.in = row < rows_out(h, t);
+            b.of_cols = diagonal_of(t.kind == MULT ? t.b : t.a);
+            b.of_row = t.kind != GRAM && row < h.M && (t.kind != APPLY || h.left) ? __ldcg(diagonal_of(t.a) + row) : 0.0f;
+            b.of_row_b = t.kind == MULT && row < h.M ? __ldcg(diagonal_of(t.b) + row) : 0.0f;
             auto wait_accumulator = [&]() {
                 const bool full = __all_sync(0xffffffffu, short_wait(tfull_bar(acc), acc_ph, abort_flag, p.status));
                 tc_fence_after();
@@ -687,8 +751,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             };
             using Yes = std::true_type;
             using No = std::false_type;
-            if (t.product == FIRST) ok = make(std::integral_constant<int, K_FIRST>(), No(), No());
-            else if (t.product == SECOND) ok = make(std::integral_constant<int, K_SECOND>(), Yes(), No());
+            if (t.kind == GRAM) ok = make(std::integral_constant<int, K_FIRST>(), No(), No());
+            else if (t.kind == POLY) ok = make(std::integral_constant<int, K_SECOND>(), Yes(), No());
+            else if (t.kind == MULT) ok = make(std::integral_constant<int, K_MULT>(), Yes(), No());
             else if (!last) ok = h.left ? make(std::integral_constant<int, K_THIRD>(), No(), No()) : make(std::integral_constant<int, K_THIRD>(), Yes(), No());
             else if (h.cols % 32 == 0) ok = h.left ? make(std::integral_constant<int, K_LAST>(), No(), Yes()) : make(std::integral_constant<int, K_LAST>(), Yes(), Yes());
             else ok = h.left ? make(std::integral_constant<int, K_LAST>(), No(), No()) : make(std::integral_constant<int, K_LAST>(), Yes(), No());
@@ -708,7 +773,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
 }
 
 // ------------------------------------------------------------------------------------------ host
-constexpr int64_t GROUP_TILES = 222;  // of A in a group, on SM pairs (74): three for each; twice as many on single SMs
+// Tiles of A in a group, on SM pairs (74): two for each, twice as many on single SMs. A pair with one has to wait for others' tiles (256 of 512 x 1024, graph replay: 4911 us with 74, 4455 with
+// 111, 4335 with 148), more only take workspace (4287 with 222, 4377 with 296; 32 of 1024 x 4096: 4312, 4122, 3954, 4050, 4019).
+constexpr int64_t GROUP_TILES = 148;
 void tiles_of(int32_t rows, int32_t cols, bool pair, NsShape *s) {
     const int side = pair ? 256 : 128;
     const int64_t edge = cdiv(imin(rows, cols), side);
@@ -725,9 +792,26 @@ int64_t groups_of(const MuonBatch &b, bool pair) {
     }
     return imax(1, square / (pair ? GROUP_TILES : 2 * GROUP_TILES));
 }
-struct NsScratch { __half *x, *a, *b; };
+// How many steps a segment has: what makes the fewest 64-deep blocks of products
+int32_t together_of(const MuonBatch &b, int32_t steps, bool pair) {
+    int32_t best = 1;
+    int64_t least = 0;
+    for (int32_t n = 1; n <= MOST_TOGETHER; ++n) {
+        int64_t work = 0;
+        for (int i = 0; i < b.shapes; ++i) {
+            NsShape s;
+            tiles_of(b.s[i].rows, b.s[i].cols, pair, &s);
+            const int64_t M = cdiv(imin(b.s[i].rows, b.s[i].cols), BK), N = cdiv(imax(b.s[i].rows, b.s[i].cols), BK);
+            const auto segment = [&](int32_t k) { return k ? s.square * (N + (programs_host[k].squares - 1) * M) + s.tiles3 * M : 0; };
+            work += b.s[i].matrices * (steps / n * segment(n) + segment(steps % n));
+        }
+        if (n == 1 || work < least) { best = n; least = work; }
+    }
+    return best;
+}
+struct NsScratch { __half *x, *s[SYMMETRIC]; };
 // Everything about a shape but its place in memory, and with scratch that too
-NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, Carver &cv, NsScratch *at) {
+NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, int32_t together, Carver &cv, NsScratch *at) {
     NsShape s = {};
     tiles_of(m.rows, m.cols, pair, &s);
     s.rows = m.rows; s.cols = m.cols; s.ld = m.ld;
@@ -737,11 +821,9 @@ NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, Carver &cv, NsSc
     s.group = (int32_t)cdiv(m.matrices, groups);
     s.slots = (int32_t)imin(m.matrices, 2 * (int64_t)s.group);  // a group's begin while the last one's end
     at->x = cv.take<__half>((int64_t)s.slots * s.rows * s.ld);
-    at->a = cv.take<__half>((int64_t)s.slots * s.M * s.Mld);
-    at->b = cv.take<__half>((int64_t)s.slots * s.M * s.Mld);
-    s.d = cv.take<float>((int64_t)s.slots * s.M);
-    s.r = cv.take<float>((int64_t)s.slots * s.M);
-    s.x[0] = m.x; s.x[1] = at->x; s.a = at->a;
+    for (int i = 0; i < symmetric_of(together); ++i) s.s[i] = at->s[i] = cv.take<__half>((int64_t)s.slots * s.M * s.Mld);
+    s.d = cv.take<float>((int64_t)symmetric_of(together) * s.slots * s.M);
+    s.x[0] = m.x; s.x[1] = at->x;
     return s;
 }
 // [count][rows][ld] halves: boxes of 64 columns x 128 rows (of stores too), and of 64 rows x two pieces of 64 columns
@@ -791,8 +873,10 @@ int64_t ns_tiles(int32_t rows, int32_t cols, bool pair) {
 int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair) {
     Carver cv(nullptr);
     const int64_t groups = groups_of(batch, pair);
+    int32_t together = 1;  // whatever the number of steps: a segment that pays among more pays alone
+    for (int32_t steps = 2; steps <= MOST_TOGETHER; ++steps) together = (int32_t)imax(together, together_of(batch, steps, pair));
     NsScratch at;
-    for (int i = 0; i < batch.shapes; ++i) shape_of(batch.s[i], pair, groups, cv, &at);
+    for (int i = 0; i < batch.shapes; ++i) shape_of(batch.s[i], pair, groups, together, cv, &at);
     return (int64_t)cv.off;
 }
 
@@ -803,17 +887,17 @@ int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st) {
     NsAllMaps maps;
     NsArgs p = {};
     int64_t total = 0;
-    p.shapes = b.shapes; p.steps = w.steps;
+    p.shapes = b.shapes; p.steps = w.steps; p.together = together_of(b, w.steps, w.pair);
     for (int i = 0; i < b.shapes; ++i) {
         NsScratch at;
         NsShape &s = p.s[i];
         NsMaps &m = maps.m[i];
-        s = shape_of(b.s[i], w.pair, groups, cv, &at);
+        s = shape_of(b.s[i], w.pair, groups, p.together, cv, &at);
         MOE_TRY(maps_of(b.s[i].x, s.matrices, s.rows, s.ld, &m.x_k[0], &m.x_mn[0]));
         MOE_TRY(maps_of(at.x, s.slots, s.rows, s.ld, &m.x_k[1], &m.x_mn[1]));
-        MOE_TRY(maps_of(at.a, s.slots, s.M, s.Mld, &m.a_k, &m.a_mn));
-        MOE_TRY(maps_of(at.b, s.slots, s.M, s.Mld, &m.b_k, &m.b_mn));
-        total += (int64_t)s.matrices * w.steps * (2 * (int64_t)s.square + s.tiles3);
+        for (int j = 0; j < symmetric_of(p.together); ++j) MOE_TRY(maps_of(at.s[j], s.slots, s.M, s.Mld, &m.s_k[j], &m.s_mn[j]));
+        const int32_t rest = w.steps % p.together;
+        total += s.matrices * (w.steps / p.together * (programs_host[p.together].squares * (int64_t)s.square + s.tiles3) + (rest ? programs_host[rest].squares * (int64_t)s.square + s.tiles3 : 0));
         p.groups = (int32_t)imax(p.groups, cdiv(s.matrices, s.group));
     }
     if (total > (int64_t)1 << 30) return MOE_ERR_UNSUPPORTED;

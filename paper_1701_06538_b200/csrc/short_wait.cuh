@@ -14,8 +14,8 @@ __device__ __forceinline__ bool short_wait(uint32_t bar, uint32_t parity, volati
     return mbar_wait(bar, parity, abort_flag, status);
 }
 
-// tc_mma_bf16, tc_mma2_bf16, tc_commit and tc_commit2 for all lanes of a warp together, one of which (always the same) does it: what the instructions want in uniform registers is then
-// computed there. In a branch of one lane every product is preceded by moves into them, 170 cycles each where the tensor core needs 40 to 128.
+// tc_mma_bf16, tc_mma2_bf16, tc_commit and tc_commit2 for all lanes of a warp together, one of which (always the same, so that a commit is of this warp's products) does it: the loop
+// around them stays without branches of single lanes.
 __device__ __forceinline__ void warp_mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n .reg .pred p, q;\n elect.sync _|q, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
