@@ -30,7 +30,10 @@ struct Scratch {
     double *z;         // [chunks] sums of lse^2
     double *balance;   // [SUM_BLOCKS]
 };
-int64_t rows_of_chunk(int64_t T) { return imax(32, cdiv(cdiv(T, ROW_BLOCKS), 32) * 32); }
+// Tokens of a block, a multiple of the most rows that a warp has at a time. (Multiples of 32: 477 x 376 of 324 sequences 47 us instead of 21, one after the other in 15 blocks; 4190 x 1276 39 instead
+// of 30; 20000 x 512 33 instead of 32. Of 8: 477 x 376 25 us.)
+constexpr int64_t CHUNK_ROWS = 4;
+int64_t rows_of_chunk(int64_t T) { return cdiv(cdiv(imax(T, 1), ROW_BLOCKS), CHUNK_ROWS) * CHUNK_ROWS; }
 int64_t chunks_of(int64_t T) { return cdiv(imax(T, 1), rows_of_chunk(T)); }
 Scratch scratch_at(Carver &cv, int64_t T, int32_t n, int32_t S) {
     Scratch s;
