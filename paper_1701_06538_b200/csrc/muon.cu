@@ -95,10 +95,12 @@ __device__ __forceinline__ void normalise_block(const MuonEntry &t, const MuonSh
 __global__ void __launch_bounds__(THREADS) muon_normalise_kernel(const __grid_constant__ MuonBatch b, const MuonPasses k) {
     __shared__ double sh[WARPS];
     wait_previous_kernel();
+    // Backwards: what the first pass has touched last is in L2 still, and so is what the products read first
+    const int32_t id = (int32_t)(gridDim.x - 1 - blockIdx.x);
     int q = 0;
-    while (q + 1 < b.shapes && (int32_t)blockIdx.x >= b.s[q + 1].blocks_before) ++q;
+    while (q + 1 < b.shapes && id >= b.s[q + 1].blocks_before) ++q;
     const MuonShape &s = b.s[q];
-    const int32_t here = (int32_t)blockIdx.x - s.blocks_before, in_shape = here / s.blocks, block = here - in_shape * s.blocks, matrix = s.first + in_shape;
+    const int32_t here = id - s.blocks_before, in_shape = here / s.blocks, block = here - in_shape * s.blocks, matrix = s.first + in_shape;
     double v = 0.0;
     for (int32_t c = threadIdx.x; c < s.chunks; c += THREADS) v += k.part[s.chunks_before + (int64_t)in_shape * s.chunks + c];
     v = sqrt(sum_of_block(v, sh)) + (double)k.eps;
