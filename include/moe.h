@@ -533,7 +533,7 @@ int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe
  * The products' operands are X, X X', the polynomials and products of these in fp16, scaled so that nothing overflows, with sums in float: X is off by 7e-4 of itself (root mean square; 2e-3 where few
  * directions hold most of u) for u of any size; what u holds in directions below 2^-12 of its largest is lost in that. g and m may be as large as 2^60 or so: a matrix with a larger or no finite element in u becomes NaN as a whole. A matrix whose u is zero
  * keeps its weights but for the decay.
- * All pointers but host_tensors, host_params are device pointers; w, g, m, master on 32-byte boundaries. The list is read before the call returns; tensors of a list may not overlap.
+ * All pointers but host_tensors, host_params are device pointers; w, g, m, master on 16-byte boundaries. The list is read before the call returns; tensors of a list may not overlap.
  * Matrices are taken together from whatever tensors of the list: a list of a model's layers is three launches, more for more than six shapes, 128 tensors or
  * 1 GiB of X; matrices of up to 128 x 768 take one launch of their own, where they are not a small part of a list of larger ones.
  * rates: NULL, or a moe_muon_rates in device memory that takes the place of lr and grad_scale when the kernels run, for recorded graphs.

@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(THREADS) muon_normalise_kernel(const __grid_co
     else normalise_block<false>(b.t[i], s, first, x, begin, grad_scale, by, k);
 }
 
+bool starts_at(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 int32_t check_tensor(const moe_muon_tensor &t) {
     if (t.count < 0 || t.count > (int64_t)1 << 24 || t.rows <= 0 || t.cols <= 0 || t.rows > MOE_MUON_MAX_SIDE || t.cols > MOE_MUON_MAX_SIDE) return MOE_ERR_INVALID_ARG;
     for (int32_t type : {t.w_type, t.g_type, t.m_type})
@@ -123,8 +124,8 @@ int32_t check_tensor(const moe_muon_tensor &t) {
     if (t.count == 0) return MOE_OK;
     const void *all[] = {t.w, t.g, t.m};
     for (const void *p : all)
-        if (!p || !aligned16(p)) return MOE_ERR_INVALID_ARG;
-    if (t.master && (t.w_type != MOE_BF16 || !aligned16(t.master))) return MOE_ERR_INVALID_ARG;
+        if (!p || !starts_at(p, 16)) return MOE_ERR_INVALID_ARG;
+    if (t.master && (t.w_type != MOE_BF16 || !starts_at(t.master, 16))) return MOE_ERR_INVALID_ARG;
     return MOE_OK;
 }
 
@@ -162,7 +163,7 @@ bool fill_batch(const moe_muon_tensor *tensors, const Shape *const *shapes, int 
                 e.w = on(t.w, t.w_type); e.g = on(t.g, t.g_type); e.m = on(t.m, t.m_type);
                 e.master = t.master ? t.master + (a - at) * each : nullptr;
                 e.scale = t.scale; e.decay = t.weight_decay;
-                e.kind = (t.w_type == MOE_BF16 ? 1 : 0) | (t.g_type == MOE_BF16 ? 2 : 0) | (t.m_type == MOE_BF16 ? 4 : 0) | (t.master ? 8 : 0);
+                e.kind = (t.w_type == MOE_BF16 ? 1 : 0) | (t.g_type == MOE_BF16 ? 2 : 0) | (t.m_type == MOE_BF16 ? 4 : 0) | (t.master ? 8 : 0) | (starts_at(t.w, 32) && starts_at(t.master, 32) ? 16 : 0);
                 b->before[b->n + 1] = b->before[b->n] + (int32_t)(z - a);
                 ++b->n;
             }

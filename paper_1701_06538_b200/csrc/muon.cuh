@@ -14,7 +14,7 @@ struct MuonEntry {
     const void *g;
     float *master;
     float scale, decay;
-    int32_t kind;  // bit 0: bf16 weights, 1: bf16 gradients, 2: bf16 momentum, 3: float masters
+    int32_t kind;  // bit 0: bf16 weights, 1: bf16 gradients, 2: bf16 momentum, 3: float masters, 4: weights and masters begin at 32 bytes
 };
 struct MuonShape {
     int32_t rows, cols, ld;      // ld: elements between rows of the operands, zeros behind the columns

@@ -301,7 +301,7 @@ __device__ __forceinline__ void load_32B(const void *from, uint32_t *r) {
 __device__ __forceinline__ void store_32B(void *to, const uint32_t *r) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-// A row's 32 weights, a row a lane, where rows begin at 32 bytes: read while the products run
+// A row's 32 weights, a row a lane, where rows begin at 32 bytes (columns and tensors: slices of a model's layers may begin at 16): read while the products run
 struct RowOfWeights {
     float *floats;   // what the step is taken on: float weights or masters, or nullptr
     bf16 *halves;    // bf16 weights, or nullptr
@@ -760,7 +760,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             else if (t.kind == POLY) ok = make(std::integral_constant<int, K_SECOND>(), Yes(), No());
             else if (t.kind == MULT) ok = make(std::integral_constant<int, K_MULT>(), Yes(), No());
             else if (!last) ok = h.left ? make(std::integral_constant<int, K_THIRD>(), No(), No()) : make(std::integral_constant<int, K_THIRD>(), Yes(), No());
-            else if (h.cols % 32 == 0) ok = h.left ? make(std::integral_constant<int, K_LAST>(), No(), Yes()) : make(std::integral_constant<int, K_LAST>(), Yes(), Yes());
+            else if (h.cols % 32 == 0 && (e.kind & 16)) ok = h.left ? make(std::integral_constant<int, K_LAST>(), No(), Yes()) : make(std::integral_constant<int, K_LAST>(), Yes(), Yes());
             else ok = h.left ? make(std::integral_constant<int, K_LAST>(), No(), No()) : make(std::integral_constant<int, K_LAST>(), Yes(), No());
             box_ph ^= 1u;
             if (++acc == 2) { acc = 0; acc_ph ^= 1u; }

@@ -94,6 +94,27 @@ def test_steps(steps):
     check(before, t, steps=steps, off=OFF * max(1.0, 1.6 ** (steps - 5)))
 
 
+@pytest.mark.parametrize("shape", [(2, 8, 16), (2, 64, 128), (1, 16, 4096), (1, 192, 448), (1, 448, 192)], ids=str)
+@pytest.mark.parametrize("w,g,m,master", [("f32", "f32", "f32", False), ("bf16", "bf16", "bf16", False), ("bf16", "f32", "bf16", True)])
+def test_tensors_at_16_bytes(shape, w, g, m, master):
+    """Slices of a model's layers begin where the layers before end."""
+    t = [tensor(shape, w, g, m, master, seed=5)]
+    whole = {}
+    for q in [q for q, v in t[0].items() if torch.is_tensor(v)]:
+        v = t[0][q]
+        lead = 16 // v.element_size()
+        whole[q] = torch.full((v.numel() + 2 * lead,), 7.0, dtype=v.dtype, device="cuda")
+        whole[q][lead:-lead] = v.reshape(-1)
+        t[0][q] = whole[q][lead:-lead].view(shape)
+        assert t[0][q].data_ptr() % 32 == 16
+    before = copies(t)
+    step(t)
+    check(before, t)
+    for v in whole.values():
+        lead = 16 // v.element_size()
+        assert (v[:lead] == 7.0).all() and (v[-lead:] == 7.0).all()
+
+
 def test_a_models_list():
     """Tensors of several layers, shapes mixed, some of no matrices; what is taken together does not change a result."""
     t = []
