@@ -4,8 +4,10 @@
 //
 // P is a polynomial of A, so that all of them commute and a step's A follows from the one before: (P X)(P X)' = P A P. A segment of up to three steps stays with the M x M matrices
 // (T = P A, A <- P T, Q <- P Q) and touches X twice, for the first A and for X <- Q X. What that costs in 64-deep blocks of products decides (together_of): a step is M^2 N / 2 + M^3 / 2 +
-// M^2 N operations by itself and three together are M^2 N / 2 + 9/2 M^3 + M^2 N, fewer from N = 2 M on. 32 of 1024 x 4096: 5727 -> 3448 us, 16 of 1024 x 2048: 1416 -> 1220, 256 of
-// 512 x 1024: 4196 -> 4103. Four or five steps in one segment would leave fp16's range: Q reaches 3.4445^n.
+// M^2 N operations by itself and three together are M^2 N / 2 + 9/2 M^3 + M^2 N: an eighth fewer from N = 1.7 M or so on. 32 of 1024 x 4096: 5727 -> 3750 us, 16 of 1024 x 2048: 1416 -> 1250,
+// 256 of 512 x 1024: 4196 -> 4060. A shorter segment goes first: small singular values, which rounding of A hurts most, have grown when A is made of X anew. (Five steps, errors of X by their
+// simulation, one by one / 3 and 2 / 2 and 3: 7.5e-4, 1.4e-3, 5.7e-4 for momentum with gradients of 20 to 90 rows; 7e-4, 7e-4, 5e-4 for normal numbers; 3.6e-3, 2.7e-3, 9.9e-3 for singular
+// values spread evenly over two powers of ten.) Four or five steps in one segment would leave fp16's range: Q reaches 3.4445^n.
 //
 // Bound by the tensor cores, which run against the power limit here (990 W; 1965 MHz become 1300 to 1500). All M x M matrices are symmetric: the lower half is made, by tiles, and what
 // reads a tile of the upper half reads the stored one in its place, transposed by the operand's major-ness, which an instruction has of its own.
@@ -104,9 +106,10 @@ template <bool PAIR> struct NsOrder {
             applies += here(s) * p.s[s].tiles3;
         }
     }
-    __device__ __forceinline__ int32_t full() const { return p.steps / p.together; }  // segments of p.together steps; one of the rest may follow
+    __device__ __forceinline__ int32_t full() const { return p.steps / p.together; }  // segments of p.together steps
+    __device__ __forceinline__ int32_t rest() const { return p.steps % p.together; }  // steps of one before them, or 0
     __device__ __forceinline__ int32_t segment_tiles(int steps) const { return steps ? programs[steps].squares * squares + applies : 0; }
-    __device__ __forceinline__ int32_t group_tiles() const { return full() * segment_tiles(p.together) + segment_tiles(p.steps % p.together); }
+    __device__ __forceinline__ int32_t group_tiles() const { return full() * segment_tiles(p.together) + segment_tiles(rest()); }
     __device__ __forceinline__ int4 find(int32_t id) {
         while (group < p.groups && id - base >= group_tiles()) {
             base += group_tiles();
@@ -115,10 +118,17 @@ template <bool PAIR> struct NsOrder {
         }
         if (group >= p.groups) return make_int4(-1, 0, 0, 0);
         int32_t r = id - base;
-        const int32_t each = segment_tiles(p.together), segment = min(r / each, full());
-        r -= segment * each;
-        const NsProgram &g = programs[segment < full() ? p.together : p.steps % p.together];
-        int32_t squares_before = segment * programs[p.together].squares;
+        int32_t segment = 0, squares_before = 0, steps = rest();
+        if (r >= segment_tiles(steps)) {
+            r -= segment_tiles(steps);
+            if (steps) { segment = 1; squares_before = programs[steps].squares; }
+            steps = p.together;
+            const int32_t each = segment_tiles(steps), more = r / each;
+            r -= more * each;
+            segment += more;
+            squares_before += more * programs[steps].squares;
+        }
+        const NsProgram &g = programs[steps];
         for (int phase = 0;; ++phase) {
             const NsPhase &f = g.phase[phase];
             const bool apply = phase == g.n - 1;
@@ -145,8 +155,7 @@ template <bool PAIR> struct NsOrder {
         }
     }
     __device__ __forceinline__ int32_t tiles_of(const NsShape &h) const {  // of a matrix, in all
-        const int32_t rest = p.steps % p.together;
-        return (full() * programs[p.together].squares + (rest ? programs[rest].squares : 0)) * h.square + (full() + (rest > 0)) * h.tiles3;
+        return (full() * programs[p.together].squares + (rest() ? programs[rest()].squares : 0)) * h.square + (full() + (rest() > 0)) * h.tiles3;
     }
 };
 __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
@@ -797,20 +806,21 @@ int64_t groups_of(const MuonBatch &b, bool pair) {
     }
     return imax(1, square / (pair ? GROUP_TILES : 2 * GROUP_TILES));
 }
-// How many steps a segment has: what makes the fewest 64-deep blocks of products
-int32_t together_of(const MuonBatch &b, int32_t steps, bool pair) {
+// How many steps a segment has at most: what makes the fewest 64-deep blocks of products a step, one where that saves less than an eighth (near-square matrices have small singular values,
+// see above: X of 512 x 576 normal numbers is off by 1.5e-3 in segments and by 8e-4 without)
+int32_t together_of(const MuonBatch &b, bool pair) {
     int32_t best = 1;
-    int64_t least = 0;
+    int64_t least = 0, alone = 0;  // blocks of six steps
     for (int32_t n = 1; n <= MOST_TOGETHER; ++n) {
         int64_t work = 0;
         for (int i = 0; i < b.shapes; ++i) {
             NsShape s;
             tiles_of(b.s[i].rows, b.s[i].cols, pair, &s);
             const int64_t M = cdiv(imin(b.s[i].rows, b.s[i].cols), BK), N = cdiv(imax(b.s[i].rows, b.s[i].cols), BK);
-            const auto segment = [&](int32_t k) { return k ? s.square * (N + (programs_host[k].squares - 1) * M) + s.tiles3 * M : 0; };
-            work += b.s[i].matrices * (steps / n * segment(n) + segment(steps % n));
+            work += b.s[i].matrices * (s.square * (N + (programs_host[n].squares - 1) * M) + s.tiles3 * M) * (6 / n);
         }
-        if (n == 1 || work < least) { best = n; least = work; }
+        if (n == 1) least = alone = work;
+        else if (work < least && 8 * work <= 7 * alone) { best = n; least = work; }
     }
     return best;
 }
@@ -878,8 +888,7 @@ int64_t ns_tiles(int32_t rows, int32_t cols, bool pair) {
 int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair) {
     Carver cv(nullptr);
     const int64_t groups = groups_of(batch, pair);
-    int32_t together = 1;  // whatever the number of steps: a segment that pays among more pays alone
-    for (int32_t steps = 2; steps <= MOST_TOGETHER; ++steps) together = (int32_t)imax(together, together_of(batch, steps, pair));
+    const int32_t together = together_of(batch, pair);  // enough for any number of steps
     NsScratch at;
     for (int i = 0; i < batch.shapes; ++i) shape_of(batch.s[i], pair, groups, together, cv, &at);
     return (int64_t)cv.off;
@@ -892,7 +901,7 @@ int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st) {
     NsAllMaps maps;
     NsArgs p = {};
     int64_t total = 0;
-    p.shapes = b.shapes; p.steps = w.steps; p.together = together_of(b, w.steps, w.pair);
+    p.shapes = b.shapes; p.steps = w.steps; p.together = (int32_t)imin(w.steps, together_of(b, w.pair));
     for (int i = 0; i < b.shapes; ++i) {
         NsScratch at;
         NsShape &s = p.s[i];
