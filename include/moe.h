@@ -535,7 +535,7 @@ int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe
  * g and m may be as large as 2^60 or so: a matrix with a larger or no finite element in u becomes NaN as a whole. A matrix whose u is zero keeps its weights but for the decay.
  * All pointers but host_tensors, host_params are device pointers; w, g, m, master on 16-byte boundaries. The list is read before the call returns; tensors of a list may not overlap.
  * Matrices are taken together from whatever tensors of the list: a list of a model's layers is three launches, more for more than six shapes, 128 tensors or
- * 1 GiB of X; matrices of up to 128 x 768 take one launch of their own, where they are not a small part of a list of larger ones.
+ * 1 GiB of X; matrices of up to 128 x 768 and 49152 elements take one launch of their own, where they are not a small part of a list of larger ones.
  * rates: NULL, or a moe_muon_rates in device memory that takes the place of lr and grad_scale when the kernels run, for recorded graphs.
  * ws: moe_muon_workspace_bytes, its own in every call that may run at the same time; 256-byte aligned. MOE_ERR_TIMEOUT in its status word: see moe_check_status.
  * ------------------------------------------------------------------------------------------ */

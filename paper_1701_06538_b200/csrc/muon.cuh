@@ -66,7 +66,7 @@ struct NsWork {
     float lr;
     const moe_muon_rates *rates;  // or nullptr
 };
-static inline bool ns_pairs(int32_t rows, int32_t cols) { return imin(rows, cols) > 128; }  // whether a shape fills tiles of SM pairs
+static inline bool ns_pairs(int32_t rows, int32_t cols) { return imin(rows, cols) > 128; }  // whether a shape takes tiles of SM pairs (768 of 184 x 144: 835 us, by single SMs 1340; 128 of 192 x 448 242 and 342; 64 of 512 x 1024 580 and 712)
 int64_t ns_tiles(int32_t rows, int32_t cols, bool pair);                                   // of a matrix, a step
 int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair);
 int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st);

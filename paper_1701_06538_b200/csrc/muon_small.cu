@@ -1,8 +1,8 @@
-// The whole Muon step of a small matrix, M up to 128 and N up to 768 (the shorter and the longer side), by one block: momentum, norm, all Newton-Schulz products and the weights in one launch. See
+// The whole Muon step of a small matrix, M up to 128, N up to 768 (the shorter and the longer side) and 49152 elements, by one block: momentum, norm, all Newton-Schulz products and the weights in one launch. See
 // newton_schulz.cu for the products, their scaling and their diagonals.
 //
 // Bound by latency: 15 products, each of which needs the one before. X stays in shared memory, A and B in one place of it and accumulators in tensor memory, so that from product to product there
-// is a barrier and not a way through L2 (8 experts of 64 x 128 and their gate by newton_schulz.cu: 80 us).
+// is a barrier and not a way through L2 (8 experts of 64 x 128 and their gate: 31 us, by newton_schulz.cu 89; 40 of 72 x 520: 89 and 151).
 //
 // X is held as [N][128] whichever way the matrix lies, M columns and zeros behind them: 64-column pieces of 128-byte rows, 128-byte swizzle. A = X' X takes it MN-major twice, X B K-major by 128 rows
 // of it at a time, whose accumulators lie beside each other in tensor memory, four at most; X B takes the place of X.
@@ -388,7 +388,10 @@ __global__ void __launch_bounds__(THREADS) muon_small_kernel(const __grid_consta
 
 }  // namespace
 
-bool muon_is_small(int32_t rows, int32_t cols) { return imin(rows, cols) <= 128 && imax(rows, cols) <= MAX_N; }
+// By one block: what its shared memory holds, and no more elements than it has done while tiles of several SMs have (newton_schulz.cu; matrices and their transposes: 16 of 128 x 128 31 us by blocks, 98
+// by tiles, 500 of them 148 and 228; of 128 x 256 95 and 117, 298 and 341; of 96 x 512 119 and 117, 384 and 415; of 64 x 768 138 and 106, 449 and 440; of 128 x 768 259 and 125, 200 of them 398 and 266)
+constexpr int64_t MOST_ELEMENTS = 49152;
+bool muon_is_small(int32_t rows, int32_t cols) { return imin(rows, cols) <= 128 && imax(rows, cols) <= MAX_N && (int64_t)rows * cols <= MOST_ELEMENTS; }
 
 int32_t launch_muon_small(const MuonBatch &b, const MuonPasses &k, float lr, int32_t steps, cudaStream_t st) {
     int64_t longest = 0;

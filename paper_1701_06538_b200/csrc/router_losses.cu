@@ -463,8 +463,8 @@ __global__ void __launch_bounds__(THREADS) router_small_kernel(const RouterLossA
     if (threadIdx.x == 0) put_losses(a, all, balance, w.z[0]);
 }
 
-// One block: as many rows and columns as it has done while a second launch would begin
-constexpr int64_t SMALL = 8192;
+// One block: as many rows and columns as it has done while three launches follow one another (256 x 64 in a recorded graph 9.5 us by one, 13.0 by three; 16 x 1000 10.2 and 15.7; 512 x 64 14.0 and 13.7)
+constexpr int64_t SMALL = 16384;
 bool small(const RouterLossArgs &a) { return a.T * a.n <= SMALL && (int64_t)a.S * a.n <= SMALL && a.n <= 1024 && a.S <= 16; }
 
 template <int LANES, int U, int VEC, int R> int32_t rows(const RouterLossArgs &a, const Scratch &w, cudaStream_t st) {
@@ -503,7 +503,7 @@ int32_t launch_rows(const RouterLossArgs &a, const Scratch &w, cudaStream_t st) 
 
 int32_t launch_counts(const RouterLossArgs &a, const Scratch &w, cudaStream_t st) {
     const size_t bytes = (size_t)(a.n + 1) * sizeof(int32_t);  // at most 32 KiB and a word
-    // blocks for a sequence, so that most SMs have one
+    // blocks for a sequence, so that most SMs have one (one each: 131072 x 128 of one sequence 96 us instead of 41, 32768 x 64 of eight 27.7 instead of 23.5, of 30 21.7 instead of 20.7)
     const int parts = a.S <= 9 ? 16 : a.S <= 18 ? 8 : a.S <= 37 ? 4 : a.S <= 74 ? 2 : 1;
     if (parts == 1) {
         launch_kernel(router_counts_kernel<false>, dim3((unsigned)a.S), dim3(COUNT_THREADS), bytes, st, a, w, Divisor::of(a.k), 1);
@@ -544,7 +544,9 @@ int32_t launch_router_losses(const RouterLossArgs &a, void *ws, cudaStream_t st)
     MOE_TRY(launch_rows(a, w, st));
     if (one) return MOE_OK;
     const int64_t items = (int64_t)a.S * cdiv(a.n, 32), chunk = rows_of_chunk(a.T);
-    const bool blocks = a.T > 4 * chunk * a.S;  // a warp each where a sequence lies in four chunks or fewer
+    // A warp each where a sequence lies in four chunks or fewer for every turn that blocks would take. (131072 x 128, one sequence: blocks 41 us, warps 69; 32768 x 64 of 40: 21 and 24; 32768 x 256
+    // of 61, two turns: 33.9 and 31.0; 8443 x 84 of 118: 20.8 and 19.3)
+    const bool blocks = a.T > 4 * chunk * a.S * cdiv(items, SUM_BLOCKS);
     launch_kernel(blocks ? router_sums_kernel<true> : router_sums_kernel<false>, dim3((unsigned)imin(blocks ? items : cdiv(items, SUM_WARPS), SUM_BLOCKS)), dim3(SUM_WARPS * 32), 0, st, a, w,
                   (int32_t)chunk, (int32_t)chunks_of(a.T));
     MOE_LAUNCHED();
