@@ -511,7 +511,7 @@ int32_t launch_counts(const RouterLossArgs &a, const Scratch &w, cudaStream_t st
         return MOE_OK;
     }
     static PerDevice wide;
-    const bool sixteen = wide.get([]() {
+    const bool sixteen = wide.get([&]() {
         return cudaFuncSetAttribute(reinterpret_cast<const void *>(router_counts_kernel<true>), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess ? 1 : 0;
     }) > 0;
     if (!sixteen) return MOE_ERR_CUDA;
