@@ -393,9 +393,10 @@ Team backward_team(int32_t d, int32_t act) {  // 16 elements of a row a thread, 
 }
 // Rows of a team at a time: two vectors of a row and its gradient are what fits beside the sums of columns (bf16 backward of 65536 x 1024 with two rows of two: 121 us, with one 86)
 constexpr int rows_at_once(int V, bool backward) { return backward ? (V == 1 ? 2 : 1) : V >= 4 ? 1 : 4 / V; }
-// 512 threads an SM: two blocks, three of teams of five warps (7234 x 1160 forward with two 14.5 us, with three 11.6; backward 21.9 and 19.4), one of teams of more than eight
+// 512 threads an SM: two blocks, three of teams of five warps (7234 x 1160 forward with two 14.5 us, with three 11.6; backward 21.9 and 19.4), one of teams of more than eight.
+// Backward of four vectors a thread: two, whose rings of 96 KiB an SM holds
 int64_t blocks_of(int64_t T, const Team &t, bool backward) {
-    return imin(cdiv(T, (int64_t)rows_at_once(t.V, backward) * (t.threads / (32 * t.warps))), 148 * (512 / t.threads));
+    return imin(cdiv(T, (int64_t)rows_at_once(t.V, backward) * (t.threads / (32 * t.warps))), 148 * imin(512 / t.threads, backward && t.V > 2 ? 2 : 3));
 }
 
 template <typename T, int V, int THREADS, bool ONE> int32_t forward(const LayerNormArgs &a, const Team &t, cudaStream_t st) {

@@ -267,7 +267,7 @@ int32_t muon_bytes(const moe_muon_tensor *tensors, int32_t count, int64_t *bytes
 
 int32_t launch_muon(const moe_muon_tensor *tensors, int32_t count, const moe_muon_params &p, const moe_muon_rates *rates, void *ws, cudaStream_t st) {
     bool first = true;
-    return for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
+    MOE_TRY(for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
         const bool pair = how == PAIRS;
         Carver cv(ws);
         int32_t *status = static_cast<int32_t *>(cv.take_bytes(kWsHeader));
@@ -285,7 +285,9 @@ int32_t launch_muon(const moe_muon_tensor *tensors, int32_t count, const moe_muo
         MOE_LAUNCHED();
         const NsWork w = {&b, pair, p.steps, s.done, s.next, status, s.products, (float)p.lr, rates};
         return launch_newton_schulz(w, st);
-    });
+    }));
+    if (first) MOE_CUDA(cudaMemsetAsync(ws, 0, sizeof(int32_t), st));  // no matrices: no launch that clears the status
+    return MOE_OK;
 }
 
 }  // namespace moe
