@@ -538,6 +538,7 @@ int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe
  * 1 GiB of X; matrices of up to 128 x 768 and 49152 elements take one launch of their own, where they are not a small part of a list of larger ones.
  * rates: NULL, or a moe_muon_rates in device memory that takes the place of lr and grad_scale when the kernels run, for recorded graphs.
  * ws: moe_muon_workspace_bytes, its own in every call that may run at the same time; 256-byte aligned. MOE_ERR_TIMEOUT in its status word: see moe_check_status.
+ * A list without matrices launches nothing and leaves the workspace and its status word as they were.
  * ------------------------------------------------------------------------------------------ */
 #define MOE_MUON_MAX_SIDE 32768
 #define MOE_MUON_MAX_STEPS 16

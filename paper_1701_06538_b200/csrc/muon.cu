@@ -17,7 +17,7 @@ namespace moe {
 
 namespace {
 
-constexpr int THREADS = PASS_THREADS, WARPS = THREADS / 32, CHUNK = PASS_CHUNK;
+constexpr int THREADS = PASS_THREADS, WARPS = THREADS / 32, CHUNK = THREADS * EACH * TURNS;  // CHUNK: of the second pass
 constexpr int64_t MOST_X = (int64_t)1 << 30;   // bytes of X of a launch (one matrix at least)
 
 __device__ __forceinline__ double sum_of_block(double v, double *sh) {
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(THREADS) muon_momentum_kernel(const __grid_con
         }
     }
     const int32_t i = b.entry_of(matrix);
-    const int64_t each = (int64_t)s.rows * s.cols, first = (matrix - b.before[i]) * each, at = first + (int64_t)chunk * CHUNK, end = min(at + CHUNK, first + each);
+    const int64_t each = (int64_t)s.rows * s.cols, first = (matrix - b.before[i]) * each, at = first + (int64_t)chunk * PASS_CHUNK, end = min(at + PASS_CHUNK, first + each);
     const float grad_scale = k.rates ? k.rates->grad_scale : k.grad_scale;
     // vectors of eight where every matrix begins at one
     double v = each % EACH == 0 ? momentum_block<true>(b.t[i], at, end, grad_scale, k) : momentum_block<false>(b.t[i], at, end, grad_scale, k);
@@ -147,7 +147,7 @@ bool fill_batch(const moe_muon_tensor *tensors, const Shape *const *shapes, int 
         MuonShape &s = b->s[b->shapes++];
         s.rows = h.rows; s.cols = h.cols; s.ld = (int32_t)muon_ld(h.cols);
         s.first = b->before[b->n]; s.matrices = (int32_t)(to - from);
-        s.chunks = (int32_t)cdiv(each, CHUNK); s.blocks = (int32_t)cdiv((int64_t)s.rows * s.ld, CHUNK);
+        s.chunks = (int32_t)cdiv(each, PASS_CHUNK); s.blocks = (int32_t)cdiv((int64_t)s.rows * s.ld, CHUNK);
         s.chunks_before = (int32_t)chunks; s.blocks_before = (int32_t)blocks;
         s.x = nullptr;
         chunks += (to - from) * s.chunks; blocks += (to - from) * s.blocks;
@@ -267,7 +267,7 @@ int32_t muon_bytes(const moe_muon_tensor *tensors, int32_t count, int64_t *bytes
 
 int32_t launch_muon(const moe_muon_tensor *tensors, int32_t count, const moe_muon_params &p, const moe_muon_rates *rates, void *ws, cudaStream_t st) {
     bool first = true;
-    MOE_TRY(for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
+    return for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
         const bool pair = how == PAIRS;
         Carver cv(ws);
         int32_t *status = static_cast<int32_t *>(cv.take_bytes(kWsHeader));
@@ -285,9 +285,7 @@ int32_t launch_muon(const moe_muon_tensor *tensors, int32_t count, const moe_muo
         MOE_LAUNCHED();
         const NsWork w = {&b, pair, p.steps, s.done, s.next, status, s.products, (float)p.lr, rates};
         return launch_newton_schulz(w, st);
-    }));
-    if (first) MOE_CUDA(cudaMemsetAsync(ws, 0, sizeof(int32_t), st));  // no matrices: no launch that clears the status
-    return MOE_OK;
+    });
 }
 
 }  // namespace moe

@@ -254,10 +254,14 @@ def test_nothing_is_written_outside():
 
 
 def test_lists_without_matrices():
-    step([])
     t = [tensor((0, 8, 16)), tensor((0, 200, 300))]
     before = copies(t)
-    step(t)
+    for tensors in ([], t):
+        L = B.moe_muon_list(tensors)
+        ws = B.empty_bytes(B.moe_muon_workspace_bytes(L))
+        ws.fill_(0xff)
+        B.moe_muon(L, LR, MU, EPS, 5, True, ws)
+        assert bool((ws == 0xff).all())
     assert all(torch.equal(a["w"], b["w"]) for a, b in zip(t, before))
 
 
