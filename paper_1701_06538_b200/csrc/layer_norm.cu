@@ -114,10 +114,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_kernel(const Layer
     const int64_t step = (int64_t)gridDim.x * teams * K;
     int64_t row = ((int64_t)blockIdx.x * teams + threadIdx.x / threads) * K;
     const Places<T, V> at(a.d, lane, threads);
-    float2 w[V][P], b[V][P];
-    load_weights<T, V>(a.w, lane, threads, at, w);
-    load_weights<T, V>(a.b, lane, threads, at, b);
-    wait_previous_kernel();
+    wait_previous_kernel();  // (the weights too may be what the launch before writes: an optimiser's)
     const char *from = static_cast<const char *>(a.x) + at.first + row * at.row_bytes;
     char *to = static_cast<char *>(a.xn) + at.first + row * at.row_bytes;
     const int64_t step_bytes = step * at.row_bytes;
@@ -138,6 +135,9 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_kernel(const Layer
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) fetch(s);
+    float2 w[V][P], b[V][P];  // on their way together with the first rows
+    load_weights<T, V>(a.w, lane, threads, at, w);
+    load_weights<T, V>(a.b, lane, threads, at, b);
     int stage = 0;
     for (; row < a.T; row += step, to += step_bytes) {
         fetch(stage == 0 ? STAGES - 1 : stage - 1);
@@ -211,8 +211,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
     const int64_t step = (int64_t)gridDim.x * teams * K;
     int64_t row = ((int64_t)blockIdx.x * teams + team) * K;
     const Places<T, V> at(a.d, lane, threads);
+    wait_previous_kernel();
     float2 held[HELD ? V : 1][P];
-    if constexpr (HELD) load_weights<T, V>(a.w, lane, threads, at, held);
     auto weights = [&](int v, float2 (&w)[P]) {
         if constexpr (HELD) {
 #pragma unroll
@@ -223,7 +223,6 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
             if (at.in[v]) load_floats(a.w + (int64_t)(lane + v * threads) * N, w);
         }
     };
-    wait_previous_kernel();
     const int64_t offset = at.first + row * at.row_bytes, step_bytes = step * at.row_bytes;
     const char *x_from = static_cast<const char *>(a.x) + offset, *g_from = static_cast<const char *>(a.dxn) + offset, *res_from = static_cast<const char *>(a.dres) + offset;
     char *to = static_cast<char *>(a.dX) + offset;
@@ -262,6 +261,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
         for (int i = 0; i < P; ++i) dw[v][i] = db[v][i] = both(0.0f);
 #pragma unroll
     for (int i = 0; i < S; ++i) fetch(i);
+    if constexpr (HELD) load_weights<T, V>(a.w, lane, threads, at, held);
     statistics(row);
     int stage = 0;
     for (; row < a.T; row += step, to += step_bytes) {
