@@ -532,7 +532,8 @@ int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe
  * large as those of an Adam step. With `master` (float, only beside bf16 weights) the step is taken on the master and w is its rounding.
  * The products' operands are X, X X', the polynomials and products of these in fp16, scaled so that nothing overflows, with sums in float: for u of any size X is off by 7e-4 of itself (root mean
  * square), up to 3e-3 where matrices are near-square, 1e-2 where u's singular values are spread evenly over two powers of ten; what u holds in directions below 2^-12 of its largest is lost in that.
- * g and m may be as large as 2^60 or so: a matrix with a larger or no finite element in u becomes NaN as a whole. A matrix whose u is zero keeps its weights but for the decay.
+ * g and m may be as large as 2^60 or so, and as small as float's least numbers, whatever eps is (a normal number of float): a matrix with a larger or no finite element in u becomes NaN as a whole. A
+ * matrix whose u is zero keeps its weights but for the decay.
  * All pointers but host_tensors, host_params are device pointers; w, g, m, master on 16-byte boundaries. The list is read before the call returns; tensors of a list may not overlap.
  * Matrices are taken together from whatever tensors of the list: a list of a model's layers is three launches, more for more than six shapes, 128 tensors or
  * 1 GiB of X; matrices of up to 128 x 768 and 49152 elements take one launch of their own, where they are not a small part of a list of larger ones.

@@ -3,7 +3,6 @@
 // Here: the two passes before the products, both bound by memory. The first makes m and the sums of u's squares, the second X, which needs the whole matrix' norm. u is made of the
 // momentum as it is held, so that the second pass makes the same one again.
 #include <float.h>
-#include <math_constants.h>
 
 #include <vector>
 
@@ -56,7 +55,7 @@ __global__ void __launch_bounds__(THREADS) muon_momentum_kernel(const __grid_con
 
 // X in rows of ld elements, zeros behind the columns: a block has CHUNK of them, a piece of eight a thread at a time
 template <typename GT, typename MT, bool VECTORS>
-__device__ __forceinline__ void normalise_chunk(const GT *g, const MT *m, int64_t first, __half *x, int64_t begin, int64_t pieces, int32_t cols, int32_t ld, float grad_scale, float by,
+__device__ __forceinline__ void normalise_chunk(const GT *g, const MT *m, int64_t first, __half *x, int64_t begin, int64_t pieces, int32_t cols, int32_t ld, float grad_scale, const Factor &by,
                                                 const MuonPasses &k) {
     const int32_t in_row = ld / EACH;
 #pragma unroll
@@ -74,7 +73,7 @@ __device__ __forceinline__ void normalise_chunk(const GT *g, const MT *m, int64_
             for (int j = 0; j < EACH; j += 2) {
                 float u[2];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) u[q] = (k.nesterov ? fmaf(k.momentum, mv[j + q], gv[j + q] * grad_scale) : mv[j + q]) * by;
+                for (int q = 0; q < 2; ++q) u[q] = by(k.nesterov ? fmaf(k.momentum, mv[j + q], gv[j + q] * grad_scale) : mv[j + q]);
                 const __half2 h = __floats2half2_rn(u[0], u[1]);
                 out[j / 2] = *reinterpret_cast<const uint32_t *>(&h);
             }
@@ -83,7 +82,7 @@ __device__ __forceinline__ void normalise_chunk(const GT *g, const MT *m, int64_
     }
 }
 template <bool VECTORS>
-__device__ __forceinline__ void normalise_block(const MuonEntry &t, const MuonShape &s, int64_t first, __half *x, int64_t begin, float grad_scale, float by, const MuonPasses &k) {
+__device__ __forceinline__ void normalise_block(const MuonEntry &t, const MuonShape &s, int64_t first, __half *x, int64_t begin, float grad_scale, const Factor &by, const MuonPasses &k) {
     const int64_t pieces = (int64_t)s.rows * (s.ld / EACH);
     switch (t.kind & 6) {
         case 0: return normalise_chunk<float, float, VECTORS>(static_cast<const float *>(t.g), static_cast<const float *>(t.m), first, x, begin, pieces, s.cols, s.ld, grad_scale, by, k);
@@ -103,9 +102,7 @@ __global__ void __launch_bounds__(THREADS) muon_normalise_kernel(const __grid_co
     const int32_t here = id - s.blocks_before, in_shape = here / s.blocks, block = here - in_shape * s.blocks, matrix = s.first + in_shape;
     double v = 0.0;
     for (int32_t c = threadIdx.x; c < s.chunks; c += THREADS) v += k.part[s.chunks_before + (int64_t)in_shape * s.chunks + c];
-    v = sqrt(sum_of_block(v, sh)) + (double)k.eps;
-    // a matrix whose norm is no finite number becomes NaN as a whole
-    const float by = v <= (double)FLT_MAX ? (float)((double)MUON_UNIT / v) : CUDART_NAN_F;
+    const Factor by(sqrt(sum_of_block(v, sh)) + (double)k.eps);
     const int32_t i = b.entry_of(matrix);
     const int64_t first = (int64_t)(matrix - b.before[i]) * s.rows * s.cols, begin = (int64_t)block * (CHUNK / EACH);
     __half *x = s.x + (int64_t)in_shape * s.rows * s.ld;

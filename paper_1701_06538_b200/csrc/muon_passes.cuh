@@ -1,6 +1,9 @@
 // The first pass of the Muon step over a block's elements, 256 threads a chunk (muon.cu, muon_small.cu): m = momentum m + g and the squares of u
 #pragma once
 
+#include <float.h>
+#include <math_constants.h>
+
 #include "muon.cuh"
 #include "vectors.cuh"
 
@@ -48,6 +51,29 @@ template <typename T, bool VECTORS> __device__ __forceinline__ void store8(T *p,
     }
 }
 template <typename T> __device__ __forceinline__ float held(float v) { return to_f32(from_f32<T>(v)); }
+
+// The sum of eight squares, s as it came out in float. Squares of elements below 2^-63 or so are no normal numbers, below 2^-75 they are 0: where s is small (below 2^-100, of which what s lost is 2^-46), of
+// 2^100 times the elements, none of which is then above 2^50 or, but for zeros, below 2^-49
+__device__ __forceinline__ double squares(float s, const float (&u)[EACH]) {
+    if (s >= 0x1p-100f) return (double)s;
+    float t = 0.0f;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const float v = u[j] * 0x1p100f;
+        t = fmaf(v, v, t);
+    }
+    return (double)t * 0x1p-200;
+}
+// What u is multiplied by to make X of it, held as MUON_UNIT: `lift` first and `by` then, since MUON_UNIT over the least norm (eps) is beyond float's range and u times `lift` is not. A matrix whose norm is
+// no finite number becomes NaN as a whole
+struct Factor {
+    float lift, by;
+    __device__ __forceinline__ explicit Factor(double norm) {
+        lift = norm < 0x1p-64 ? 0x1p64f : 1.0f;
+        by = norm <= (double)FLT_MAX ? (float)((double)MUON_UNIT / (norm * (double)lift)) : CUDART_NAN_F;
+    }
+    __device__ __forceinline__ float operator()(float u) const { return u * lift * by; }
+};
 
 // Eight elements as they are loaded
 template <typename T, bool VECTORS> struct Eight {
@@ -100,18 +126,18 @@ __device__ __forceinline__ double momentum_chunk(const GT *g, MT *m, int64_t at,
         for (int i = 0; i < ROUND; ++i) {
             const int64_t here = first + (int64_t)(round + i) * (PASS_THREADS * EACH), live = end - here;
             if (live <= 0) continue;
-            float gv[EACH], mv[EACH], s = 0.0f;
+            float gv[EACH], mv[EACH], u[EACH], s = 0.0f;
             gq[i].get(gv);
             mq[i].get(mv);
 #pragma unroll
             for (int j = 0; j < EACH; ++j) {
                 const float gj = gv[j] * grad_scale;
                 mv[j] = held<MT>(fmaf(k.momentum, mv[j], gj));
-                const float u = k.nesterov ? fmaf(k.momentum, mv[j], gj) : mv[j];
-                s = fmaf(u, u, s);
+                u[j] = k.nesterov ? fmaf(k.momentum, mv[j], gj) : mv[j];
+                s = fmaf(u[j], u[j], s);
             }
             store8<MT, VECTORS>(m, here, live, mv);
-            sum += (double)s;
+            sum += squares(s, u);
         }
     }
     return sum;

@@ -6,9 +6,6 @@
 //
 // X is held as [N][128] whichever way the matrix lies, M columns and zeros behind them: 64-column pieces of 128-byte rows, 128-byte swizzle. A = X' X takes it MN-major twice, X B K-major by 128 rows
 // of it at a time, whose accumulators lie beside each other in tensor memory, four at most; X B takes the place of X.
-#include <float.h>
-#include <math_constants.h>
-
 #include <type_traits>
 
 #include "muon.cuh"
@@ -79,22 +76,22 @@ template <typename GT, typename MT, bool VECTORS> __device__ __forceinline__ dou
         for (int q = 0; q < 4; ++q) {
             const int32_t at = i + q * THREADS * EACH;
             if (at >= each) continue;
-            float s = 0.0f;
+            float u[EACH], s = 0.0f;
 #pragma unroll
             for (int j = 0; j < EACH; ++j) {
                 const float gj = gv[q][j] * grad_scale;
                 mv[q][j] = held<MT>(fmaf(k.momentum, mv[q][j], gj));
-                const float u = k.nesterov ? fmaf(k.momentum, mv[q][j], gj) : mv[q][j];
-                s = fmaf(u, u, s);
+                u[j] = k.nesterov ? fmaf(k.momentum, mv[q][j], gj) : mv[q][j];
+                s = fmaf(u[j], u[j], s);
             }
             store8<MT, VECTORS>(p, at, each - at, mv[q]);
-            sum += (double)s;
+            sum += squares(s, u);
         }
     }
     return sum;
 }
 // X, eight columns of a row a thread, two of them at a time; neighbours have neighbouring elements of memory. What lies behind rows and columns is zero already
-template <typename GT, typename MT> __device__ __forceinline__ void make_x(const Matrix &a, const GT *g, const MT *p, const MuonPasses &k, float grad_scale, float by, uint8_t *x) {
+template <typename GT, typename MT> __device__ __forceinline__ void make_x(const Matrix &a, const GT *g, const MT *p, const MuonPasses &k, float grad_scale, const Factor &by, uint8_t *x) {
     const int32_t stride = a.stride(), eights = (a.M + 7) / 8, all = a.N * eights, inner = a.left ? a.N : eights;
     const float by_inner = 1.0f / (float)inner;
     for (int32_t i = threadIdx.x; i < all; i += 2 * THREADS) {
@@ -127,7 +124,7 @@ template <typename GT, typename MT> __device__ __forceinline__ void make_x(const
             float2 v[4];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float u = (k.nesterov ? fmaf(k.momentum, mv[q][j], gv[q][j]) : mv[q][j]) * by;
+                const float u = by(k.nesterov ? fmaf(k.momentum, mv[q][j], gv[q][j]) : mv[q][j]);
                 (j & 1 ? v[j / 2].y : v[j / 2].x) = j < live[q] ? u : 0.0f;  // (a NaN factor leaves the zeros behind the columns alone)
             }
             *reinterpret_cast<uint4 *>(x + (m[q] >> 6) * (a.Np * 128) + n[q] * 128 + ((((m[q] & 63) >> 3) ^ (n[q] & 7)) << 4)) = pack8(v);
@@ -201,7 +198,7 @@ __global__ void __launch_bounds__(THREADS) muon_small_kernel(const __grid_consta
     });
     for (int32_t i = threadIdx.x; i < a.Np * 16; i += THREADS) reinterpret_cast<uint4 *>(x)[i] = make_uint4(0u, 0u, 0u, 0u);
     sum = sqrt(block_sum(sum, sh)) + (double)k.eps;  // (whose barrier is behind the block's last store of a momentum, and of a zero)
-    const float by = sum <= (double)FLT_MAX ? (float)((double)MUON_UNIT / sum) : CUDART_NAN_F;
+    const Factor by(sum);
     typed([&](auto *g, auto *m) {
         using GT = std::decay_t<decltype(*g)>;
         using MT = std::decay_t<decltype(*m)>;
