@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             r[k] = next_r[k];
-            off[k] = -next_mean[k] * r[k];
+            off[k] = -next_mean[k];
         }
         statistics(row + step);
         copies_wait<S - 1>();
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_grads_kernel(const
                 weights(v, w);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    n[k][v][i] = fma2(x.get(2 * i), both(r[k]), both(off[k]));
+                    n[k][v][i] = mul2(add2(x.get(2 * i), both(off[k])), both(r[k]));  // (x r - mean r loses what the mean is larger than the spread)
                     const float2 d = g[k][v].get(2 * i), u = mul2(d, w[i]);
                     first = add2(u, first);
                     second = fma2(u, n[k][v][i], second);
