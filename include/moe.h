@@ -531,7 +531,10 @@ int32_t moe_adamw(const moe_adamw_tensor *host_tensors, int32_t count, const moe
  * After five steps X's singular values lie between 0.7 and 1.2, wherever those of u were between 1 and 1/1000 or so of its norm. scale: 0.2 sqrt(max(rows, cols)) makes the update's elements as
  * large as those of an Adam step. With `master` (float, only beside bf16 weights) the step is taken on the master and w is its rounding.
  * The products' operands are X, X X', the polynomials and products of these in fp16, scaled so that nothing overflows, with sums in float: for u of any size X is off by 7e-4 of itself (root mean
- * square), up to 3e-3 where matrices are near-square, 1e-2 where u's singular values are spread evenly over two powers of ten; what u holds in directions below 2^-12 of its largest is lost in that.
+ * square), up to 3e-3 where matrices are near-square, 1e-2 where u's singular values are spread evenly over two powers of ten; what u holds in directions below 2^-12 of its largest is lost in that,
+ * and directions that it has nothing in get up to 0.15 of the norm that X begins with, 1, beside the square root of u's rank at X's end (gradients of experts with few rows: 0.04 of X at a rank of 16).
+ * How a matrix' steps are taken together depends on its shape alone, not on what else is in the list (near-square ones go step by step); beside much larger ones, matrices whose shorter side is at
+ * most 128 are made in other tiles, by the same bounds.
  * g and m may be as large as 2^60 or so, and as small as float's least numbers, whatever eps is (a normal number of float): a matrix with a larger or no finite element in u becomes NaN as a whole. A
  * matrix whose u is zero keeps its weights but for the decay.
  * All pointers but host_tensors, host_params are device pointers; w, g, m, master on 16-byte boundaries. The list is read before the call returns; tensors of a list may not overlap.

@@ -20,7 +20,7 @@
 // multiplies such an error by 5 (a gate of 512 x 32, whose A is nearly diagonal, was off by 3e-3 with rounded diagonals). Accumulators are float, and the last X is not rounded at all.
 //
 // All products of all matrices, of several shapes, are one launch: tiles are drawn one after the other in an order in which what a tile reads is always drawn before it (group of
-// matrices, segment, phase, shape, matrix, tile), and a count of stored tiles for every matrix tells when it is there. With a group that fills the SMs more than once, what a tile waits
+// matrices, phase, shape, matrix, tile: muon_order.cuh), and a count of stored tiles for every matrix tells when it is there. With a group that fills the SMs more than once, what a tile waits
 // for was stored long ago, and the chain of a lone matrix' products (a gate's) runs beside the others'. (A launch for every product leaves its last wave of tiles half empty: 3 tiles of A and P
 // and 8 of X for each of 512 x 1024.) Whoever waits does so for tiles of blocks that run already, so that no number of resident blocks is presumed.
 //
@@ -32,6 +32,7 @@
 #include <type_traits>
 
 #include "muon.cuh"
+#include "muon_order.cuh"
 #include "pairs.cuh"
 #include "short_wait.cuh"
 #include "tc.cuh"
@@ -47,117 +48,19 @@ constexpr int NS_STAGES = 5;
 constexpr uint32_t BOX = 4096;                // a warp's 32 rows of 64 columns
 constexpr int NS_DATA = NS_STAGES * STAGE2_BYTES + 2 * 8 * BOX, NS_SMEM = NS_DATA + 1024 /*alignment*/ + 512 /*barriers, ring*/ + 8 * 128 /*factors*/;
 
-// What a tile is of: A = X X', P = a I + b A + c A A, a product of two of the symmetric matrices, X <- Q X
-enum Kind4 { GRAM = 0, POLY = 1, MULT = 2, APPLY = 3 };
-// The symmetric matrices
-enum { S_A = 0, S_P = 1, S_T = 2, S_P2 = 3, S_Q = 4, SYMMETRIC = 5 };
 struct NsMaps { CUtensorMap x_k[2], x_mn[2], s_k[SYMMETRIC], s_mn[SYMMETRIC]; };  // x[0]: all matrices, the others: a ring of slots
-struct NsShape {
-    int32_t rows, cols, ld, M, Mld, first, matrices, left;
-    int32_t square, cols3, tiles3;            // tiles of a symmetric matrix (lower half), tiles of X beside each other, of X
-    int32_t group, slots;
-    const __half *x[2], *s[SYMMETRIC];        // [matrices or slots][rows][ld], [slots][M][Mld]
-    float *d;                                 // [SYMMETRIC][slots][M] their diagonals
-};
-struct NsArgs {
-    NsShape s[MUON_MAX_SHAPES];
-    int32_t shapes, steps, together, groups;  // together: steps of a segment
+struct NsArgs : NsPlan {
     int32_t *done, *next, *status;
     float lr;
     const moe_muon_rates *rates;
 };
 struct NsAllMaps { NsMaps m[MUON_MAX_SHAPES]; };
 struct NsTile { int32_t matrix, shape, segment, kind, a, b, out, row, col, slot; };
-
-// A segment of n steps as phases, each of which needs all before it: two products at most, a * b -> out. Q of the steps goes from P (or P2) over S_Q to S_T.
-struct NsOp { uint8_t kind, a, b, out; };
-struct NsPhase { NsOp op[2]; uint8_t n; };
-struct NsProgram { NsPhase phase[10]; uint8_t n, squares; };  // squares: products of symmetric matrices, A among them
-__host__ __device__ constexpr NsProgram program_of(int steps) {
-    constexpr NsOp none = {0, 0, 0, 0}, gram = {GRAM, 0, 0, S_A};
-    if (steps == 1) return {{{{gram, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{APPLY, S_P, 0, 0}, none}, 1}}, 3, 2};
-    if (steps == 2)
-        return {{{{gram, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{MULT, S_P, S_A, S_T}, none}, 1}, {{{MULT, S_P, S_T, S_A}, none}, 1}, {{{POLY, S_A, S_A, S_P2}, none}, 1},
-                 {{{MULT, S_P2, S_P, S_T}, none}, 1}, {{{APPLY, S_T, 0, 0}, none}, 1}}, 7, 6};
-    return {{{{gram, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{MULT, S_P, S_A, S_T}, none}, 1}, {{{MULT, S_P, S_T, S_A}, none}, 1}, {{{POLY, S_A, S_A, S_P2}, none}, 1},
-             {{{MULT, S_P2, S_A, S_T}, {MULT, S_P2, S_P, S_Q}}, 2}, {{{MULT, S_P2, S_T, S_A}, none}, 1}, {{{POLY, S_A, S_A, S_P}, none}, 1}, {{{MULT, S_P, S_Q, S_T}, none}, 1},
-             {{{APPLY, S_T, 0, 0}, none}, 1}}, 10, 10};
-}
-__constant__ const NsProgram programs[4] = {program_of(1), program_of(1), program_of(2), program_of(3)};
-constexpr NsProgram programs_host[4] = {program_of(1), program_of(1), program_of(2), program_of(3)};
-constexpr int MOST_TOGETHER = 3;
-constexpr int symmetric_of(int together) { return together == 1 ? 2 : together == 2 ? 4 : 5; }  // that a segment uses, in their order
+static_assert(MUON_MAX_SHAPES == NS_MAX_SHAPES, "shapes of a launch");
 
 template <bool PAIR> constexpr int tile_side() { return PAIR ? 256 : 128; }
 template <bool PAIR> constexpr int arrivals() { return PAIR ? 2 : 1; }  // of a stored tile: CTAs
 
-// The tiles in their order: {matrix or -1, shape << 16 | segment << 11 | kind << 9 | a << 6 | b << 3 | out, tile's row << 16 | column, slot} of ascending numbers
-template <bool PAIR> struct NsOrder {
-    const NsArgs &p;
-    int32_t group, base;         // the group that is at, its first number
-    int32_t squares, applies;    // tiles of a group: of a symmetric matrix, of X
-    int32_t tiles_before;        // of the found one's matrix, in earlier phases
-    __device__ __forceinline__ explicit NsOrder(const NsArgs &p_) : p(p_), group(0), base(0) { count(); }
-    __device__ __forceinline__ int32_t here(int s) const { return min(p.s[s].group, max(0, p.s[s].matrices - group * p.s[s].group)); }
-    __device__ __forceinline__ void count() {
-        squares = applies = 0;
-        for (int s = 0; s < p.shapes; ++s) {
-            squares += here(s) * p.s[s].square;
-            applies += here(s) * p.s[s].tiles3;
-        }
-    }
-    __device__ __forceinline__ int32_t full() const { return p.steps / p.together; }  // segments of p.together steps
-    __device__ __forceinline__ int32_t rest() const { return p.steps % p.together; }  // steps of one before them, or 0
-    __device__ __forceinline__ int32_t segment_tiles(int steps) const { return steps ? programs[steps].squares * squares + applies : 0; }
-    __device__ __forceinline__ int32_t group_tiles() const { return full() * segment_tiles(p.together) + segment_tiles(rest()); }
-    __device__ __forceinline__ int4 find(int32_t id) {
-        while (group < p.groups && id - base >= group_tiles()) {
-            base += group_tiles();
-            ++group;
-            count();
-        }
-        if (group >= p.groups) return make_int4(-1, 0, 0, 0);
-        int32_t r = id - base;
-        int32_t segment = 0, squares_before = 0, steps = rest();
-        if (r >= segment_tiles(steps)) {
-            r -= segment_tiles(steps);
-            if (steps) { segment = 1; squares_before = programs[steps].squares; }
-            steps = p.together;
-            const int32_t each = segment_tiles(steps), more = r / each;
-            r -= more * each;
-            segment += more;
-            squares_before += more * programs[steps].squares;
-        }
-        const NsProgram &g = programs[steps];
-        for (int phase = 0;; ++phase) {
-            const NsPhase &f = g.phase[phase];
-            const bool apply = phase == g.n - 1;
-            const int32_t all = apply ? applies : f.n * squares;
-            if (r >= all) { r -= all; squares_before += f.n; continue; }
-            for (int s = 0;; ++s) {
-                const NsShape &h = p.s[s];
-                const int32_t tiles = apply ? h.tiles3 : f.n * h.square, mine = here(s) * tiles;
-                if (r >= mine) { r -= mine; continue; }
-                const int32_t m = r / tiles, matrix = group * h.group + m;
-                int32_t t = r - m * tiles, row, col, which = 0;
-                if (apply) {
-                    row = t / h.cols3;
-                    col = t - row * h.cols3;
-                } else {
-                    if (t >= h.square) { t -= h.square; which = 1; }
-                    for (row = 0; t > row; ++row) t -= row + 1;
-                    col = t;
-                }
-                tiles_before = squares_before * h.square + segment * h.tiles3;
-                const NsOp &o = f.op[which];
-                return make_int4(matrix, s << 16 | segment << 11 | o.kind << 9 | o.a << 6 | o.b << 3 | o.out, row << 16 | col, matrix % h.slots);
-            }
-        }
-    }
-    __device__ __forceinline__ int32_t tiles_of(const NsShape &h) const {  // of a matrix, in all
-        return (full() * programs[p.together].squares + (rest() ? programs[rest()].squares : 0)) * h.square + (full() + (rest() > 0)) * h.tiles3;
-    }
-};
 __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
     int32_t v;
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
@@ -528,7 +431,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
     auto cols_out = [&](const NsShape &s, const NsTile &t) { return t.kind == APPLY ? s.ld : s.Mld; };
     auto rows_out = [&](const NsShape &s, const NsTile &t) { return t.kind == APPLY ? s.rows : s.M; };
     auto width_of = [&](const NsShape &s, const NsTile &t) { return PAIR && cols_out(s, t) - t.col > 128 ? 256 : 128; };
-    auto is_last = [&](const NsTile &t) { return t.kind == APPLY && (t.segment + 1) * p.together >= p.steps; };
+    auto is_last = [&](const NsShape &s, const NsTile &t) { return t.kind == APPLY && (t.segment + 1) * s.together >= p.steps; };
     // Where an operand lies in a product whose contraction runs along the shorter side: block kb of it is in the lower half for rows from `at` on, or has to be transposed
     auto upper = [&](int kb, int32_t at) { return kb * BK / SIDE > at / SIDE; };
     auto a_is_mn = [&](const NsShape &s, const NsTile &t, int kb) { return t.kind == GRAM ? !s.left : t.kind == APPLY && !s.left ? false : upper(kb, t.row); };
@@ -629,7 +532,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
         // ------------------------------------------------------------------ drawing tiles (even CTA, one thread)
         if (rank == 0 && lane == 0) {
             const uint32_t peer_ring = PAIR ? peer_smem_addr(ring, 1) : 0u, peer_full0 = PAIR ? peer_smem_addr(ring_full0, 1) : 0u;
-            NsOrder<PAIR> order(p);
+            NsOrder order(p);
             for (int i = 0;; ++i) {
                 const uint32_t slot = (uint32_t)i % RING;
                 if (i >= RING) {  // every reader of the record this slot held has its copy
@@ -637,13 +540,14 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
                     if (!short_wait(ring_empty0 + 8u * slot, par, abort_flag, p.status)) break;
                     if (PAIR) mbar_try_wait_cluster(ring_empty0 + 8u * slot, par);
                 }
-                const int4 a = order.find(atomicAdd(p.next, 1));
+                const NsTileRecord drawn = order.find(atomicAdd(p.next, 1));
+                const int4 a = make_int4(drawn.matrix, drawn.what, drawn.place, drawn.slot);
                 if (a.x >= 0) {  // handed out when what it reads is there: then nobody else has to look
                     const NsShape &h = p.s[a.y >> 16];
                     const int32_t *count = p.done + h.first + a.x;
                     bool ok = wait_count(count, arrivals<PAIR>() * order.tiles_before, abort_flag, p.status);
                     if (ok && order.tiles_before == 0 && a.x >= h.slots)  // and the slot's last user has read what is overwritten now
-                        ok = wait_count(count - h.slots, arrivals<PAIR>() * order.tiles_of(h), abort_flag, p.status);
+                        ok = wait_count(count - h.slots, arrivals<PAIR>() * tiles_of_matrix(h, p.steps), abort_flag, p.status);
                     if (!ok) break;
                     fence_async();  // what other SMs' copies have stored, before copies read it
                 }
@@ -664,7 +568,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             while (ok && tiles.next(t)) {
                 const NsShape &h = p.s[t.shape];
                 const NsMaps &maps = all_maps.m[t.shape];
-                const bool last = is_last(t);
+                const bool last = is_last(h, t);
                 const int to = (t.segment & 1) ^ 1;  // of X
                 const CUtensorMap *out = t.kind == APPLY ? &maps.x_k[to] : &maps.s_k[t.out];
                 const int matrix = t.kind == APPLY && !to ? t.matrix : t.slot;
@@ -711,7 +615,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) newton_schulz_kernel(const __gr
             b.boxes_n = boxes_of(h, t, w, b.row0, b.first);
             const int32_t row = b.row0 + lane;
             const int slot = t.slot, x = t.segment & 1;
-            const bool last = is_last(t);
+            const bool last = is_last(h, t);
             auto diagonal_of = [&](int s) { return h.d + ((int64_t)s * h.slots + slot) * h.M; };
             auto symmetric_at = [&](int s) { return h.s[s] + ((int64_t)slot * h.M + row) * h.Mld + b.first; };
             b.boxes = boxes_at; b.factors = factors; b.M = h.M;
@@ -807,18 +711,15 @@ int64_t groups_of(const MuonBatch &b, bool pair) {
     return imax(1, square / (pair ? GROUP_TILES : 2 * GROUP_TILES));
 }
 // How many steps a segment has at most: what makes the fewest 64-deep blocks of products a step, one where that saves less than an eighth (near-square matrices have small singular values,
-// see above: X of 512 x 576 normal numbers is off by 1.5e-3 in segments and by 8e-4 without)
-int32_t together_of(const MuonBatch &b, bool pair) {
+// see above: X of 512 x 576 normal numbers is off by 1.5e-3 in segments and by 8e-4 without). By the shape alone, whatever else is in the list and wherever its tiles are made
+int32_t together_of(int32_t rows, int32_t cols) {
     int32_t best = 1;
     int64_t least = 0, alone = 0;  // blocks of six steps
+    NsShape s;
+    tiles_of(rows, cols, ns_pairs(rows, cols), &s);
+    const int64_t M = cdiv(imin(rows, cols), BK), N = cdiv(imax(rows, cols), BK);
     for (int32_t n = 1; n <= MOST_TOGETHER; ++n) {
-        int64_t work = 0;
-        for (int i = 0; i < b.shapes; ++i) {
-            NsShape s;
-            tiles_of(b.s[i].rows, b.s[i].cols, pair, &s);
-            const int64_t M = cdiv(imin(b.s[i].rows, b.s[i].cols), BK), N = cdiv(imax(b.s[i].rows, b.s[i].cols), BK);
-            work += b.s[i].matrices * (s.square * (N + (programs_host[n].squares - 1) * M) + s.tiles3 * M) * (6 / n);
-        }
+        const int64_t work = (s.square * (N + (programs_host[n].squares - 1) * M) + s.tiles3 * M) * (6 / n);
         if (n == 1) least = alone = work;
         else if (work < least && 8 * work <= 7 * alone) { best = n; least = work; }
     }
@@ -826,8 +727,10 @@ int32_t together_of(const MuonBatch &b, bool pair) {
 }
 struct NsScratch { __half *x, *s[SYMMETRIC]; };
 // Everything about a shape but its place in memory, and with scratch that too
-NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, int32_t together, Carver &cv, NsScratch *at) {
+NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, int32_t steps, Carver &cv, NsScratch *at) {
     NsShape s = {};
+    s.together = (int32_t)imin(steps, together_of(m.rows, m.cols));
+    s.turns = turns_of(steps, s.together);
     tiles_of(m.rows, m.cols, pair, &s);
     s.rows = m.rows; s.cols = m.cols; s.ld = m.ld;
     s.M = (int32_t)imin(m.rows, m.cols);
@@ -836,8 +739,8 @@ NsShape shape_of(const MuonShape &m, bool pair, int64_t groups, int32_t together
     s.group = (int32_t)cdiv(m.matrices, groups);
     s.slots = (int32_t)imin(m.matrices, 2 * (int64_t)s.group);  // a group's begin while the last one's end
     at->x = cv.take<__half>((int64_t)s.slots * s.rows * s.ld);
-    for (int i = 0; i < symmetric_of(together); ++i) s.s[i] = at->s[i] = cv.take<__half>((int64_t)s.slots * s.M * s.Mld);
-    s.d = cv.take<float>((int64_t)symmetric_of(together) * s.slots * s.M);
+    for (int i = 0; i < symmetric_of(s.together); ++i) s.s[i] = at->s[i] = cv.take<__half>((int64_t)s.slots * s.M * s.Mld);
+    s.d = cv.take<float>((int64_t)symmetric_of(s.together) * s.slots * s.M);
     s.x[0] = m.x; s.x[1] = at->x;
     return s;
 }
@@ -888,9 +791,8 @@ int64_t ns_tiles(int32_t rows, int32_t cols, bool pair) {
 int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair) {
     Carver cv(nullptr);
     const int64_t groups = groups_of(batch, pair);
-    const int32_t together = together_of(batch, pair);  // enough for any number of steps
     NsScratch at;
-    for (int i = 0; i < batch.shapes; ++i) shape_of(batch.s[i], pair, groups, together, cv, &at);
+    for (int i = 0; i < batch.shapes; ++i) shape_of(batch.s[i], pair, groups, MOE_MUON_MAX_STEPS, cv, &at);  // (enough for any number of steps)
     return (int64_t)cv.off;
 }
 
@@ -901,17 +803,17 @@ int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st) {
     NsAllMaps maps;
     NsArgs p = {};
     int64_t total = 0;
-    p.shapes = b.shapes; p.steps = w.steps; p.together = (int32_t)imin(w.steps, together_of(b, w.pair));
+    p.shapes = b.shapes; p.steps = w.steps;
     for (int i = 0; i < b.shapes; ++i) {
         NsScratch at;
         NsShape &s = p.s[i];
         NsMaps &m = maps.m[i];
-        s = shape_of(b.s[i], w.pair, groups, p.together, cv, &at);
+        s = shape_of(b.s[i], w.pair, groups, w.steps, cv, &at);
         MOE_TRY(maps_of(b.s[i].x, s.matrices, s.rows, s.ld, &m.x_k[0], &m.x_mn[0]));
         MOE_TRY(maps_of(at.x, s.slots, s.rows, s.ld, &m.x_k[1], &m.x_mn[1]));
-        for (int j = 0; j < symmetric_of(p.together); ++j) MOE_TRY(maps_of(at.s[j], s.slots, s.M, s.Mld, &m.s_k[j], &m.s_mn[j]));
-        const int32_t rest = w.steps % p.together;
-        total += s.matrices * (w.steps / p.together * (programs_host[p.together].squares * (int64_t)s.square + s.tiles3) + (rest ? programs_host[rest].squares * (int64_t)s.square + s.tiles3 : 0));
+        for (int j = 0; j < symmetric_of(s.together); ++j) MOE_TRY(maps_of(at.s[j], s.slots, s.M, s.Mld, &m.s_k[j], &m.s_mn[j]));
+        total += (int64_t)s.matrices * tiles_of_matrix(s, w.steps);
+        p.turns = (int32_t)imax(p.turns, s.turns);
         p.groups = (int32_t)imax(p.groups, cdiv(s.matrices, s.group));
     }
     if (total > (int64_t)1 << 30) return MOE_ERR_UNSUPPORTED;
