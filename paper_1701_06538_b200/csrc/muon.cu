@@ -4,6 +4,7 @@
 // momentum as it is held, so that the second pass makes the same one again.
 #include <float.h>
 
+#include <memory>
 #include <vector>
 
 #include "muon.cuh"
@@ -243,6 +244,14 @@ Scratch scratch_of(Carver &cv, MuonBatch &b, bool pair) {
     return s;
 }
 
+// Everything is made before the first launch: what is refused is refused before anything has changed
+struct Ready {
+    MuonBatch batch;
+    How how;
+    MuonPasses passes;
+    NsLaunch products;
+};
+
 }  // namespace
 
 int32_t muon_check(const moe_muon_tensor *tensors, int32_t count) {
@@ -263,26 +272,44 @@ int32_t muon_bytes(const moe_muon_tensor *tensors, int32_t count, int64_t *bytes
 }
 
 int32_t launch_muon(const moe_muon_tensor *tensors, int32_t count, const moe_muon_params &p, const moe_muon_rates *rates, void *ws, cudaStream_t st) {
-    bool first = true;
-    return for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
+    std::vector<std::unique_ptr<Ready>> all;
+    MOE_TRY(for_each_launch(tensors, count, [&](MuonBatch &b, How how) -> int32_t {
         const bool pair = how == PAIRS;
         Carver cv(ws);
         int32_t *status = static_cast<int32_t *>(cv.take_bytes(kWsHeader));
         MuonPasses k = {};
         k.status = status;
-        k.clear_status = first; k.nesterov = p.nesterov;
+        k.clear_status = all.empty(); k.nesterov = p.nesterov;
         k.momentum = (float)p.momentum; k.eps = (float)p.eps; k.grad_scale = (float)p.grad_scale; k.rates = rates;
-        first = false;
-        if (how == SMALL) return launch_muon_small(b, k, (float)p.lr, p.steps, st);
-        const Scratch s = scratch_of(cv, b, pair);
-        k.part = s.part; k.done = s.done; k.next = s.next;
+        all.push_back(std::unique_ptr<Ready>(new Ready));
+        Ready &r = *all.back();
+        r.how = how;
+        if (how == SMALL) {
+            MOE_TRY(muon_small_ready());
+        } else {
+            const Scratch s = scratch_of(cv, b, pair);
+            k.part = s.part; k.done = s.done; k.next = s.next;
+            const NsWork w = {&b, pair, p.steps, s.done, s.next, status, s.products, (float)p.lr, rates};
+            MOE_TRY(prepare_newton_schulz(w, &r.products));
+        }
+        r.batch = b;
+        r.passes = k;
+        return MOE_OK;
+    }));
+    for (const auto &one : all) {
+        const MuonBatch &b = one->batch;
+        const MuonPasses &k = one->passes;
+        if (one->how == SMALL) {
+            MOE_TRY(launch_muon_small(b, k, (float)p.lr, p.steps, st));
+            continue;
+        }
         launch_kernel(muon_momentum_kernel, dim3((unsigned)blocks_of(b, false)), dim3(THREADS), 0, st, b, k);
         MOE_LAUNCHED();
         launch_kernel(muon_normalise_kernel, dim3((unsigned)blocks_of(b, true)), dim3(THREADS), 0, st, b, k);
         MOE_LAUNCHED();
-        const NsWork w = {&b, pair, p.steps, s.done, s.next, status, s.products, (float)p.lr, rates};
-        return launch_newton_schulz(w, st);
-    });
+        MOE_TRY(launch_newton_schulz(one->products, b, st));
+    }
+    return MOE_OK;
 }
 
 }  // namespace moe

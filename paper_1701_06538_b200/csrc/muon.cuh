@@ -4,6 +4,7 @@
 #include <cuda_fp16.h>
 
 #include "block.cuh"
+#include "muon_order.cuh"
 
 namespace moe {
 
@@ -52,6 +53,7 @@ struct MuonPasses {
 
 // The whole step by a block a matrix, for small ones (muon_small.cu)
 bool muon_is_small(int32_t rows, int32_t cols);
+int32_t muon_small_ready();  // whether the device can run it
 int32_t launch_muon_small(const MuonBatch &b, const MuonPasses &k, float lr, int32_t steps, cudaStream_t st);
 
 // Newton-Schulz products of a batch's matrices and the step on their weights. Scratch: ns_scratch_bytes
@@ -66,9 +68,25 @@ struct NsWork {
     float lr;
     const moe_muon_rates *rates;  // or nullptr
 };
+// The launch of them, made before anything of the step is launched: all that may be refused is refused then, and no momentum has taken a step that weights do not take
+struct NsMaps { CUtensorMap x_k[2], x_mn[2], s_k[SYMMETRIC], s_mn[SYMMETRIC]; };  // x[0]: all matrices, the others: a ring of slots
+struct NsAllMaps { NsMaps m[MUON_MAX_SHAPES]; };
+struct NsArgs : NsPlan {
+    int32_t *done, *next, *status;
+    float lr;
+    const moe_muon_rates *rates;
+};
+static_assert(MUON_MAX_SHAPES == NS_MAX_SHAPES, "shapes of a launch");
+struct NsLaunch {
+    NsAllMaps maps;
+    NsArgs args;
+    int64_t tiles;
+    bool pair;
+};
 static inline bool ns_pairs(int32_t rows, int32_t cols) { return imin(rows, cols) > 128; }  // whether a shape takes tiles of SM pairs (768 of 184 x 144: 835 us, by single SMs 1340; 128 of 192 x 448 242 and 342; 64 of 512 x 1024 580 and 712)
 int64_t ns_tiles(int32_t rows, int32_t cols, bool pair);                                   // of a matrix, a step
 int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair);
-int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st);
+int32_t prepare_newton_schulz(const NsWork &w, NsLaunch *to);
+int32_t launch_newton_schulz(const NsLaunch &l, const MuonBatch &batch, cudaStream_t st);
 
 }  // namespace moe

@@ -8,8 +8,6 @@ struct __half;
 
 namespace moe {
 
-namespace {
-
 constexpr int NS_MAX_SHAPES = 6;
 // What a tile is of: A = X X', P = a I + b A + c A A, a product of two of the symmetric matrices, X <- Q X
 enum Kind4 { GRAM = 0, POLY = 1, MULT = 2, APPLY = 3 };
@@ -43,7 +41,7 @@ __host__ __device__ constexpr NsProgram program_of(int steps) {
              {{{APPLY, S_T, 0, 0}, none}, 1}}, 10, 10};
 }
 #ifdef __CUDACC__
-__constant__ const NsProgram programs_device[4] = {program_of(1), program_of(1), program_of(2), program_of(3)};
+static __constant__ const NsProgram programs_device[4] = {program_of(1), program_of(1), program_of(2), program_of(3)};
 #endif
 constexpr NsProgram programs_host[4] = {program_of(1), program_of(1), program_of(2), program_of(3)};
 __host__ __device__ __forceinline__ const NsProgram &program(int steps) {
@@ -127,7 +125,5 @@ struct NsOrder {
         }
     }
 };
-
-}  // namespace
 
 }  // namespace moe

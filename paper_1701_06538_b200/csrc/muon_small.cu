@@ -390,14 +390,17 @@ __global__ void __launch_bounds__(THREADS) muon_small_kernel(const __grid_consta
 constexpr int64_t MOST_ELEMENTS = 49152;
 bool muon_is_small(int32_t rows, int32_t cols) { return imin(rows, cols) <= 128 && imax(rows, cols) <= MAX_N && (int64_t)rows * cols <= MOST_ELEMENTS; }
 
+int32_t muon_small_ready() {
+    static PerDevice allowed;
+    return allow_shared(allowed, muon_small_kernel, MAX_N * 256 + 128 * 256 + 1024) ? MOE_OK : MOE_ERR_CUDA;
+}
+
 int32_t launch_muon_small(const MuonBatch &b, const MuonPasses &k, float lr, int32_t steps, cudaStream_t st) {
     int64_t longest = 0;
     for (int q = 0; q < b.shapes; ++q) longest = imax(longest, imax(b.s[q].rows, b.s[q].cols));
     const int64_t x_rows = cdiv(longest, 128) * 128, tiles = x_rows / 128;
     const uint32_t tmem_cols = tiles <= 1 ? 128 : tiles == 2 ? 256 : 512;  // (an SM holds three blocks of one tile, two of two, one of more)
     const int bytes = (int)(x_rows * 256 + 128 * 256 + 1024);
-    static PerDevice allowed;
-    if (!allow_shared(allowed, muon_small_kernel, MAX_N * 256 + 128 * 256 + 1024)) return MOE_ERR_CUDA;
     launch_kernel(muon_small_kernel, dim3((unsigned)b.matrices()), dim3(THREADS), (size_t)bytes, st, b, k, lr, steps, (int32_t)x_rows, tmem_cols);
     MOE_LAUNCHED();
     return MOE_OK;

@@ -32,7 +32,6 @@
 #include <type_traits>
 
 #include "muon.cuh"
-#include "muon_order.cuh"
 #include "pairs.cuh"
 #include "short_wait.cuh"
 #include "tc.cuh"
@@ -48,15 +47,7 @@ constexpr int NS_STAGES = 5;
 constexpr uint32_t BOX = 4096;                // a warp's 32 rows of 64 columns
 constexpr int NS_DATA = NS_STAGES * STAGE2_BYTES + 2 * 8 * BOX, NS_SMEM = NS_DATA + 1024 /*alignment*/ + 512 /*barriers, ring*/ + 8 * 128 /*factors*/;
 
-struct NsMaps { CUtensorMap x_k[2], x_mn[2], s_k[SYMMETRIC], s_mn[SYMMETRIC]; };  // x[0]: all matrices, the others: a ring of slots
-struct NsArgs : NsPlan {
-    int32_t *done, *next, *status;
-    float lr;
-    const moe_muon_rates *rates;
-};
-struct NsAllMaps { NsMaps m[MUON_MAX_SHAPES]; };
 struct NsTile { int32_t matrix, shape, segment, kind, a, b, out, row, col, slot; };
-static_assert(MUON_MAX_SHAPES == NS_MAX_SHAPES, "shapes of a launch");
 
 template <bool PAIR> constexpr int tile_side() { return PAIR ? 256 : 128; }
 template <bool PAIR> constexpr int arrivals() { return PAIR ? 2 : 1; }  // of a stored tile: CTAs
@@ -754,7 +745,8 @@ int32_t maps_of(const __half *at, int64_t count, int64_t rows, int64_t ld, CUten
     return tc_make_map(mn, at, 4, dims4, str4, box4);
 }
 
-template <bool PAIR> int32_t launch_ns(const NsAllMaps &maps, const NsArgs &p, const MuonBatch &batch, int64_t total, cudaStream_t st) {
+// By as many CTAs, or pairs of them, as the device runs at once. l == nullptr: only whether it runs any
+template <bool PAIR> int32_t launch_ns(const NsLaunch *l, const MuonBatch *batch, cudaStream_t st) {
     static PerDevice most;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
@@ -774,8 +766,9 @@ template <bool PAIR> int32_t launch_ns(const NsAllMaps &maps, const NsArgs &p, c
         return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
     });
     if (workers <= 0) return MOE_ERR_CUDA;
-    cfg.gridDim = dim3((PAIR ? 2 : 1) * (unsigned)imin(total, workers));
-    MOE_CUDA(cudaLaunchKernelEx(&cfg, kernel, maps, p, batch));
+    if (!l) return MOE_OK;
+    cfg.gridDim = dim3((PAIR ? 2 : 1) * (unsigned)imin(l->tiles, workers));
+    MOE_CUDA(cudaLaunchKernelEx(&cfg, kernel, l->maps, l->args, *batch));
     MOE_LAUNCHED();
     return MOE_OK;
 }
@@ -796,29 +789,32 @@ int64_t ns_scratch_bytes(const MuonBatch &batch, bool pair) {
     return (int64_t)cv.off;
 }
 
-int32_t launch_newton_schulz(const NsWork &w, cudaStream_t st) {
+int32_t prepare_newton_schulz(const NsWork &w, NsLaunch *to) {
     const MuonBatch &b = *w.batch;
     Carver cv(w.scratch);
     const int64_t groups = groups_of(b, w.pair);
-    NsAllMaps maps;
-    NsArgs p = {};
-    int64_t total = 0;
+    NsArgs &p = to->args;
+    p = {};
+    to->pair = w.pair;
+    to->tiles = 0;
     p.shapes = b.shapes; p.steps = w.steps;
     for (int i = 0; i < b.shapes; ++i) {
         NsScratch at;
         NsShape &s = p.s[i];
-        NsMaps &m = maps.m[i];
+        NsMaps &m = to->maps.m[i];
         s = shape_of(b.s[i], w.pair, groups, w.steps, cv, &at);
         MOE_TRY(maps_of(b.s[i].x, s.matrices, s.rows, s.ld, &m.x_k[0], &m.x_mn[0]));
         MOE_TRY(maps_of(at.x, s.slots, s.rows, s.ld, &m.x_k[1], &m.x_mn[1]));
         for (int j = 0; j < symmetric_of(s.together); ++j) MOE_TRY(maps_of(at.s[j], s.slots, s.M, s.Mld, &m.s_k[j], &m.s_mn[j]));
-        total += (int64_t)s.matrices * tiles_of_matrix(s, w.steps);
+        to->tiles += (int64_t)s.matrices * tiles_of_matrix(s, w.steps);
         p.turns = (int32_t)imax(p.turns, s.turns);
         p.groups = (int32_t)imax(p.groups, cdiv(s.matrices, s.group));
     }
-    if (total > (int64_t)1 << 30) return MOE_ERR_UNSUPPORTED;
+    if (to->tiles > (int64_t)1 << 30) return MOE_ERR_UNSUPPORTED;
     p.done = w.done; p.next = w.next; p.status = w.status; p.lr = w.lr; p.rates = w.rates;
-    return w.pair ? launch_ns<true>(maps, p, b, total, st) : launch_ns<false>(maps, p, b, total, st);
+    return w.pair ? launch_ns<true>(nullptr, nullptr, nullptr) : launch_ns<false>(nullptr, nullptr, nullptr);
 }
+
+int32_t launch_newton_schulz(const NsLaunch &l, const MuonBatch &batch, cudaStream_t st) { return l.pair ? launch_ns<true>(&l, &batch, st) : launch_ns<false>(&l, &batch, st); }
 
 }  // namespace moe
