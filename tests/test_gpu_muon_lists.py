@@ -22,7 +22,7 @@ def test_alone_and_together(shapes, steps):
 
 
 def test_a_square_matrix_beside_wide_ones():
-    """Off by what it is off alone: in segments of three steps it would be 2.5 times as much."""
+    """Off by what it is off alone: in segments of two and three steps it would be 2.8 times as much (8.9e-4 and 2.5e-3 of X, every rounding simulated in 64 bits)."""
     t = [tensor((2, 512, 512), seed=1), tensor((20, 512, 2048), seed=2)]
     before, alone = copies(t), copies(t[:1])
     step(t)
