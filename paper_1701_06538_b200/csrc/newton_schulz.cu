@@ -9,7 +9,8 @@
 // simulation, one by one / 3 and 2 / 2 and 3: 7.5e-4, 1.4e-3, 5.7e-4 for momentum with gradients of 20 to 90 rows; 7e-4, 7e-4, 5e-4 for normal numbers; 3.6e-3, 2.7e-3, 9.9e-3 for singular
 // values spread evenly over two powers of ten.) Four or five steps in one segment would leave fp16's range: Q reaches 3.4445^n.
 //
-// Bound by the tensor cores, which run against the power limit here (990 W; 1965 MHz become 1300 to 1500). All M x M matrices are symmetric: the lower half is made, by tiles, and what
+// Bound by results (a pair's tile of 512 x 1024: 7500 cycles, products 4500) and in long lists by the power limit too (990 W; 1965 MHz become 1300 to 1500): 593 TFLOP/s of the operations that are needed for
+// 512 of 512 x 1024, 1007 for 64 of 1024 x 4096, where a plain product holds 1402. Every M x M matrix goes through L2 as a result, as an operand and as what is added. All M x M matrices are symmetric: the lower half is made, by tiles, and what
 // reads a tile of the upper half reads the stored one in its place, transposed by the operand's major-ness, which an instruction has of its own.
 //
 // Operands are fp16, not bf16: a step multiplies small singular values by 3.4 and what rounding has put beside them too. X over its Frobenius norm and everything made of it stay
